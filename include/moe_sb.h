@@ -37,7 +37,9 @@ enum {
     MOE_ERR_TOO_LARGE = -5    /* the problem needs more scratch memory than the library's static array holds */
 };
 
-enum { MOE_DTYPE_BF16 = 0, MOE_DTYPE_FP8_E4M3 = 1 };
+/* (FP32 and MX4 are types of the router's logits, of what is quantised and of the weights of moe_layer_few_tokens; the products over
+ * [E][K][N] weights take BF16 and FP8_E4M3.) */
+enum { MOE_DTYPE_BF16 = 0, MOE_DTYPE_FP8_E4M3 = 1, MOE_DTYPE_FP32 = 2, MOE_DTYPE_MX4 = 3 };
 
 /* Storage order of the expert weights (moe_gemm_desc.w_layout).  KN is the layout of the problem statement:
  * W[e][k][n], n contiguous.  NK is a pre-packed alternative, W[e][n][k], k contiguous (the order in which
@@ -457,6 +459,122 @@ int64_t moe_reduce_task_tiles(int T, int N);
  */
 int moe_grouped_gemm_batched(const void* X, const void* W, const void* task_map, void* Y, const moe_gemm_desc* desc,
                              const moe_reduce_task* red, void* stream);
+
+/*
+ * The router: from a token's logits over the experts to its k experts and their weights, what the calls above take as
+ * topk_ids and topk_weights.
+ *   logits        DEVICE [T][E] fp32 or bf16, rows row_stride elements apart (>= E)
+ *   topk_ids      DEVICE int32 [T, k]: the experts of the k largest logits in falling order, equal logits by rising index
+ *                 (NaN counts as larger than every number, +0 and -0 as equal)
+ *   topk_weights  DEVICE fp32 [T, k]:  softmax p_e = exp(l_e - max) / sum over all E;  sigmoid p_e = 1 / (1 + exp(-l_e));
+ *                 with `renormalize` divided by their sum over the k chosen ones (0 where that is 0); times `scale`.
+ * An expert whose logit is -inf is masked: weight 0, chosen only where fewer than k are left.  A row of nothing but -inf has
+ * weights 0 (its ids are still experts, 0 .. k-1).  A NaN or +inf in a softmax row makes its weights NaN.
+ * 1 <= k <= E <= 1024, T*k <= 2^24, T = 0 does nothing; other types MOE_ERR_UNSUPPORTED.  Deterministic.
+ */
+enum { MOE_SCORE_SOFTMAX = 0, MOE_SCORE_SIGMOID = 1 };
+typedef struct moe_route_desc {
+    int32_t T, k, E;
+    int32_t dtype;        /* MOE_DTYPE_FP32 or MOE_DTYPE_BF16: type of the logits */
+    int64_t row_stride;   /* elements from one token's logits to the next one's */
+    int32_t score;        /* MOE_SCORE_* */
+    int32_t renormalize;  /* 0 or 1 */
+    float scale;
+} moe_route_desc;
+int moe_route(const void* logits, const moe_route_desc* desc, int32_t* topk_ids, float* topk_weights, void* stream);
+
+/*
+ * Values in 4 bits with a shared scale.  32 consecutive elements along K share a power of two 2^s, stored as the byte s + 127;
+ * an element is a sign bit (bit 3) and a code 0 .. 7 for the magnitudes 0, 0.5, 1, 1.5, 2, 3, 4, 6 (e2m1), and stands for
+ * +-magnitude * 2^s.  Quantisation: s = floor(log2 a) - 2 with a the largest magnitude of the 32 (at least -127); x / 2^s goes
+ * to the nearest element, ties to the even code, and ends at 6.  A block with a NaN or an infinity gets the byte 255 and
+ * stands for NaN throughout.  Exact but for that rounding: the same input gives the same bytes.
+ *
+ * Token rows:
+ *   src     DEVICE [rows][cols] fp32 or bf16, rows row_stride elements apart (>= cols), any alignment of its type
+ *   codes   DEVICE [rows][Kp / 2] bytes, Kp = cols rounded up to 128; element 2 i in the low half of byte i; 16-byte aligned
+ *   scales  DEVICE [rows][Kp / 32] bytes; 4-byte aligned.  Elements beyond cols are written as zeros.
+ *   values  DEVICE bf16 [rows][cols], or NULL: what the codes stand for (exact)
+ * rows * Kp < 2^35, else MOE_ERR_UNSUPPORTED.
+ */
+int moe_mx4_quantize(const void* src, int dtype, int64_t rows, int cols, int64_t row_stride, void* codes, void* scales, void* values, void* stream);
+/* Bytes of the two buffers (HOST, pure; 0 on invalid arguments). */
+size_t moe_mx4_row_code_bytes(int64_t rows, int cols);
+size_t moe_mx4_row_scale_bytes(int64_t rows, int cols);
+
+/*
+ * Expert weights: the same with blocks along K, laid out for the matrix instructions in tiles of 64 columns x 128 k (a tile
+ * is 4 KB of codes and 256 bytes of scales in one piece; columns and K are padded with zeros to whole tiles).
+ *   W       DEVICE [E][K][N] (MOE_W_LAYOUT_KN) or [E][N][K] (MOE_W_LAYOUT_NK), fp32 or bf16, contiguous
+ *   gated   1: N = [gate | up] halves; the packed columns alternate units of 16 gate columns and the 16 up columns of the same
+ *           outputs (N / 2 padded to 16), which is what a product with the gated activation takes.  0: columns in order.
+ *   codes   DEVICE, moe_mx4_weight_code_bytes(E, K, N, gated) bytes, 16-byte aligned; expert e at e / E of it
+ *   scales  DEVICE, moe_mx4_weight_scale_bytes(E, K, N, gated) bytes, 16-byte aligned; likewise
+ *   values  DEVICE bf16 in W's layout, or NULL: what the codes stand for (exact)
+ * Experts may be packed one by one: E = 1 and the pointers moved on.
+ * E <= 1024 and less than 2^24 tiles in one call, else MOE_ERR_UNSUPPORTED.
+ */
+int moe_mx4_pack_weights(const void* W, int dtype, int w_layout, int E, int K, int N, int gated, void* codes, void* scales, void* values, void* stream);
+/* HOST, pure; 0 on invalid or unsupported arguments. */
+size_t moe_mx4_weight_code_bytes(int E, int K, int N, int gated);
+size_t moe_mx4_weight_scale_bytes(int E, int K, int N, int gated);
+/* Packed columns of a weight of N columns: N, or 2 * (N / 2 rounded up to 16).  HOST, pure; 0 on invalid arguments. */
+int64_t moe_mx4_packed_columns(int N, int gated);
+
+/*
+ * The statically batched expert product over 4-bit tokens and 4-bit weights:
+ *     Y[t, j, :] = X[t, :] . W[e(t,j), :, :]        gated: Y[t, j, i] = silu(gate_i) * up_i,  Y is [T, k, N / 2]
+ *   x_codes, x_scales  what moe_mx4_quantize made of X [T][K]
+ *   w_codes, w_scales  what moe_mx4_pack_weights made of W, with the same `gated`
+ *   task_map           built for the routing with N = moe_mx4_packed_columns(N, gated) and this tile_m, tile_n, ascending or
+ *                      any other order, one strategy, no slack rows
+ *   Y                  DEVICE bf16, 16-byte aligned, written once per element
+ * Sums are fp32, the gated activation is fp32, one rounding to bf16.  Any K >= 1 and N >= 1.  A map that does not match `desc`,
+ * or whose status is non-zero, makes the kernel a no-op.  Tiles: moe_mx4_tile_supported; others MOE_ERR_UNSUPPORTED.
+ */
+typedef struct moe_mx4_gemm_desc {
+    int32_t T, k, E, K, N;
+    int32_t gated;
+    int32_t tile_m, tile_n;
+} moe_mx4_gemm_desc;
+int moe_mx4_grouped_gemm(const void* x_codes, const void* x_scales, const void* w_codes, const void* w_scales, const void* task_map, void* Y,
+                         const moe_mx4_gemm_desc* desc, void* stream);
+/* 1 if moe_mx4_grouped_gemm has a kernel for this tile, else 0.  HOST, pure. */
+int moe_mx4_tile_supported(int tile_m, int tile_n);
+/* A reasonable tiling for these sizes (HOST, pure); MOE_ERR_INVALID_ARG on bad arguments. */
+int moe_mx4_default_tiling(int T, int k, int E, int K, int N, int gated, moe_tiling* out);
+
+/*
+ * A whole layer for at most 16 tokens, in two launches and without a task map:
+ *     topk_ids, topk_weights = moe_route(logits)
+ *     h[t, j] = silu(X[t] . W_gate[e]) * (X[t] . W_up[e]),  e = topk_ids[t, j]
+ *     out[t]  = sum_j topk_weights[t, j] * (h[t, j] . W_down[e])
+ *   X        DEVICE bf16 [T][hidden], 16-byte aligned
+ *   logits   DEVICE [T][E], of logits_dtype, contiguous
+ *   w_up     w_dtype BF16: DEVICE [E][hidden][2 inter], gate columns first.  MX4: codes of moe_mx4_pack_weights(K = hidden,
+ *            N = 2 inter, gated = 1), up_scales its scales.  Activations are bf16 either way.
+ *   w_down   BF16: DEVICE [E][inter][hidden].  MX4: codes for K = inter, N = hidden, gated = 0; down_scales its scales.
+ *            All 16-byte aligned; up_scales and down_scales are not looked at for BF16.
+ *   topk_ids, topk_weights   DEVICE int32 / fp32 [T, k], written
+ *   out      DEVICE bf16 [T][hidden]
+ *   workspace  DEVICE, 16-byte aligned, at least moe_few_tokens_workspace_bytes(desc) bytes, contents undefined before and after;
+ *            calls that share one must not overlap.
+ * Sums are fp32; h is rounded to bf16 once, out once.  A token is not touched by what is in the weights of experts that it did not
+ * choose, nor by other tokens.  Deterministic.
+ * T <= 16, k <= 16, hidden a multiple of 8 (BF16: inter too), both at most 2^20, else MOE_ERR_UNSUPPORTED; limits of moe_route.
+ */
+typedef struct moe_few_tokens_desc {
+    int32_t T, k, E, hidden, inter;
+    int32_t w_dtype;       /* MOE_DTYPE_BF16 or MOE_DTYPE_MX4 */
+    int32_t logits_dtype;  /* MOE_DTYPE_FP32 or MOE_DTYPE_BF16 */
+    int32_t score, renormalize;
+    float scale;
+} moe_few_tokens_desc;
+int moe_layer_few_tokens(const void* X, const void* logits, const void* w_up, const void* up_scales, const void* w_down, const void* down_scales,
+                         const moe_few_tokens_desc* desc, int32_t* topk_ids, float* topk_weights, void* out, void* workspace, size_t workspace_bytes,
+                         void* stream);
+/* HOST, pure; 0 on invalid or unsupported arguments and for T = 0. */
+size_t moe_few_tokens_workspace_bytes(const moe_few_tokens_desc* desc);
 
 /* Static string for a return code. */
 const char* moe_strerror(int code);

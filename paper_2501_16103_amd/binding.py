@@ -26,10 +26,14 @@ MOE_ERR_HIP = -4
 MOE_ERR_TOO_LARGE = -5
 MOE_DTYPE_BF16 = 0
 MOE_DTYPE_FP8_E4M3 = 1
+MOE_DTYPE_FP32 = 2
+MOE_DTYPE_MX4 = 3
 MOE_W_LAYOUT_KN = 0
 MOE_W_LAYOUT_NK = 1
 MOE_EPILOGUE_NONE = 0
 MOE_EPILOGUE_SWIGLU = 1
+MOE_SCORE_SOFTMAX = 0
+MOE_SCORE_SIGMOID = 1
 MOE_ORDER_ASCENDING = 0
 MOE_ORDER_SPREAD = 1
 MOE_ORDER_INTERLEAVE = 2
@@ -61,6 +65,9 @@ EXPORTS = [
     "moe_grouped_gemm_splitk", "moe_splitk_workspace_bytes", "moe_default_k_parts",
     "moe_grouped_gemm_splitk_static", "moe_splitk_static_scratch_bytes",
     "moe_grouped_gemm_batched", "moe_reduce_task_tiles", "moe_grouped_gemm_tail_split", "moe_tail_split_workspace_bytes", "moe_default_tail_split",
+    "moe_route", "moe_mx4_quantize", "moe_mx4_row_code_bytes", "moe_mx4_row_scale_bytes", "moe_mx4_pack_weights",
+    "moe_mx4_weight_code_bytes", "moe_mx4_weight_scale_bytes", "moe_mx4_packed_columns", "moe_mx4_grouped_gemm",
+    "moe_mx4_tile_supported", "moe_mx4_default_tiling", "moe_layer_few_tokens", "moe_few_tokens_workspace_bytes",
     "moe_strerror",
 ]
 
@@ -89,6 +96,20 @@ class moe_tiling(ctypes.Structure):
     _fields_ = [("tile_m", ctypes.c_int32), ("tile_n", ctypes.c_int32), ("order", ctypes.c_int32),
                 ("tile_m_small", ctypes.c_int32), ("small_max_rows", ctypes.c_int32),
                 ("tile_m_slack", ctypes.c_int32)]
+
+
+class moe_route_desc(ctypes.Structure):
+    _fields_ = [("T", ctypes.c_int32), ("k", ctypes.c_int32), ("E", ctypes.c_int32), ("dtype", ctypes.c_int32),
+                ("row_stride", ctypes.c_int64), ("score", ctypes.c_int32), ("renormalize", ctypes.c_int32), ("scale", ctypes.c_float)]
+
+
+class moe_mx4_gemm_desc(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("T", "k", "E", "K", "N", "gated", "tile_m", "tile_n")]
+
+
+class moe_few_tokens_desc(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("T", "k", "E", "hidden", "inter", "w_dtype", "logits_dtype", "score", "renormalize")] + [
+        ("scale", ctypes.c_float)]
 
 
 _lib = None
@@ -174,6 +195,31 @@ def lib() -> ctypes.CDLL:
         L.moe_splitk_workspace_bytes.argtypes = [ctypes.c_int] * 4
         L.moe_default_k_parts.restype = ctypes.c_int
         L.moe_default_k_parts.argtypes = [ctypes.c_int] * 5
+        L.moe_route.restype = ctypes.c_int
+        L.moe_route.argtypes = [ctypes.c_void_p, ctypes.POINTER(moe_route_desc)] + [ctypes.c_void_p] * 3
+        L.moe_mx4_quantize.restype = ctypes.c_int
+        L.moe_mx4_quantize.argtypes = [ctypes.c_void_p, ctypes.c_int, ctypes.c_int64, ctypes.c_int, ctypes.c_int64] + [ctypes.c_void_p] * 4
+        for n in ("moe_mx4_row_code_bytes", "moe_mx4_row_scale_bytes"):
+            getattr(L, n).restype = ctypes.c_size_t
+            getattr(L, n).argtypes = [ctypes.c_int64, ctypes.c_int]
+        L.moe_mx4_pack_weights.restype = ctypes.c_int
+        L.moe_mx4_pack_weights.argtypes = [ctypes.c_void_p] + [ctypes.c_int] * 6 + [ctypes.c_void_p] * 4
+        for n in ("moe_mx4_weight_code_bytes", "moe_mx4_weight_scale_bytes"):
+            getattr(L, n).restype = ctypes.c_size_t
+            getattr(L, n).argtypes = [ctypes.c_int] * 4
+        L.moe_mx4_packed_columns.restype = ctypes.c_int64
+        L.moe_mx4_packed_columns.argtypes = [ctypes.c_int] * 2
+        L.moe_mx4_grouped_gemm.restype = ctypes.c_int
+        L.moe_mx4_grouped_gemm.argtypes = [ctypes.c_void_p] * 6 + [ctypes.POINTER(moe_mx4_gemm_desc), ctypes.c_void_p]
+        L.moe_mx4_tile_supported.restype = ctypes.c_int
+        L.moe_mx4_tile_supported.argtypes = [ctypes.c_int] * 2
+        L.moe_mx4_default_tiling.restype = ctypes.c_int
+        L.moe_mx4_default_tiling.argtypes = [ctypes.c_int] * 6 + [ctypes.POINTER(moe_tiling)]
+        L.moe_layer_few_tokens.restype = ctypes.c_int
+        L.moe_layer_few_tokens.argtypes = [ctypes.c_void_p] * 6 + [ctypes.POINTER(moe_few_tokens_desc)] + [ctypes.c_void_p] * 4 + [
+            ctypes.c_size_t, ctypes.c_void_p]
+        L.moe_few_tokens_workspace_bytes.restype = ctypes.c_size_t
+        L.moe_few_tokens_workspace_bytes.argtypes = [ctypes.POINTER(moe_few_tokens_desc)]
         L.moe_strerror.restype = ctypes.c_char_p
         L.moe_strerror.argtypes = [ctypes.c_int]
         _lib = L
@@ -469,6 +515,208 @@ def moe_grouped_gemm_splitk_static(X: torch.Tensor, W: torch.Tensor, task_map: t
     if check and rc != MOE_OK:
         raise MoeError(rc, "moe_grouped_gemm_splitk_static")
     return rc
+
+
+_DTYPES = {torch.bfloat16: MOE_DTYPE_BF16, torch.float32: MOE_DTYPE_FP32}
+
+
+def _dtype(t: torch.Tensor) -> int:
+    """The library's number for a tensor's type; -1, which every call refuses, for one it does not know."""
+    return _DTYPES.get(t.dtype, -1)
+
+
+def moe_route(logits: torch.Tensor, k: int, topk_ids: torch.Tensor, topk_weights: torch.Tensor, score: int = MOE_SCORE_SOFTMAX,
+              renormalize: bool = True, scale: float = 1.0, check: bool = True) -> int:
+    """logits [T, E], fp32 or bf16, rows of consecutive elements -> topk_ids int32 [T, k], topk_weights fp32 [T, k]."""
+    T, E = logits.shape
+    d = moe_route_desc(T, k, E, _dtype(logits), logits.stride(0), score, int(renormalize), scale)
+    rc = MOE_ERR_INVALID_ARG if E > 1 and logits.stride(1) != 1 else lib().moe_route(_ptr(logits), ctypes.byref(d), _ptr(topk_ids),
+                                                                                     _ptr(topk_weights), _stream())
+    if check and rc != MOE_OK:
+        raise MoeError(rc, "moe_route")
+    return rc
+
+
+def moe_mx4_quantize(src: torch.Tensor, codes: torch.Tensor, scales: torch.Tensor, values: Optional[torch.Tensor] = None, check: bool = True) -> int:
+    """src [rows, cols], fp32 or bf16, rows of consecutive elements; `values` bf16 [rows, cols], contiguous."""
+    rows, cols = src.shape
+    rc = MOE_ERR_INVALID_ARG if cols > 1 and src.stride(1) != 1 else lib().moe_mx4_quantize(
+        _ptr(src), _dtype(src), rows, cols, src.stride(0), _ptr(codes), _ptr(scales), _ptr(values), _stream())
+    if check and rc != MOE_OK:
+        raise MoeError(rc, "moe_mx4_quantize")
+    return rc
+
+
+def moe_mx4_row_code_bytes(rows: int, cols: int) -> int:
+    return int(lib().moe_mx4_row_code_bytes(rows, cols))
+
+
+def moe_mx4_row_scale_bytes(rows: int, cols: int) -> int:
+    return int(lib().moe_mx4_row_scale_bytes(rows, cols))
+
+
+def moe_mx4_pack_weights(W: torch.Tensor, w_layout: int, E: int, K: int, N: int, gated: bool, codes, scales, values: Optional[torch.Tensor] = None,
+                         check: bool = True) -> int:
+    """W [E, K, N] or [E, N, K], contiguous; `codes`, `scales`: tensors or device addresses."""
+    at = [p if isinstance(p, int) else _ptr(p) for p in (codes, scales)]
+    rc = lib().moe_mx4_pack_weights(_ptr(W), _dtype(W), w_layout, E, K, N, int(gated), *at, _ptr(values), _stream())
+    if check and rc != MOE_OK:
+        raise MoeError(rc, "moe_mx4_pack_weights")
+    return rc
+
+
+def moe_mx4_weight_code_bytes(E: int, K: int, N: int, gated: bool = False) -> int:
+    return int(lib().moe_mx4_weight_code_bytes(E, K, N, int(gated)))
+
+
+def moe_mx4_weight_scale_bytes(E: int, K: int, N: int, gated: bool = False) -> int:
+    return int(lib().moe_mx4_weight_scale_bytes(E, K, N, int(gated)))
+
+
+def moe_mx4_packed_columns(N: int, gated: bool = False) -> int:
+    return int(lib().moe_mx4_packed_columns(N, int(gated)))
+
+
+def moe_mx4_tile_supported(tile_m: int, tile_n: int) -> bool:
+    return bool(lib().moe_mx4_tile_supported(tile_m, tile_n))
+
+
+def moe_mx4_default_tiling(T: int, k: int, E: int, K: int, N: int, gated: bool = False) -> Tiling:
+    g = moe_tiling()
+    rc = lib().moe_mx4_default_tiling(T, k, E, K, N, int(gated), ctypes.byref(g))
+    if rc != MOE_OK:
+        raise MoeError(rc, "moe_mx4_default_tiling")
+    return Tiling(g.tile_m, g.tile_n, g.order, g.tile_m_small, g.small_max_rows, g.tile_m_slack)
+
+
+def _contiguous(where: str, t: torch.Tensor, shape: tuple, dtype: Optional[torch.dtype] = None) -> None:
+    """The classes below take tensors whose sizes the C entry points cannot see: what does not fit is refused here."""
+    if tuple(t.shape) != shape or not t.is_contiguous() or (dtype is not None and t.dtype != dtype):
+        raise MoeError(MOE_ERR_INVALID_ARG, where)
+
+
+class Mx4Rows:
+    """Up to `rows` token rows of `cols` elements in 4 bits: the buffers that moe_mx4_quantize fills."""
+
+    def __init__(self, rows: int, cols: int, device="cuda:0"):
+        self.rows, self.cols = rows, cols
+        sizes = moe_mx4_row_code_bytes(rows, cols), moe_mx4_row_scale_bytes(rows, cols)
+        if rows < 0 or (rows > 0 and 0 in sizes):
+            raise MoeError(MOE_ERR_INVALID_ARG, "moe_mx4_row_code_bytes")
+        self.codes, self.scales = (torch.empty(n, dtype=torch.uint8, device=device) for n in sizes)
+
+    def quantize(self, src: torch.Tensor, values: Optional[torch.Tensor] = None) -> "Mx4Rows":
+        if src.dim() != 2 or src.shape[0] > self.rows or src.shape[1] != self.cols:
+            raise MoeError(MOE_ERR_INVALID_ARG, "Mx4Rows.quantize")
+        if values is not None:
+            _contiguous("Mx4Rows.quantize", values, tuple(src.shape), torch.bfloat16)
+        moe_mx4_quantize(src, self.codes, self.scales, values)
+        return self
+
+
+class Mx4Weights:
+    """The weights [K, N] of E experts in 4 bits, as the products take them.  gated: N = [gate | up] halves."""
+
+    def __init__(self, E: int, K: int, N: int, gated: bool = False, device="cuda:0"):
+        self.E, self.K, self.N, self.gated = E, K, N, bool(gated)
+        nbytes = moe_mx4_weight_code_bytes(E, K, N, gated)
+        if nbytes == 0:
+            raise MoeError(MOE_ERR_INVALID_ARG, "moe_mx4_weight_code_bytes")
+        self.codes = torch.empty(nbytes, dtype=torch.uint8, device=device)
+        self.scales = torch.empty(moe_mx4_weight_scale_bytes(E, K, N, gated), dtype=torch.uint8, device=device)
+
+    def pack(self, W: torch.Tensor, w_layout: int = MOE_W_LAYOUT_KN, values: Optional[torch.Tensor] = None) -> "Mx4Weights":
+        """W [E, K, N] (or [E, N, K] with MOE_W_LAYOUT_NK), bf16 or fp32; `values`: bf16, of W's shape."""
+        _contiguous("Mx4Weights.pack", W, (self.E, self.N, self.K) if w_layout == MOE_W_LAYOUT_NK else (self.E, self.K, self.N))
+        if values is not None:
+            _contiguous("Mx4Weights.pack", values, tuple(W.shape), torch.bfloat16)
+        moe_mx4_pack_weights(W, w_layout, self.E, self.K, self.N, self.gated, self.codes, self.scales, values)
+        return self
+
+    def pack_expert(self, e: int, W: torch.Tensor, w_layout: int = MOE_W_LAYOUT_KN) -> "Mx4Weights":
+        """One expert's weight, [K, N] or [N, K]: for layers whose full-size weights do not fit beside each other."""
+        _contiguous("Mx4Weights.pack_expert", W, (self.N, self.K) if w_layout == MOE_W_LAYOUT_NK else (self.K, self.N))
+        if not 0 <= e < self.E:
+            raise MoeError(MOE_ERR_INVALID_ARG, "Mx4Weights.pack_expert")
+        at = [_ptr(b) + e * (b.numel() // self.E) for b in (self.codes, self.scales)]
+        moe_mx4_pack_weights(W, w_layout, 1, self.K, self.N, self.gated, *at)
+        return self
+
+
+def moe_mx4_grouped_gemm(X: Mx4Rows, W: Mx4Weights, T: int, k: int, task_map: torch.Tensor, Y: torch.Tensor, tiling: Tiling, check: bool = True) -> int:
+    d = moe_mx4_gemm_desc(T, k, W.E, W.K, W.N, int(W.gated), tiling.tile_m, tiling.tile_n)
+    rc = lib().moe_mx4_grouped_gemm(_ptr(X.codes), _ptr(X.scales), _ptr(W.codes), _ptr(W.scales), _ptr(task_map), _ptr(Y), ctypes.byref(d), _stream())
+    if check and rc != MOE_OK:
+        raise MoeError(rc, "moe_mx4_grouped_gemm")
+    return rc
+
+
+class MoeMx4ProductPlan:
+    """Buffers and tiling of one product over 4-bit experts: quantise the tokens -> task map -> product, on the current stream.
+    gated: the experts' weights are [gate | up] halves and the product ends with the gated activation."""
+
+    def __init__(self, T: int, k: int, E: int, K: int, N: int, gated: bool = False, device="cuda:0"):
+        self.T, self.k, self.E, self.K, self.N, self.gated = T, k, E, K, N, bool(gated)
+        self.g = moe_mx4_default_tiling(T, k, E, K, N, gated)
+        self.columns = moe_mx4_packed_columns(N, gated)
+        self.map = alloc_task_map(T, k, E, self.g.tile_m, self.g.tile_n, self.columns, device)
+        self.rows = Mx4Rows(T, K, device)
+        self.out = torch.empty((T, k, N // 2 if gated else N), dtype=torch.bfloat16, device=device)
+
+    def forward(self, X: torch.Tensor, W: Mx4Weights, topk_ids: torch.Tensor) -> torch.Tensor:
+        """X [T, K] bf16 or fp32; topk_ids int32 [T, k].  Returns out [T, k, N or N / 2] (the plan's buffer)."""
+        if (W.E, W.K, W.N, W.gated) != (self.E, self.K, self.N, self.gated) or tuple(X.shape) != (self.T, self.K):
+            raise MoeError(MOE_ERR_INVALID_ARG, "MoeMx4ProductPlan.forward")
+        _contiguous("MoeMx4ProductPlan.forward", topk_ids, (self.T, self.k), torch.int32)
+        if self.T == 0:
+            return self.out
+        moe_build_task_map_ex(topk_ids, self.T, self.k, self.E, self.columns, self.g, self.map)
+        self.rows.quantize(X)
+        moe_mx4_grouped_gemm(self.rows, W, self.T, self.k, self.map, self.out, self.g)
+        return self.out
+
+
+class MoeFewTokensPlan:
+    """Buffers of moe_layer_few_tokens: one whole layer for at most 16 tokens, over bf16 weights ([E, hidden, 2 inter] and
+    [E, inter, hidden]) or over 4-bit ones (Mx4Weights, the first of them gated)."""
+
+    def __init__(self, T: int, k: int, E: int, hidden: int, inter: int, score: int = MOE_SCORE_SOFTMAX, renormalize: bool = True,
+                 scale: float = 1.0, device="cuda:0"):
+        self.T, self.k, self.E, self.hidden, self.inter = T, k, E, hidden, inter
+        self.score, self.renormalize, self.scale = score, renormalize, scale
+        self.ids = torch.empty((T, k), dtype=torch.int32, device=device)
+        self.weights = torch.empty((T, k), dtype=torch.float32, device=device)
+        self.out = torch.empty((T, hidden), dtype=torch.bfloat16, device=device)
+        sizes = [int(lib().moe_few_tokens_workspace_bytes(ctypes.byref(self._desc(dt, MOE_DTYPE_FP32)))) for dt in (MOE_DTYPE_BF16, MOE_DTYPE_MX4)]
+        if T > 0 and max(sizes) == 0:
+            raise MoeError(MOE_ERR_UNSUPPORTED, "moe_few_tokens_workspace_bytes")
+        self.workspace = torch.empty(max(sizes), dtype=torch.uint8, device=device)
+
+    def _desc(self, w_dtype: int, logits_dtype: int) -> moe_few_tokens_desc:
+        return moe_few_tokens_desc(self.T, self.k, self.E, self.hidden, self.inter, w_dtype, logits_dtype, self.score, int(self.renormalize), self.scale)
+
+    def forward(self, X: torch.Tensor, logits: torch.Tensor, W_gate_up, W_down) -> tuple:
+        """X bf16 [T, hidden]; logits [T, E], fp32 or bf16.  Returns (out [T, hidden], topk_ids [T, k], topk_weights [T, k]), the
+        plan's buffers."""
+        where = "MoeFewTokensPlan.forward"
+        _contiguous(where, X, (self.T, self.hidden), torch.bfloat16)
+        _contiguous(where, logits, (self.T, self.E))
+        mx4 = isinstance(W_gate_up, Mx4Weights)
+        if mx4:
+            if not isinstance(W_down, Mx4Weights) or (W_gate_up.E, W_gate_up.K, W_gate_up.N, W_gate_up.gated) != (self.E, self.hidden, 2 * self.inter, True) or (
+                    W_down.E, W_down.K, W_down.N, W_down.gated) != (self.E, self.inter, self.hidden, False):
+                raise MoeError(MOE_ERR_INVALID_ARG, where)
+            weights = (_ptr(W_gate_up.codes), _ptr(W_gate_up.scales), _ptr(W_down.codes), _ptr(W_down.scales))
+        else:
+            _contiguous(where, W_gate_up, (self.E, self.hidden, 2 * self.inter), torch.bfloat16)
+            _contiguous(where, W_down, (self.E, self.inter, self.hidden), torch.bfloat16)
+            weights = (_ptr(W_gate_up), None, _ptr(W_down), None)
+        d = self._desc(MOE_DTYPE_MX4 if mx4 else MOE_DTYPE_BF16, _dtype(logits))
+        rc = lib().moe_layer_few_tokens(_ptr(X), _ptr(logits), *weights, ctypes.byref(d), _ptr(self.ids), _ptr(self.weights), _ptr(self.out),
+                                        _ptr(self.workspace), self.workspace.numel(), _stream())
+        if rc != MOE_OK:
+            raise MoeError(rc, "moe_layer_few_tokens")
+        return self.out, self.ids, self.weights
 
 
 class MoeLayerPlan:

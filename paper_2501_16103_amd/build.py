@@ -9,13 +9,13 @@ import tempfile
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 LIB = os.path.join(HERE, "libmoe_sb.so")
-SRC = os.path.join(HERE, "csrc", "moe_sb.hip")
+SRCS = [os.path.join(HERE, "csrc", f) for f in ("moe_sb.hip", "moe_mx4.hip")]
 # measurement kernels, kept out of the product library
 PROBE_LIB = os.path.join(HERE, "libmoe_probe.so")
-PROBE_SRC = os.path.join(HERE, "csrc", "moe_probe.hip")
+PROBE_SRCS = [os.path.join(HERE, "csrc", "moe_probe.hip")]
 
 HIPCC_FLAGS = [
-    "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-shared",
+    "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC",
     # packed-FP32 instructions are switched off for all device code
     "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
     # The k loops are unrolled completely by pragma; at the default size limit for pragma-unrolled loops the largest
@@ -135,37 +135,47 @@ def check_mfma_operand_distance(asm_text: str) -> None:
                 todo += [(q, waited) for q in before(p)]
 
 
-def _compile(src: str, lib: str, check_asm: bool, verbose: bool) -> str:
+def _compile(srcs: list, lib: str, check_asm: bool, verbose: bool) -> str:
     hipcc = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
     with tempfile.TemporaryDirectory() as tmp:
-        out = os.path.join(tmp, os.path.basename(lib))
-        cmd = [hipcc] + HIPCC_FLAGS + ["-save-temps=obj", src, "-o", out]
+        jobs = []
+        for src in srcs:   # side by side, each in a folder of its own for the files it leaves
+            out = os.path.join(tmp, os.path.splitext(os.path.basename(src))[0])
+            os.mkdir(out)
+            cmd = [hipcc] + HIPCC_FLAGS + ["-save-temps=obj", "-c", src, "-o", os.path.join(out, "out.o")]
+            jobs.append((out, cmd, subprocess.Popen(cmd, cwd=out, stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)))
+        logs = [job.communicate()[0] for _, _, job in jobs]   # (all of them end before the folder goes)
+        for (out, cmd, job), log in zip(jobs, logs):
+            if job.returncode != 0:
+                raise RuntimeError("hipcc failed:\n" + log)
+            if check_asm:
+                asm = [f for f in os.listdir(out) if f.endswith(".s") and "amdgcn" in f]
+                if not asm:
+                    raise RuntimeError("no device assembly found next to the object file")
+                with open(os.path.join(out, asm[0])) as f:
+                    asm_text = f.read()
+                check_no_spill_in_k_loops(asm_text)
+                check_mfma_operand_distance(asm_text)
+            if verbose:
+                print(" ".join(cmd))
+        linked = os.path.join(tmp, os.path.basename(lib))
+        cmd = [hipcc, "--offload-arch=gfx950", "-shared", "-fPIC"] + [os.path.join(out, "out.o") for out, _, _ in jobs] + ["-o", linked]
         res = subprocess.run(cmd, cwd=tmp, capture_output=True, text=True)
         if res.returncode != 0:
-            raise RuntimeError("hipcc failed:\n" + res.stdout + res.stderr)
-        if check_asm:
-            asm = [f for f in os.listdir(tmp) if f.endswith(".s") and "amdgcn" in f]
-            if not asm:
-                raise RuntimeError("no device assembly found next to the built library")
-            with open(os.path.join(tmp, asm[0])) as f:
-                asm_text = f.read()
-            check_no_spill_in_k_loops(asm_text)
-            check_mfma_operand_distance(asm_text)
-        shutil.copyfile(out, lib)
+            raise RuntimeError("linking failed:\n" + res.stdout + res.stderr)
+        shutil.copyfile(linked, lib)
         os.chmod(lib, 0o755)
-    if verbose:
-        print(" ".join(cmd))
     return lib
 
 
 def build_library(verbose: bool = False) -> str:
     """libmoe_sb.so: the product library."""
-    return _compile(SRC, LIB, True, verbose)
+    return _compile(SRCS, LIB, True, verbose)
 
 
 def build_probe_library(verbose: bool = False) -> str:
     """libmoe_probe.so: the measurement kernels (bench.py --mfma-probe and two tests load it)."""
-    return _compile(PROBE_SRC, PROBE_LIB, False, verbose)
+    return _compile(PROBE_SRCS, PROBE_LIB, False, verbose)
 
 
 if __name__ == "__main__":

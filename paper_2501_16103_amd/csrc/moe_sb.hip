@@ -10,8 +10,9 @@
 #include "../../include/moe_sb.h"
 #include "gemm_kernel.hpp"
 #include "combine.hpp"
+#include "launch_attr.hpp"
 #include "launch_rules.hpp"
-#include "task_map.hpp"
+#include "task_map_kernels.hpp"
 
 using namespace moe;
 
@@ -34,25 +35,10 @@ int check_map_args(int T, int k, int E, int tile_m, int tile_n, int N) {
     return MOE_OK;
 }
 
-// Guards the launch-attribute caches below (set once per kernel and device): calls may come from several host threads.
-std::mutex g_attr_lock;
-
 int nchunks_for(int64_t R) { return (int)((R + kChunkRows - 1) / kChunkRows); }
 
 // `mode` is moe_gemm_desc.launch_mode (only the launches that have a resident form look at it)
 typedef int (*gemm_launch_fn)(const GemmArgs&, int64_t grid, int mode, hipStream_t);
-
-// The large-LDS attribute of a kernel is set once per device (bit d of *done: device d, d < 64).
-inline int ensure_lds_attr(const void* fn, int lds, unsigned long long* done) {
-    std::lock_guard<std::mutex> hold(g_attr_lock);
-    int dev = 0;
-    if (hipGetDevice(&dev) != hipSuccess) return MOE_ERR_HIP;
-    const unsigned long long bit = dev >= 0 && dev < 64 ? 1ull << dev : 0;
-    if (bit && (*done & bit)) return MOE_OK;
-    if (hipFuncSetAttribute(fn, hipFuncAttributeMaxDynamicSharedMemorySize, lds) != hipSuccess) return MOE_ERR_HIP;
-    *done |= bit;
-    return MOE_OK;
-}
 
 template <class C, class... Tails>
 int launch_pipe(const GemmArgs& a, int64_t grid, int /*mode*/, hipStream_t s) {

@@ -1,0 +1,133 @@
+// The router's choice: from a token's logits over the experts to its k experts and their weights.
+//
+// ids[t][0 .. k) are the experts of the k largest logits in falling order, equal logits by rising index (a NaN counts as
+// larger than every number, +0 and -0 as equal).  Both scores rise with the logit, so the order needs none of them and is
+// the same however they are computed.  Weights are fp32:
+//   softmax  p_e = exp(l_e - max l) / sum over all experts;   sigmoid  p_e = 1 / (1 + exp(-l_e));
+// with `renormalize` divided by the sum over the k chosen ones; times `scale`.  An expert whose logit is -inf has
+// weight 0; a row of nothing else has weights 0 (its ids are 0 .. k-1: still experts, so the row can go on through the
+// layer and comes out as zeros).
+#pragma once
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include "mx4.hpp"
+
+namespace moe {
+
+struct RouteArgs {
+    const void* logits;
+    int64_t row_stride;
+    int T, E, k;
+    int sigmoid, renormalize;
+    float scale;
+};
+
+// Order of logits as unsigned integers: a larger logit has a larger key, NaN the largest, -0 is +0; 0 is below every logit.
+__device__ __forceinline__ uint32_t route_key(float x) {
+    const uint32_t b = __float_as_uint(x == 0.f ? 0.f : x);
+    if ((b & 0x7fffffffu) > 0x7f800000u) return 0xffffffffu;
+    return b & 0x80000000u ? ~b : b | 0x80000000u;
+}
+__device__ __forceinline__ float route_logit(uint32_t key) {   // the logit a key stands for
+    if (key == 0xffffffffu) return __uint_as_float(0x7fc00000u);
+    return __uint_as_float(key & 0x80000000u ? key & 0x7fffffffu : ~key);
+}
+
+__device__ __forceinline__ uint32_t wave_max_u32(uint32_t v) {
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) {
+        const uint32_t o = (uint32_t)__shfl_xor((int)v, d);
+        v = o > v ? o : v;
+    }
+    return v;
+}
+__device__ __forceinline__ float wave_sum(float v) {
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) v += __shfl_xor(v, d);
+    return v;
+}
+
+// One token by one wavefront.  EPL: logits per lane, expert 64 j + lane in slot j.  The i-th choice comes back in slot i / 64 of
+// lane i % 64: its expert and its weight (lanes past the k choices hold nothing of use).
+template <int EPL, class Src>
+__device__ __forceinline__ void route_token(const RouteArgs& a, int64_t t, int (&ids)[EPL], float (&weights)[EPL]) {
+    const int lane = __lane_id();
+    const Src* row = static_cast<const Src*>(a.logits) + t * a.row_stride;
+    uint32_t key[EPL];
+#pragma unroll
+    for (int j = 0; j < EPL; ++j) key[j] = 64 * j + lane < a.E ? route_key(mx4_load(row + 64 * j + lane)) : 0;
+    auto largest = [&]() {
+        uint32_t m = 0;
+#pragma unroll
+        for (int j = 0; j < EPL; ++j) m = key[j] > m ? key[j] : m;
+        return wave_max_u32(m);
+    };
+    uint32_t now = largest();
+    const float top = route_logit(now);
+    const bool empty = top == -__builtin_inff();
+    float total = 0.f;
+    if (!a.sigmoid && !empty) {
+#pragma unroll
+        for (int j = 0; j < EPL; ++j) total += key[j] != 0 ? expf(route_logit(key[j]) - top) : 0.f;
+        total = wave_sum(total);
+    }
+    uint32_t chosen[EPL];
+#pragma unroll
+    for (int s = 0; s < EPL; ++s) {
+        ids[s] = 0;
+        chosen[s] = 0;
+        const int end = a.k - 64 * s < 64 ? a.k - 64 * s : 64;
+        for (int i = 0; i < end; ++i) {
+            int e = -1;
+#pragma unroll
+            for (int j = 0; j < EPL; ++j) {
+                const unsigned long long at = __ballot(key[j] == now);
+                if (e < 0 && at != 0) {
+                    e = 64 * j + __builtin_ctzll(at);
+                    if (lane == __builtin_ctzll(at)) key[j] = 0;
+                }
+            }
+            if (lane == i) {
+                ids[s] = e;
+                chosen[s] = now;
+            }
+            now = largest();
+        }
+    }
+    float sum = 0.f;
+#pragma unroll
+    for (int s = 0; s < EPL; ++s) {
+        const float l = route_logit(chosen[s]);
+        float w = a.sigmoid ? 1.f / (1.f + expf(-l)) : empty ? 0.f : expf(l - top) / total;
+        if (64 * s + lane >= a.k) w = 0.f;
+        weights[s] = w;
+        sum += w;
+    }
+    if (a.renormalize) {
+        sum = wave_sum(sum);
+#pragma unroll
+        for (int s = 0; s < EPL; ++s) weights[s] = sum == 0.f ? 0.f : weights[s] / sum;
+    }
+#pragma unroll
+    for (int s = 0; s < EPL; ++s) weights[s] *= a.scale;
+}
+
+template <int EPL, class Src>
+__global__ __launch_bounds__(256) void route_kernel(RouteArgs a, int32_t* __restrict__ ids, float* __restrict__ weights) {
+    const int64_t t = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+    if (t >= a.T) return;
+    int id[EPL];
+    float w[EPL];
+    route_token<EPL, Src>(a, t, id, w);
+#pragma unroll
+    for (int s = 0; s < EPL; ++s) {
+        const int i = 64 * s + __lane_id();
+        if (i < a.k) {
+            ids[t * a.k + i] = id[s];
+            weights[t * a.k + i] = w[s];
+        }
+    }
+}
+
+}  // namespace moe
