@@ -529,7 +529,7 @@ int64_t moe_mx4_packed_columns(int N, int gated);
  *   task_map           built for the routing with N = moe_mx4_packed_columns(N, gated) and this tile_m, tile_n, ascending or
  *                      any other order, one strategy, no slack rows
  *   Y                  DEVICE bf16, 16-byte aligned, written once per element
- * Sums are fp32, the gated activation is fp32, one rounding to bf16.  Any K >= 1 and N >= 1.  A map that does not match `desc`,
+ * Sums are fp32, the gated activation is fp32, one rounding to bf16.  Any K >= 1 and N >= 1, x_codes of less than 4 GiB.  A map that does not match `desc`,
  * or whose status is non-zero, makes the kernel a no-op.  Tiles: moe_mx4_tile_supported; others MOE_ERR_UNSUPPORTED.
  */
 typedef struct moe_mx4_gemm_desc {

@@ -75,6 +75,13 @@ int launch_mx4_rows(const Mx4GemmArgs& a, int64_t grid, hipStream_t s) {
     return launched();
 }
 
+template <int WM>
+int launch_mx4_lds(const Mx4GemmArgs& a, int64_t grid, hipStream_t s) {
+    if (!work_items_fit(grid, 256 * WM)) return MOE_ERR_UNSUPPORTED;
+    mx4_gemm_lds<WM><<<dim3((unsigned)grid), 256 * WM, 0, s>>>(a);
+    return launched();
+}
+
 struct Mx4Tile {
     int tile_m, tile_n;
     int (*launch)(const Mx4GemmArgs&, int64_t grid, hipStream_t);
@@ -82,6 +89,8 @@ struct Mx4Tile {
 const Mx4Tile kMx4Tiles[] = {
     {16, 256, &launch_mx4_rows<1>},
     {64, 256, &launch_mx4_rows<4>},
+    {128, 256, &launch_mx4_lds<1>},
+    {256, 256, &launch_mx4_lds<2>},
 };
 const Mx4Tile* find_mx4_tile(int tile_m, int tile_n) {
     for (const Mx4Tile& t : kMx4Tiles)
@@ -217,7 +226,7 @@ int moe_mx4_tile_supported(int tile_m, int tile_n) { return find_mx4_tile(tile_m
 
 int moe_mx4_default_tiling(int T, int k, int E, int K, int N, int gated, moe_tiling* out) {
     if (!out || T < 0 || k < 1 || k > E || check_mx4_weights(E, K, N, gated) == MOE_ERR_INVALID_ARG) return MOE_ERR_INVALID_ARG;
-    const moe_tiling g = {(int64_t)T * k > 16 * (int64_t)E ? 64 : 16, 256, MOE_ORDER_ASCENDING, 0, 0, 0};
+    const moe_tiling g = {(int64_t)T * k > 32 * (int64_t)E ? 128 : (int64_t)T * k > 16 * (int64_t)E ? 64 : 16, 256, MOE_ORDER_ASCENDING, 0, 0, 0};
     *out = g;
     return MOE_OK;
 }
@@ -231,6 +240,7 @@ int moe_mx4_grouped_gemm(const void* x_codes, const void* x_scales, const void* 
     if ((int64_t)d->T * d->k > (1 << 24)) return MOE_ERR_UNSUPPORTED;
     const Mx4Tile* tile = find_mx4_tile(d->tile_m, d->tile_n);
     if (!tile) return MOE_ERR_UNSUPPORTED;
+    if (d->T * (mx4_padded_k(d->K) / 2) >= (int64_t)1 << 32) return MOE_ERR_UNSUPPORTED;   // (offsets of token rows in 32 bits)
     if (d->T == 0) return MOE_OK;
     if (!x_codes || !x_scales || !w_codes || !w_scales || !Y) return MOE_ERR_INVALID_ARG;
     if (misaligned(x_codes, 16) || misaligned(x_scales, 4) || misaligned(w_codes, 16) || misaligned(w_scales, 16) || misaligned(Y, 16)) return MOE_ERR_INVALID_ARG;

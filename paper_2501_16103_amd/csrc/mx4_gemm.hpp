@@ -98,4 +98,256 @@ __global__ __launch_bounds__(256) void mx4_gemm_rows(Mx4GemmArgs a) {
     }
 }
 
+// acc += A (32 columns of weights) . B (32 tokens), 64 k; byte J of wscale, byte JX of xscale (0 or 2) are the lanes' scales.
+// Written out so that the sum stays in its registers: left to itself the register allocator, with nine tenths of the registers
+// taken, moves accumulators about and spills (seen at 128 of them: 92 registers in memory).  What reads acc outside the loop
+// has to keep its distance by itself, and so has what writes an operand in front of it (the build checks that).
+template <int J, int JX>
+__device__ __forceinline__ void mx4_mfma32(const u32x4_t w, const u32x4_t x, f32x16_t& acc, uint32_t wscale, uint32_t xscale) {
+    static_assert((J == 0 || J == 2) && (JX == 0 || JX == 2), "op_sel_hi");
+    asm volatile("v_mfma_scale_f32_32x32x64_f8f6f4 %0, %1, %2, %0, %3, %4 op_sel_hi:[%5,%6,0] cbsz:4 blgp:4"
+                 : "+v"(acc) : "v"(w), "v"(x), "v"(wscale), "v"(xscale), "n"(J / 2), "n"(JX / 2));
+}
+
+// Tiles of 128 WM rows x 256 packed columns, 4 WM wavefronts of 128 rows x 64 columns.  Token rows go through LDS, which every
+// wavefront column reads: stages of 256 k (128 bytes a row), two of them, loaded into registers a stage ahead and written behind the
+// barrier that frees the other one.  Weights go straight to registers, two k-steps of 128 ahead: packed, a wavefront's step is 4 KB in
+// one piece.  Scales likewise.  Block b of 32 rows belongs to wavefront row b % WM; each wavefront runs the copy of the loop for the
+// blocks it has (MB of them, none included).
+template <int WM>
+struct Mx4TileLds {
+    static constexpr int ROWS = 128 * WM, THREADS = 256 * WM, STAGE = ROWS * 128, SCALES = ROWS * 8, LDS = 2 * (STAGE + SCALES);
+    const Mx4GemmArgs& a;
+    const TileCoord& tc;
+    const int32_t* rows;
+    char* smem;
+    int wave, lane, wm, wn, h, r32;
+
+    template <int MB>
+    __device__ __forceinline__ void run() const {
+        const int tid = threadIdx.x;
+        const int64_t kp = (int64_t)a.tiles_k * kMxTileK;
+        // token rows: 16-byte chunk tid % 8 of rows tid / 8 + 32 WM i
+        const int pos = tid & 7;
+        uint32_t xp[4];
+        const int x_lds = (tid >> 3) * 128 + ((pos ^ ((tid >> 3) & 7)) << 4);   // (32 WM rows further on the swizzle is the same)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int row = (tid >> 3) + 32 * WM * i;
+            xp[i] = (uint32_t)(rows[row < tc.rows ? row : 0] / a.k) * (uint32_t)(kp / 2) + pos * 16;
+        }
+        // their scales: eight bytes of a stage for row tid
+        const bool has_scales = tid < ROWS;
+        const uint32_t sp = (uint32_t)(rows[tid < tc.rows ? tid : 0] / a.k) * (uint32_t)(kp / kMxBlock);
+        const int nt_all = tc.n_tile * 4 + wn, nt = nt_all < a.tiles_n ? nt_all : a.tiles_n - 1;
+        const int64_t tile = ((int64_t)tc.e * a.tiles_n + nt) * a.tiles_k;
+        // lane (h, r32): column r32 % 16 of block r32 / 16 of a 32-column pair, chunk h of the two that a 64 k instruction takes
+        const char* wp = static_cast<const char*>(a.W) + tile * kMxTileBytes;
+        const uint8_t* wsp = a.ws + tile * kMxTileScales;
+        const uint32_t w_off = (r32 >> 4) * 1024 + (h * 16 + (r32 & 15)) * 16, ws_off = (h * 16 + (r32 & 15)) * 4;
+        const int wshift = 8 * (r32 >> 4), xshift = 8 * h;
+        const int steps = a.tiles_k, stages = (steps + 1) / 2;
+
+        f32x16_t acc[MB > 0 ? MB : 1][2];
+#pragma unroll
+        for (int mb = 0; mb < MB; ++mb)
+#pragma unroll
+            for (int b = 0; b < 2; ++b)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) acc[mb][b][i] = 0.f;
+
+        u32x4_t xr[2], x[2][MB > 0 ? MB : 1], w[4][2];      // x: of this 64 k instruction and the next; w[instruction of a stage][b]
+        uint32_t xsr[2], xs[2][MB > 0 ? MB : 1], ws[4];
+        // where this lane's chunk of instruction i of a stage is, and its row's scales (of block 0; blocks are a constant apart)
+        uint32_t x_rd[4], s_rd = 2 * STAGE + (32 * wm + r32) * 8;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) x_rd[i] = (32 * wm + r32) * 128 + (((2 * i + h) ^ (r32 & 7)) << 4);
+        // a stage in two halves: rows of i = 0, 1 with the scales, then of i = 2, 3.  (The second half of an odd last step does not exist:
+        // its tokens are zeros, against the weights of the step before.)
+        auto load_x = [&](int st, int half) __attribute__((always_inline)) {
+            const bool both = 2 * st + 1 < steps;
+            const char* p = static_cast<const char*>(a.X) + st * 128;
+            const uint32_t back = both ? 0u : (uint32_t)(pos & 4) * 16;
+#pragma unroll
+            for (int i = 0; i < 2; ++i) xr[i] = *reinterpret_cast<const u32x4_t*>(p + (xp[2 * half + i] - back));
+            if (half == 0 && has_scales) {
+                const uint8_t* ps = a.xs + st * 8;
+                xsr[0] = *reinterpret_cast<const uint32_t*>(ps + sp);
+                xsr[1] = *reinterpret_cast<const uint32_t*>(ps + (sp + (both ? 4u : 0u)));
+            }
+        };
+        auto store_x = [&](int st, int half) __attribute__((always_inline)) {
+            const bool zero = 2 * st + 1 >= steps && pos >= 4;
+#pragma unroll
+            for (int i = 0; i < 2; ++i)
+                *reinterpret_cast<u32x4_t*>(smem + (st & 1) * STAGE + x_lds + (2 * half + i) * (32 * WM * 128)) = zero ? u32x4_t{0u, 0u, 0u, 0u} : xr[i];
+            if (half == 0 && has_scales)
+                *reinterpret_cast<u32x2_t*>(smem + 2 * STAGE + (st & 1) * SCALES + tid * 8) = u32x2_t{xsr[0], 2 * st + 1 < steps ? xsr[1] : 0u};
+        };
+        auto load_w = [&](int st, auto i_tag) __attribute__((always_inline)) {
+            constexpr int I = decltype(i_tag)::value;
+            if (MB == 0) return;
+            const int kb = 2 * st + I / 2 < steps ? 2 * st + I / 2 : steps - 1;
+#pragma unroll
+            for (int b = 0; b < 2; ++b) w[I][b] = *reinterpret_cast<const u32x4_t*>(wp + (int64_t)kb * kMxTileBytes + (w_off + b * 2048 + (I & 1) * 512));
+            ws[I] = *reinterpret_cast<const uint32_t*>(wsp + (int64_t)kb * kMxTileScales + (ws_off + (I & 1) * 128));
+        };
+        auto read_x = [&](auto i_tag) __attribute__((always_inline)) {
+            constexpr int I = decltype(i_tag)::value;
+#pragma unroll
+            for (int mb = 0; mb < MB; ++mb) x[I & 1][mb] = *reinterpret_cast<const u32x4_t*>(smem + x_rd[I] + mb * (WM * 32 * 128));
+            if constexpr ((I & 1) == 0) {
+#pragma unroll
+                for (int mb = 0; mb < MB; ++mb) xs[I / 2][mb] = *reinterpret_cast<const uint32_t*>(smem + s_rd + mb * (WM * 32 * 8) + I * 2);
+            }
+        };
+        auto multiply = [&](auto i_tag) __attribute__((always_inline)) {
+            constexpr int I = decltype(i_tag)::value, JX = (I & 1) * 2;
+            uint32_t wsc = ws[I] >> wshift;
+            if constexpr ((I & 1) == 0) {
+#pragma unroll
+                for (int mb = 0; mb < MB; ++mb) {
+                    xs[I / 2][mb] >>= xshift;
+                    asm volatile("" : "+v"(xs[I / 2][mb]));
+                }
+            }
+            asm volatile("s_nop 1" : "+v"(wsc));      // two wait states between the shifts and what reads them
+#pragma unroll
+            for (int mb = 0; mb < MB; ++mb) {
+                mx4_mfma32<0, JX>(w[I][0], x[I & 1][mb], acc[mb][0], wsc, xs[I / 2][mb]);
+                mx4_mfma32<2, JX>(w[I][1], x[I & 1][mb], acc[mb][1], wsc, xs[I / 2][mb]);
+            }
+        };
+        auto barrier = []() __attribute__((always_inline)) {
+            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");   // this wavefront's writes (and reads) of LDS are done
+            __builtin_amdgcn_s_barrier();
+            asm volatile("" ::: "memory");
+        };
+        // (fetches past the end take the last stage again: no branches, and nothing reads them)
+        auto stage = [&](int st) __attribute__((always_inline)) { return st < stages ? st : stages - 1; };
+        using std::integral_constant;
+        constexpr integral_constant<int, 0> i0{};
+        constexpr integral_constant<int, 1> i1{};
+        constexpr integral_constant<int, 2> i2{};
+        constexpr integral_constant<int, 3> i3{};
+        load_x(0, 0);
+        load_w(0, i0); load_w(0, i1);
+        store_x(0, 0);
+        load_x(0, 1);
+        load_w(0, i2); load_w(0, i3);
+        store_x(0, 1);
+        load_x(stage(1), 0);
+        barrier();
+        read_x(i0);
+        // The reads of an instruction's fragments are a block of instructions ahead of it; its weights are fetched again as soon as it has
+        // been issued, a stage ahead.  The barrier in front of a stage's last block: the next stage is there, and nobody reads this one any more.
+#pragma unroll
+        for (int mb = 0; mb < MB; ++mb) asm volatile("" : "+v"(acc[mb][0]), "+v"(acc[mb][1]));
+        for (int st = 0; st < stages; ++st) {
+            MOE_SCHED_FENCE();
+            read_x(i1);
+            MOE_SCHED_FENCE();
+            multiply(i0);
+            MOE_SCHED_FENCE();
+            load_w(stage(st + 1), i0);
+            store_x(st + 1, 0);
+            load_x(stage(st + 1), 1);
+            MOE_SCHED_FENCE();
+            read_x(i2);
+            MOE_SCHED_FENCE();
+            multiply(i1);
+            MOE_SCHED_FENCE();
+            load_w(stage(st + 1), i1);
+            MOE_SCHED_FENCE();
+            read_x(i3);
+            MOE_SCHED_FENCE();
+            multiply(i2);
+            MOE_SCHED_FENCE();
+            load_w(stage(st + 1), i2);
+            store_x(st + 1, 1);
+            load_x(stage(st + 2), 0);
+            MOE_SCHED_FENCE();
+            barrier();
+#pragma unroll
+            for (int i = 0; i < 4; ++i) x_rd[i] ^= STAGE;
+            s_rd ^= SCALES;
+            read_x(i0);
+            MOE_SCHED_FENCE();
+            multiply(i3);
+            MOE_SCHED_FENCE();
+            load_w(stage(st + 1), i3);
+        }
+        asm volatile("s_nop 7\n\ts_nop 7\n\ts_nop 7");   // the last sums, before an ordinary instruction reads them
+        barrier();                              // the stages become the way out
+        if (MB == 0 || nt_all >= a.tiles_n) return;
+        uint16_t* y = static_cast<uint16_t*>(a.Y);
+        const int n0 = a.gated ? nt * 32 : nt * 64;
+        int rid[MB > 0 ? MB : 1];               // row of Y that this lane's row of block mb is, or -1
+#pragma unroll
+        for (int mb = 0; mb < MB; ++mb) {
+            const int row = 32 * (WM * mb + wm) + r32;
+            rid[mb] = rows[row < tc.rows ? row : 0];
+            if (row >= tc.rows) rid[mb] = -1;
+        }
+        // A lane's results are runs of four columns of one row.  They are turned in the wavefront's own 4 KB of LDS, 32 rows at a time,
+        // so that a store instruction writes whole stretches of 128 bytes (64 with the activation).
+        char* const mine = smem + wave * 4096;
+        const bool whole = (a.out_n & 7) == 0;
+        const int cu = a.gated ? 4 : 8, c = lane & (cu - 1), lr0 = lane / cu;   // 16-byte chunks of a row, this lane's, its first row
+#pragma unroll
+        for (int mb = 0; mb < MB; ++mb) {
+            uint16_t* yrow = y + (int64_t)(rid[mb] < 0 ? 0 : rid[mb]) * a.out_n;
+            auto put = [&](int chunk, float v0, float v1, float v2, float v3) __attribute__((always_inline)) {   // columns 8 chunk + 4 h ..
+                if (whole) {
+                    const int at = a.gated ? r32 * 64 + ((chunk ^ ((r32 >> 1) & 3)) << 4) : r32 * 128 + ((chunk ^ (r32 & 7)) << 4);
+                    *reinterpret_cast<u32x2_t*>(mine + at + 8 * h) = u32x2_t{pack_bf16(v0, v1), pack_bf16(v2, v3)};
+                } else if (rid[mb] >= 0) {
+                    mx4_store4(yrow, n0 + 8 * chunk + 4 * h, a.out_n, v0, v1, v2, v3);
+                }
+            };
+#pragma unroll
+            for (int b = 0; b < 2; ++b) {
+                const f32x16_t& v = acc[mb][b];
+                if (a.gated) {
+#pragma unroll
+                    for (int q = 0; q < 2; ++q)
+                        put(2 * b + q, silu_times(v[4 * q], v[4 * q + 8]), silu_times(v[4 * q + 1], v[4 * q + 9]), silu_times(v[4 * q + 2], v[4 * q + 10]),
+                            silu_times(v[4 * q + 3], v[4 * q + 11]));
+                } else {
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) put(4 * b + q, v[4 * q], v[4 * q + 1], v[4 * q + 2], v[4 * q + 3]);
+                }
+            }
+            if (!whole) continue;
+#pragma unroll
+            for (int pass = 0; pass < 4; ++pass) {
+                const int lr = pass * (64 / cu) + lr0;
+                const int r = __shfl(rid[mb], lr & 31);
+                if (lr >= 32 || r < 0 || n0 + 8 * c >= a.out_n) continue;
+                const int at = a.gated ? lr * 64 + ((c ^ ((lr >> 1) & 3)) << 4) : lr * 128 + ((c ^ (lr & 7)) << 4);
+                __builtin_nontemporal_store(*reinterpret_cast<const u32x4_t*>(mine + at), reinterpret_cast<u32x4_t*>(y + (int64_t)r * a.out_n + n0 + 8 * c));
+            }
+        }
+    }
+};
+
+template <int WM>
+__global__ __launch_bounds__(256 * WM, 2) void mx4_gemm_lds(Mx4GemmArgs a) {
+    using Tile = Mx4TileLds<WM>;
+    __shared__ __attribute__((aligned(16))) char smem[Tile::LDS];
+    MapLayout L;
+    TileCoord tc;
+    if (!locate_tile<Tile::ROWS, 256, 0, 0>(a, a.map, L, tc)) return;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const Tile t = {a, tc, a.map + L.off_rows + tc.row_base, smem, wave, lane, wave >> 2, wave & 3, lane >> 5, lane & 31};
+    const int blocks = (tc.rows + 31) / 32, mine = (blocks - t.wm + WM - 1) / WM;   // blocks wm, wm + WM, ...
+    switch (mine) {
+        case 0: t.template run<0>(); break;
+        case 1: t.template run<1>(); break;
+        case 2: t.template run<2>(); break;
+        case 3: t.template run<3>(); break;
+        default: t.template run<4>(); break;
+    }
+}
+
 }  // namespace moe
