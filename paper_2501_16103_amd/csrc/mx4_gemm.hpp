@@ -26,8 +26,7 @@ __device__ __forceinline__ f32x4_t mx4_mfma16(const u32x4_t w, const u32x4_t x, 
 __device__ __forceinline__ float silu_times(float gate, float up) { return gate * __builtin_amdgcn_rcpf(1.f + __expf(-gate)) * up; }
 
 // Four consecutive values of a row of Y from column n on; columns at and beyond out_n are padding.
-__device__ __forceinline__ void mx4_store4(uint16_t* yrow, int n, int out_n, float v0, float v1, float v2, float v3) {
-    const uint32_t lo = pack_bf16(v0, v1), hi = pack_bf16(v2, v3);
+__device__ __forceinline__ void mx4_store4(uint16_t* yrow, int n, int out_n, uint32_t lo, uint32_t hi) {
     if ((out_n & 3) == 0) {
         if (n < out_n) *reinterpret_cast<u32x2_t*>(yrow + n) = u32x2_t{lo, hi};
     } else {
@@ -88,11 +87,11 @@ __global__ __launch_bounds__(256) void mx4_gemm_rows(Mx4GemmArgs a) {
 #pragma unroll
         for (int nb = 0; nb < 4; ++nb) {
             if (!a.gated) {
-                mx4_store4(y, nt * 64 + 16 * nb + 4 * g, a.out_n, acc[nb][mb][0], acc[nb][mb][1], acc[nb][mb][2], acc[nb][mb][3]);
+                mx4_store4(y, nt * 64 + 16 * nb + 4 * g, a.out_n, pack_bf16(acc[nb][mb][0], acc[nb][mb][1]), pack_bf16(acc[nb][mb][2], acc[nb][mb][3]));
             } else if (nb % 2 == 0) {
                 const f32x4_t gate = acc[nb][mb], up = acc[nb + 1][mb];
-                mx4_store4(y, nt * 32 + 8 * nb + 4 * g, a.out_n, silu_times(gate[0], up[0]), silu_times(gate[1], up[1]),
-                           silu_times(gate[2], up[2]), silu_times(gate[3], up[3]));
+                mx4_store4(y, nt * 32 + 8 * nb + 4 * g, a.out_n, pack_bf16(silu_times(gate[0], up[0]), silu_times(gate[1], up[1])),
+                           pack_bf16(silu_times(gate[2], up[2]), silu_times(gate[3], up[3])));
             }
         }
     }
@@ -130,7 +129,9 @@ struct Mx4TileLds {
         // token rows: 16-byte chunk tid % 8 of rows tid / 8 + 32 WM i
         const int pos = tid & 7;
         uint32_t xp[4];
-        const int x_lds = (tid >> 3) * 128 + ((pos ^ ((tid >> 3) & 7)) << 4);   // (32 WM rows further on the swizzle is the same)
+        // (LDS has 64 banks: rows of 128 bytes alternate between their halves, and 16 rows' chunks spread over both; 32 WM rows further on
+        // the swizzle is the same)
+        const int x_lds = (tid >> 3) * 128 + ((pos ^ ((tid >> 4) & 7)) << 4);
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             const int row = (tid >> 3) + 32 * WM * i;
@@ -161,7 +162,7 @@ struct Mx4TileLds {
         // where this lane's chunk of instruction i of a stage is, and its row's scales (of block 0; blocks are a constant apart)
         uint32_t x_rd[4], s_rd = 2 * STAGE + (32 * wm + r32) * 8;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) x_rd[i] = (32 * wm + r32) * 128 + (((2 * i + h) ^ (r32 & 7)) << 4);
+        for (int i = 0; i < 4; ++i) x_rd[i] = (32 * wm + r32) * 128 + (((2 * i + h) ^ ((r32 >> 1) & 7)) << 4);
         // a stage in two halves: rows of i = 0, 1 with the scales, then of i = 2, 3.  (The second half of an odd last step does not exist:
         // its tokens are zeros, against the weights of the step before.)
         auto load_x = [&](int st, int half) __attribute__((always_inline)) {
@@ -289,7 +290,7 @@ struct Mx4TileLds {
             rid[mb] = rows[row < tc.rows ? row : 0];
             if (row >= tc.rows) rid[mb] = -1;
         }
-        // A lane's results are runs of four columns of one row.  They are turned in the wavefront's own 4 KB of LDS, 32 rows at a time,
+        // A lane's results are runs of four columns of one row.  Two lanes make eight of them, which are turned in the wavefront's own 4 KB of LDS, 32 rows at a time,
         // so that a store instruction writes whole stretches of 128 bytes (64 with the activation).
         char* const mine = smem + wave * 4096;
         const bool whole = (a.out_n & 7) == 0;
@@ -297,25 +298,33 @@ struct Mx4TileLds {
 #pragma unroll
         for (int mb = 0; mb < MB; ++mb) {
             uint16_t* yrow = y + (int64_t)(rid[mb] < 0 ? 0 : rid[mb]) * a.out_n;
-            auto put = [&](int chunk, float v0, float v1, float v2, float v3) __attribute__((always_inline)) {   // columns 8 chunk + 4 h ..
+            // eight columns of a row, 8 chunk .. 8 chunk + 7, from the runs v, v' of two chunks that lanes h = 0, 1 hold four columns of each:
+            // lanes h = 0 end up with the first chunk, lanes h = 1 with the second
+            auto put = [&](int chunk, u32x2_t v, u32x2_t w2) __attribute__((always_inline)) {
                 if (whole) {
-                    const int at = a.gated ? r32 * 64 + ((chunk ^ ((r32 >> 1) & 3)) << 4) : r32 * 128 + ((chunk ^ (r32 & 7)) << 4);
-                    *reinterpret_cast<u32x2_t*>(mine + at + 8 * h) = u32x2_t{pack_bf16(v0, v1), pack_bf16(v2, v3)};
+                    const auto lo = __builtin_amdgcn_permlane32_swap(v.x, w2.x, false, false);
+                    const auto hi = __builtin_amdgcn_permlane32_swap(v.y, w2.y, false, false);
+                    const int ch = chunk + h;
+                    const int at = a.gated ? r32 * 64 + ((ch ^ ((r32 >> 2) & 3)) << 4) : r32 * 128 + ((ch ^ ((r32 >> 1) & 7)) << 4);
+                    *reinterpret_cast<u32x4_t*>(mine + at) = u32x4_t{lo[0], hi[0], lo[1], hi[1]};
                 } else if (rid[mb] >= 0) {
-                    mx4_store4(yrow, n0 + 8 * chunk + 4 * h, a.out_n, v0, v1, v2, v3);
+                    mx4_store4(yrow, n0 + 8 * chunk + 4 * h, a.out_n, v.x, v.y);
+                    mx4_store4(yrow, n0 + 8 * chunk + 8 + 4 * h, a.out_n, w2.x, w2.y);
                 }
             };
 #pragma unroll
             for (int b = 0; b < 2; ++b) {
                 const f32x16_t& v = acc[mb][b];
+                auto plain = [&](int q) { return u32x2_t{pack_bf16(v[4 * q], v[4 * q + 1]), pack_bf16(v[4 * q + 2], v[4 * q + 3])}; };
+                auto gated = [&](int q) {
+                    return u32x2_t{pack_bf16(silu_times(v[4 * q], v[4 * q + 8]), silu_times(v[4 * q + 1], v[4 * q + 9])),
+                                   pack_bf16(silu_times(v[4 * q + 2], v[4 * q + 10]), silu_times(v[4 * q + 3], v[4 * q + 11]))};
+                };
                 if (a.gated) {
-#pragma unroll
-                    for (int q = 0; q < 2; ++q)
-                        put(2 * b + q, silu_times(v[4 * q], v[4 * q + 8]), silu_times(v[4 * q + 1], v[4 * q + 9]), silu_times(v[4 * q + 2], v[4 * q + 10]),
-                            silu_times(v[4 * q + 3], v[4 * q + 11]));
+                    put(2 * b, gated(0), gated(1));
                 } else {
-#pragma unroll
-                    for (int q = 0; q < 4; ++q) put(4 * b + q, v[4 * q], v[4 * q + 1], v[4 * q + 2], v[4 * q + 3]);
+                    put(4 * b, plain(0), plain(1));
+                    put(4 * b + 2, plain(2), plain(3));
                 }
             }
             if (!whole) continue;
@@ -324,7 +333,7 @@ struct Mx4TileLds {
                 const int lr = pass * (64 / cu) + lr0;
                 const int r = __shfl(rid[mb], lr & 31);
                 if (lr >= 32 || r < 0 || n0 + 8 * c >= a.out_n) continue;
-                const int at = a.gated ? lr * 64 + ((c ^ ((lr >> 1) & 3)) << 4) : lr * 128 + ((c ^ (lr & 7)) << 4);
+                const int at = a.gated ? lr * 64 + ((c ^ ((lr >> 2) & 3)) << 4) : lr * 128 + ((c ^ ((lr >> 1) & 7)) << 4);
                 __builtin_nontemporal_store(*reinterpret_cast<const u32x4_t*>(mine + at), reinterpret_cast<u32x4_t*>(y + (int64_t)r * a.out_n + n0 + 8 * c));
             }
         }
