@@ -141,18 +141,25 @@ int few_sizes(const moe_few_tokens_desc* d, FewSizes* z) {
     return MOE_OK;
 }
 
-template <class W, int EPL, class Src>
+template <class W, int EPL, class Src, int HELD>
 int launch_few(const FewArgs& a, int grid1, hipStream_t s) {
     const int lds = few_lds_bytes<W>(a.route.T);
     static unsigned long long done1 = 0, done2 = 0;
     constexpr int most = few_lds_bytes<W>(kFewTokens);
-    if (ensure_lds_attr(reinterpret_cast<const void*>(&few_tokens_up<W, EPL, Src>), most, &done1) != MOE_OK) return MOE_ERR_HIP;
+    if (ensure_lds_attr(reinterpret_cast<const void*>(&few_tokens_up<W, EPL, Src, HELD>), most, &done1) != MOE_OK) return MOE_ERR_HIP;
     if (ensure_lds_attr(reinterpret_cast<const void*>(&few_tokens_down<W>), most, &done2) != MOE_OK) return MOE_ERR_HIP;
-    few_tokens_up<W, EPL, Src><<<dim3(grid1), kFewThreads, lds, s>>>(a);
+    few_tokens_up<W, EPL, Src, HELD><<<dim3(grid1), kFewThreads, lds, s>>>(a);
     const int rc = launched();
     if (rc != MOE_OK) return rc;
     few_tokens_down<W><<<dim3(a.tiles2 * a.parts2), kFewThreads, lds, s>>>(a);
     return launched();
+}
+template <class W, int EPL, class Src>
+int launch_few(const FewArgs& a, int grid1, hipStream_t s) {
+    // (two steps of 4-bit token fragments, 32 registers, is what there is room for)
+    if constexpr (std::is_same<W, FewMx4>::value)
+        if (a.steps1 <= 2 * kFewWaves) return launch_few<W, EPL, Src, 2>(a, grid1, s);
+    return launch_few<W, EPL, Src, 0>(a, grid1, s);
 }
 template <class W, class Src>
 int launch_few(const FewArgs& a, int grid1, hipStream_t s) {

@@ -44,8 +44,11 @@ __device__ __forceinline__ uint32_t mx4_scale_byte(uint32_t largest_bits) {
 }
 // 2^(byte - 127) for byte < 255; 2^-127 is a subnormal fp32.
 __device__ __forceinline__ float mx4_scale(uint32_t byte) {
-    return __uint_as_float(byte ? byte << 23 : 0x00400000u);
+    const uint32_t bits = byte << 23;
+    return __uint_as_float(bits > 0x00400000u ? bits : 0x00400000u);
 }
+// The same for any byte: NaN for 255, which makes NaN of every code it scales.
+__device__ __forceinline__ float mx4_scale_or_nan(uint32_t byte) { return byte == 255u ? __uint_as_float(0x7fc00000u) : mx4_scale(byte); }
 
 // Codes of eight values (fp32 bits), element i in bits 4 i.  The conversion rounds to the nearest element, ties to the
 // even code, and ends at 6.
@@ -67,11 +70,6 @@ __device__ __forceinline__ u32x4_t mx4_values8(uint32_t codes, float scale) {
     o.z = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, scale, 2));
     o.w = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, scale, 3));
     return o;
-}
-// The same with a scale byte, 255 included.
-__device__ __forceinline__ u32x4_t mx4_values8_of(uint32_t codes, uint32_t byte) {
-    const u32x4_t nan = {0x7fc07fc0u, 0x7fc07fc0u, 0x7fc07fc0u, 0x7fc07fc0u};
-    return byte == 255u ? nan : mx4_values8(codes, mx4_scale(byte));
 }
 
 __device__ __forceinline__ float mx4_load(const uint16_t* p) { return __uint_as_float((uint32_t)*p << 16); }
@@ -127,7 +125,7 @@ __global__ __launch_bounds__(256) void mx4_quantize_rows(const Src* __restrict__
     codes[c] = code;
     if ((threadIdx.x & 3) == 0) scales[c >> 2] = (uint8_t)byte;
     if (values && at < cols) {
-        const u32x4_t o = mx4_values8_of(code, byte);
+        const u32x4_t o = mx4_values8(code, mx4_scale_or_nan(byte));
         uint16_t* q = values + row * cols + at;
         if constexpr (VEC) {
             *reinterpret_cast<u32x4_t*>(q) = o;
@@ -181,7 +179,7 @@ __global__ __launch_bounds__(256) void mx4_pack_weights(const Src* __restrict__ 
     if (values) {
 #pragma unroll
         for (int q = 0; q < 4; ++q) {
-            const u32x4_t o = mx4_values8_of(code[q], byte);
+            const u32x4_t o = mx4_values8(code[q], mx4_scale_or_nan(byte));
 #pragma unroll
             for (int i = 0; i < 8; ++i)
                 if (8 * q + i < have) values[first + (8 * q + i) * step] = (uint16_t)(o[i >> 1] >> (16 * (i & 1)));

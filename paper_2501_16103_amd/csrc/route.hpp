@@ -34,13 +34,17 @@ __device__ __forceinline__ float route_logit(uint32_t key) {   // the logit a ke
     return __uint_as_float(key & 0x80000000u ? key & 0x7fffffffu : ~key);
 }
 
+// Largest of the 64 lanes' values, in every lane.  Within the lanes' own registers: the same by shuffles is six round trips through
+// the LDS crossbar, and the choice of k experts is a chain of k + 1 of these.
 __device__ __forceinline__ uint32_t wave_max_u32(uint32_t v) {
-#pragma unroll
-    for (int d = 1; d < 64; d <<= 1) {
-        const uint32_t o = (uint32_t)__shfl_xor((int)v, d);
-        v = o > v ? o : v;
-    }
-    return v;
+    auto step = [&](uint32_t o) __attribute__((always_inline)) { v = o > v ? o : v; };
+    step(__builtin_amdgcn_update_dpp(0, v, 0x111, 0xf, 0xf, false));   // row_shr:1
+    step(__builtin_amdgcn_update_dpp(0, v, 0x112, 0xf, 0xf, false));   // row_shr:2
+    step(__builtin_amdgcn_update_dpp(0, v, 0x114, 0xf, 0xf, false));   // row_shr:4
+    step(__builtin_amdgcn_update_dpp(0, v, 0x118, 0xf, 0xf, false));   // row_shr:8
+    step(__builtin_amdgcn_update_dpp(0, v, 0x142, 0xa, 0xf, false));   // row_bcast:15 into rows 1 and 3
+    step(__builtin_amdgcn_update_dpp(0, v, 0x143, 0xc, 0xf, false));   // row_bcast:31 into rows 2 and 3
+    return (uint32_t)__builtin_amdgcn_readlane((int)v, 63);
 }
 __device__ __forceinline__ float wave_sum(float v) {
 #pragma unroll
@@ -49,8 +53,8 @@ __device__ __forceinline__ float wave_sum(float v) {
 }
 
 // One token by one wavefront.  EPL: logits per lane, expert 64 j + lane in slot j.  The i-th choice comes back in slot i / 64 of
-// lane i % 64: its expert and its weight (lanes past the k choices hold nothing of use).
-template <int EPL, class Src>
+// lane i % 64: its expert and its weight (lanes past the k choices hold nothing of use).  WEIGHTS false: the experts alone.
+template <int EPL, class Src, bool WEIGHTS = true>
 __device__ __forceinline__ void route_token(const RouteArgs& a, int64_t t, int (&ids)[EPL], float (&weights)[EPL]) {
     const int lane = __lane_id();
     const Src* row = static_cast<const Src*>(a.logits) + t * a.row_stride;
@@ -67,7 +71,7 @@ __device__ __forceinline__ void route_token(const RouteArgs& a, int64_t t, int (
     const float top = route_logit(now);
     const bool empty = top == -__builtin_inff();
     float total = 0.f;
-    if (!a.sigmoid && !empty) {
+    if (WEIGHTS && !a.sigmoid && !empty) {
 #pragma unroll
         for (int j = 0; j < EPL; ++j) total += key[j] != 0 ? expf(route_logit(key[j]) - top) : 0.f;
         total = wave_sum(total);
@@ -95,6 +99,7 @@ __device__ __forceinline__ void route_token(const RouteArgs& a, int64_t t, int (
             now = largest();
         }
     }
+    if (!WEIGHTS) return;
     float sum = 0.f;
 #pragma unroll
     for (int s = 0; s < EPL; ++s) {
