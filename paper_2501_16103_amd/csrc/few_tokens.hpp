@@ -6,7 +6,7 @@
 //
 // A step of so few tokens reads every chosen expert's weights once and computes next to nothing, so both launches are
 // streams of weights through registers: a wavefront loads its share straight in the layout of the matrix operand (bf16:
-// 32 k x 128 columns of [K][N] weights, turned in registers; 4 bits: the packed tiles of mx4.hpp), multiplies it with all
+// 16 k x 128 columns of [K][N] weights, turned in registers; 4 bits: the packed tiles of mx4.hpp), multiplies it with all
 // tokens at once (they are the 16 columns of the other operand, token t is column t for every expert), and the
 // wavefronts of a workgroup, which share a column tile and split its k, add their sums in LDS.  A token that an expert
 // was not chosen for is a column whose result is dropped (never a product with zero: such an expert's infinities must not
@@ -39,7 +39,9 @@ struct FewArgs {
     uint16_t* out;                // [T][hidden] bf16
     int32_t* ids;                 // [T][k]
     float* weights;               // [T][k]
-    uint16_t* h;                  // [T * k][h_pitch] bf16
+    uint16_t* h;                  // bf16 weights: [T * k][h_pitch] bf16
+    uint8_t *h_hi, *h_lo;         // 4-bit weights: [T * k][h_pitch] e4m3, see FewMx4
+    uint8_t* h_scales;            // [T * k][h_pitch / 32]
     float* partial;               // [column tile][part][16][columns of a tile]
     int* arrived;                 // [column tile]
     int hidden, inter, h_pitch;
@@ -83,11 +85,41 @@ __device__ __forceinline__ int few_row(const FewRouting& r, int t, int k, int e)
 }
 
 // Weights of one k-step in registers, and their product with the tokens.
+
+// 4-bit weights go into the matrix instruction as they are; its other operand then has 8 bits, and a token's bf16 value is two of
+// those: x = 2^s (hi + lo / 16), s the block's (of 32) exponent that puts its largest magnitude into [128, 256), hi the nearest e4m3
+// value of x / 2^s and lo that of 16 times what is left.  Exact for bf16 values down to 2^-13 of the block's largest, below that
+// off by at most 2^-21 of the largest.  (Turning the weights into bf16 instead is 64 quarter-rate conversions a step: 64 experts, 2048 /
+// 1408, 16 tokens, 75 us with them.)  A block with an infinity or NaN is NaN.
+// The instruction's 8-bit operand: lane 16 g + t holds k = 16 g + 0 .. 15 and 64 + 16 g + 0 .. 15 of token t, and the scale of
+// k = 32 g .. 32 g + 31.
 struct FewMx4 {
     static constexpr int KSTEP = kMxTileK, COLS = kMxTileN, BLOCKS = 4;
-    struct Tokens { u32x4_t x[4]; };
+    template <bool STAGED> static constexpr int AHEAD_UP = STAGED ? 3 : 1;   // steps that loads are ahead, as far as registers go
+    static constexpr int AHEAD_DOWN = 1, GROUP = 2;   // GROUP: column tiles that a workgroup of the first launch takes at a time
+    struct Raw { u32x4_t x[4]; };
+    struct Tokens {
+        i32x8_t hi, lo;
+        uint32_t scale;           // byte 0: of hi, byte 1: of lo
+    };
     u32x4_t w[4];
     uint32_t scale;
+    // Scale byte of a block whose largest magnitude has these fp32 bits; 4 less, that of lo, is a byte too.
+    static __device__ __forceinline__ uint32_t scale_byte(uint32_t largest_bits) {
+        const int e = (int)(largest_bits >> 23) - 7;
+        return largest_bits >= 0x7f800000u ? 255u : (uint32_t)(e < 4 ? 4 : e);
+    }
+    static __device__ __forceinline__ float inverse(uint32_t byte) { return __uint_as_float(byte == 255u ? 0u : (254u - byte) << 23); }
+    // hi and lo of four values v = x / 2^s, as two words
+    static __device__ __forceinline__ void split(const float (&v)[4], int& hi, int& lo) {
+        int h = 0, l = 0;
+        h = __builtin_amdgcn_cvt_pk_fp8_f32(v[0], v[1], h, false);
+        h = __builtin_amdgcn_cvt_pk_fp8_f32(v[2], v[3], h, true);
+        l = __builtin_amdgcn_cvt_pk_fp8_f32((v[0] - __builtin_amdgcn_cvt_f32_fp8(h, 0)) * 16.f, (v[1] - __builtin_amdgcn_cvt_f32_fp8(h, 1)) * 16.f, l, false);
+        l = __builtin_amdgcn_cvt_pk_fp8_f32((v[2] - __builtin_amdgcn_cvt_f32_fp8(h, 2)) * 16.f, (v[3] - __builtin_amdgcn_cvt_f32_fp8(h, 3)) * 16.f, l, true);
+        hi = h;
+        lo = l;
+    }
     // tile: weight tiles in front of this one
     __device__ __forceinline__ void load(const char* codes, const uint8_t* scales, int64_t tile) {
         const u32x4_t* p = reinterpret_cast<const u32x4_t*>(codes + tile * kMxTileBytes) + __lane_id();
@@ -95,23 +127,130 @@ struct FewMx4 {
         for (int i = 0; i < 4; ++i) w[i] = __builtin_nontemporal_load(p + 64 * i);
         scale = __builtin_nontemporal_load(reinterpret_cast<const uint32_t*>(scales + tile * kMxTileScales) + __lane_id());
     }
-    // xrow: this lane's token row; valid: elements of it
-    static __device__ __forceinline__ void load(Tokens& t, const uint16_t* xrow, int kb, int valid) {
+    // bf16 tokens.  xrow: this lane's token row; valid: elements of it (a multiple of 8)
+    static __device__ __forceinline__ void load(Raw& t, const uint16_t* xrow, int kb, int valid) {
 #pragma unroll
         for (int q = 0; q < 4; ++q) {
-            const int k = kb * KSTEP + 32 * (__lane_id() >> 4) + 8 * q;
+            const int k = kb * KSTEP + 16 * (__lane_id() >> 4) + 64 * (q >> 1) + 8 * (q & 1);
             t.x[q] = k < valid ? *reinterpret_cast<const u32x4_t*>(xrow + k) : u32x4_t{0u, 0u, 0u, 0u};
         }
     }
-    __device__ __forceinline__ void multiply(const Tokens& t, f32x4_t (&acc)[BLOCKS]) const {
+    static __device__ __forceinline__ void convert(Tokens& t, const Raw& r) {
+        // the lane's two halves belong to blocks g / 2 and 2 + g / 2, which the lanes of g ^ 1 hold the rest of
+        uint32_t byte[2];
 #pragma unroll
-        for (int nb = 0; nb < 4; ++nb) {
-            const float s = mx4_scale_or_nan((scale >> (8 * nb)) & 255u);
+        for (int half = 0; half < 2; ++half) {
+            uint32_t m = 0;
 #pragma unroll
-            for (int q = 0; q < 4; ++q)
-                acc[nb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, mx4_values8(w[nb][q], s)),
-                                                                  __builtin_bit_cast(bf16x8_t, t.x[q]), acc[nb], 0, 0, 0);
+            for (int i = 0; i < 8; ++i) {
+                const uint32_t v = r.x[2 * half + i / 4][i % 4], a = (v << 16) & 0x7fffffffu, b = v & 0x7fff0000u;
+                m = a > m ? a : m;
+                m = b > m ? b : m;
+            }
+            const uint32_t o = (uint32_t)__shfl_xor((int)m, 16);
+            byte[half] = scale_byte(o > m ? o : m);
+            const float inv = inverse(byte[half]);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const uint32_t p = r.x[2 * half + i / 2][2 * (i % 2)], q = r.x[2 * half + i / 2][2 * (i % 2) + 1];
+                const float v[4] = {__uint_as_float(p << 16) * inv, __uint_as_float(p & 0xffff0000u) * inv, __uint_as_float(q << 16) * inv,
+                                    __uint_as_float(q & 0xffff0000u) * inv};
+                int h, l;
+                split(v, h, l);
+                t.hi[4 * half + i] = h;
+                t.lo[4 * half + i] = l;
+            }
         }
+        // block g's byte: lanes of 2 g, first half (g < 2), lanes of 2 g - 4, second half
+        const int lane = __lane_id(), g = lane >> 4, from = ((2 * g) & 3) * 16 + (lane & 15);
+        const uint32_t first = (uint32_t)__shfl((int)byte[0], from), second = (uint32_t)__shfl((int)byte[1], from);
+        const uint32_t b = g < 2 ? first : second;
+        t.scale = b | (b - 4) << 8;
+    }
+    // All of X, split, in LDS: [T][pitch] hi, the same of lo, [T][pitch / 32] scales.  Rows are 16 bytes more than whole steps long, so
+    // that the 16 rows of a fragment are spread over the banks.
+    static __host__ __device__ constexpr int lds_pitch(int hidden) { return (hidden + KSTEP - 1) / KSTEP * KSTEP + 16; }
+    static __host__ __device__ constexpr int lds_bytes(int T, int hidden) { return T * (2 * lds_pitch(hidden) + lds_pitch(hidden) / 16 * 16); }
+    // eight elements a thread, four threads a block (all threads; pieces beyond the row are zeros)
+    static __device__ __forceinline__ void stage(const uint16_t* X, int T, int hidden, char* lds) {
+        const int pitch = lds_pitch(hidden), chunks = (pitch - 16) / 8;
+        uint8_t* hi = reinterpret_cast<uint8_t*>(lds);
+        uint8_t* lo = hi + T * pitch;
+        uint8_t* scales = lo + T * pitch;
+        for (int i = threadIdx.x; i < T * chunks; i += kFewThreads) {     // (a multiple of 16 a row: the four threads stay together)
+            const int t = i / chunks, at = (i - t * chunks) * 8;
+            const u32x4_t x = at < hidden ? *reinterpret_cast<const u32x4_t*>(X + (int64_t)t * hidden + at) : u32x4_t{0u, 0u, 0u, 0u};
+            uint32_t m = 0;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const uint32_t a = (x[j] << 16) & 0x7fffffffu, b = x[j] & 0x7fff0000u;
+                m = a > m ? a : m;
+                m = b > m ? b : m;
+            }
+#pragma unroll
+            for (int d = 1; d < 4; d <<= 1) {
+                const uint32_t o = (uint32_t)__shfl_xor((int)m, d);
+                m = o > m ? o : m;
+            }
+            const uint32_t byte = scale_byte(m);
+            const float inv = inverse(byte);
+            int h[2], l[2];
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+                const float v[4] = {__uint_as_float(x[2 * j] << 16) * inv, __uint_as_float(x[2 * j] & 0xffff0000u) * inv, __uint_as_float(x[2 * j + 1] << 16) * inv,
+                                    __uint_as_float(x[2 * j + 1] & 0xffff0000u) * inv};
+                split(v, h[j], l[j]);
+            }
+            *reinterpret_cast<u32x2_t*>(hi + t * pitch + at) = u32x2_t{(uint32_t)h[0], (uint32_t)h[1]};
+            *reinterpret_cast<u32x2_t*>(lo + t * pitch + at) = u32x2_t{(uint32_t)l[0], (uint32_t)l[1]};
+            if ((i & 3) == 0) scales[t * (pitch / 16) + (at >> 5)] = (uint8_t)byte;
+        }
+    }
+    // the fragment of step kb for token row t
+    static __device__ __forceinline__ void load(Tokens& f, const char* lds, int T, int hidden, int t, int kb) {
+        const int pitch = lds_pitch(hidden), g = __lane_id() >> 4;
+        const char* hi = lds + t * pitch + kb * KSTEP + 16 * g;
+        const char* lo = hi + T * pitch;
+#pragma unroll
+        for (int half = 0; half < 2; ++half) {
+            const u32x4_t h = *reinterpret_cast<const u32x4_t*>(hi + 64 * half), l = *reinterpret_cast<const u32x4_t*>(lo + 64 * half);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                f.hi[4 * half + i] = (int)h[i];
+                f.lo[4 * half + i] = (int)l[i];
+            }
+        }
+        const uint32_t b = *reinterpret_cast<const uint8_t*>(lds + 2 * T * pitch + t * (pitch / 16) + kb * 4 + g);
+        f.scale = b | (b - 4) << 8;
+    }
+    // activations that are split already.  valid: elements of a row that were written (a multiple of 32)
+    static __device__ __forceinline__ void load(Tokens& t, const uint8_t* hi, const uint8_t* lo, const uint8_t* scales, int kb, int valid) {
+        const int g = __lane_id() >> 4;
+        const u32x4_t zero = {0u, 0u, 0u, 0u};
+#pragma unroll
+        for (int half = 0; half < 2; ++half) {
+            const int k = kb * KSTEP + 16 * g + 64 * half;
+            const u32x4_t h = k < valid ? *reinterpret_cast<const u32x4_t*>(hi + k) : zero, l = k < valid ? *reinterpret_cast<const u32x4_t*>(lo + k) : zero;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                t.hi[4 * half + i] = (int)h[i];
+                t.lo[4 * half + i] = (int)l[i];
+            }
+        }
+        const uint32_t b = kb * KSTEP + 32 * g < valid ? scales[kb * 4 + g] : 127u;
+        t.scale = b | (b - 4) << 8;
+    }
+    template <int NB>
+    __device__ __forceinline__ void multiply_one(const Tokens& t, f32x4_t& acc) const {
+        const i32x8_t a = {(int)w[NB].x, (int)w[NB].y, (int)w[NB].z, (int)w[NB].w, 0, 0, 0, 0};
+        acc = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, t.hi, acc, 4, 0, NB, (int)scale, 0, (int)t.scale);
+        acc = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, t.lo, acc, 4, 0, NB, (int)scale, 1, (int)t.scale);
+    }
+    __device__ __forceinline__ void multiply(const Tokens& t, f32x4_t (&acc)[BLOCKS]) const {
+        multiply_one<0>(t, acc[0]);
+        multiply_one<1>(t, acc[1]);
+        multiply_one<2>(t, acc[2]);
+        multiply_one<3>(t, acc[3]);
     }
     // matrix row i of block b is column 16 b + i: f(column, sums of columns column .. column + 3), for token lane % 16
     template <class F>
@@ -122,39 +261,44 @@ struct FewMx4 {
     }
 };
 
+// (steps of 16 k: twice as many of them in flight as of 32, in the same registers)
 struct FewBf16 {
-    static constexpr int KSTEP = 32, COLS = 128, BLOCKS = 8;
-    struct Tokens { u32x4_t x; };
-    u32x4_t w[8];
+    static constexpr int KSTEP = 16, COLS = 128, BLOCKS = 8;
+    template <bool> static constexpr int AHEAD_UP = 3;
+    static constexpr int AHEAD_DOWN = 3, GROUP = 1;
+    struct Tokens { u32x2_t x; };
+    using Raw = Tokens;
+    static __host__ __device__ constexpr int lds_bytes(int, int) { return 0; }
+    u32x4_t w[4];
     // base: row k = 0 of the expert; col: this lane's first column; N: columns of a weight row (K is a multiple of 8)
     __device__ __forceinline__ void load(const uint16_t* base, uint32_t col, int N, int K, int kb) {
         const int g = __lane_id() >> 4;
-        const bool inside = kb * KSTEP + 8 * g < K;
+        const bool inside = kb * KSTEP + 4 * g < K;
         const char* p = reinterpret_cast<const char*>(base + (int64_t)kb * KSTEP * N);
-        uint32_t at = ((uint32_t)(inside ? 8 * g : 0) * (uint32_t)N + col) * 2;
+        uint32_t at = ((uint32_t)(inside ? 4 * g : 0) * (uint32_t)N + col) * 2;
 #pragma unroll
-        for (int r = 0; r < 8; ++r) {
+        for (int r = 0; r < 4; ++r) {
             w[r] = __builtin_nontemporal_load(reinterpret_cast<const u32x4_t*>(p + at));
             at += 2 * (uint32_t)N;
         }
         if (kb * KSTEP + KSTEP > K && !inside) {      // a short last step: the lanes beyond it hold zeros on both sides
 #pragma unroll
-            for (int r = 0; r < 8; ++r) w[r] = u32x4_t{0u, 0u, 0u, 0u};
+            for (int r = 0; r < 4; ++r) w[r] = u32x4_t{0u, 0u, 0u, 0u};
         }
     }
     static __device__ __forceinline__ void load(Tokens& t, const uint16_t* xrow, int kb, int valid) {
-        const int k = kb * KSTEP + 8 * (__lane_id() >> 4);
-        t.x = k < valid ? *reinterpret_cast<const u32x4_t*>(xrow + k) : u32x4_t{0u, 0u, 0u, 0u};
+        const int k = kb * KSTEP + 4 * (__lane_id() >> 4);
+        t.x = k < valid ? *reinterpret_cast<const u32x2_t*>(xrow + k) : u32x2_t{0u, 0u};
     }
-    // The lane holds 8 rows x 8 columns: words of two columns of a row become words of two rows of a column.
+    // The lane holds 4 rows x 8 columns: words of two columns of a row become words of two rows of a column.
     __device__ __forceinline__ void multiply(const Tokens& t, f32x4_t (&acc)[BLOCKS]) const {
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
-            u32x4_t a;
+            u32x2_t a;
 #pragma unroll
-            for (int q = 0; q < 4; ++q)
+            for (int q = 0; q < 2; ++q)
                 a[q] = __builtin_amdgcn_perm(w[2 * q + 1][j >> 1], w[2 * q][j >> 1], j & 1 ? 0x07060302u : 0x05040100u);
-            acc[j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, a), __builtin_bit_cast(bf16x8_t, t.x), acc[j], 0, 0, 0);
+            acc[j] = __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(__builtin_bit_cast(s16x4_t, a), __builtin_bit_cast(s16x4_t, t.x), acc[j], 0, 0, 0);
         }
     }
     // matrix row i of block j is column 8 i + j: f(column, sums of columns column .. column + 3)
@@ -169,20 +313,25 @@ struct FewBf16 {
     }
 };
 
-// Dynamic LDS: the wavefronts' sums, [wavefront][token][column].
+// Dynamic LDS: the wavefronts' sums, [wavefront][token][column], and behind them (first launch, STAGED) the tokens.
 template <class W>
 constexpr int few_lds_bytes(int T) { return kFewWaves * T * W::COLS * (int)sizeof(float); }
+constexpr int kFewLdsMost = 160 * 1024 - 4096;      // (the routing takes less than 4 KB)
+static_assert(sizeof(FewRouting) + 64 <= 4096, "routing");
 
 // First launch.  Workgroups take column tiles of the chosen experts one after the other.
-template <class W, int EPL, class Src, int HELD>
+template <class W, int EPL, class Src, bool STAGED>
 __global__ __launch_bounds__(kFewThreads, 4) void few_tokens_up(FewArgs a) {
     constexpr bool MX4 = std::is_same<W, FewMx4>::value;
     constexpr int OUTS = W::COLS / 2;   // outputs of a column tile
+    constexpr int NC = W::GROUP, KW = kFewWaves / NC;  // wavefronts that share a column tile
     extern __shared__ __attribute__((aligned(16))) float sums[];
     __shared__ FewRouting r;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), li = lane & 15;
     const int T = a.route.T, k = a.route.k;
+    char* const tokens = reinterpret_cast<char*>(sums + kFewWaves * T * W::COLS);      // behind the sums (STAGED)
     if (threadIdx.x < kMaxE / 32) r.chosen[threadIdx.x] = 0;
+    if constexpr (STAGED) W::stage(a.X, T, a.hidden, tokens);
     for (int t = wave; t < T; t += kFewWaves) {
         int id[EPL];
         float w[EPL];
@@ -203,14 +352,15 @@ __global__ __launch_bounds__(kFewThreads, 4) void few_tokens_up(FewArgs a) {
     FewSlots slots;
     slots.build(r, T * k);
     const uint16_t* xrow = a.X + (int64_t)(li < T ? li : 0) * a.hidden;
-    const int total = slots.all * a.tiles1;
-    // A wavefront takes every eighth k-step of a tile.  Its loads are a step ahead, across the tiles too: while the sums of one
-    // are added, the weights of the next are on their way.
-    int tile = blockIdx.x, kb = wave, c = 0;            // where the loads are
+    // A workgroup takes NC neighbouring column tiles at a time, a wavefront every KW-th k-step of one of them.  Its loads are steps ahead,
+    // across the tiles too: while the sums of one are added, the weights of the next are on their way.
+    const int groups = (a.tiles1 + NC - 1) / NC, total = slots.all * groups, sub = wave % NC, first = wave / NC;
+    int tile = blockIdx.x, kb = first, c = 0;           // where the loads are
     int64_t e = 0;
     auto enter = [&]() __attribute__((always_inline)) {
-        const int slot = tile / a.tiles1;
-        c = tile - slot * a.tiles1;
+        const int slot = tile / groups;
+        c = (tile - slot * groups) * NC + sub;
+        if (NC > 1 && c >= a.tiles1) c = a.tiles1 - 1;  // (a group with a tile less: its last one twice)
         e = slots.expert(slot);
     };
     auto load = [&](W& s) __attribute__((always_inline)) {
@@ -223,9 +373,9 @@ __global__ __launch_bounds__(kFewThreads, 4) void few_tokens_up(FewArgs a) {
         }
     };
     auto advance = [&]() __attribute__((always_inline)) {
-        kb += kFewWaves;
+        kb += KW;
         if (kb >= a.steps1) {
-            kb = wave;
+            kb = first;
             tile += gridDim.x;
             if (tile < total) enter();
         }
@@ -233,60 +383,89 @@ __global__ __launch_bounds__(kFewThreads, 4) void few_tokens_up(FewArgs a) {
     };
     if (tile >= total) return;
     enter();
-    const int mine = wave < a.steps1 ? (a.steps1 - wave + kFewWaves - 1) / kFewWaves : 0;   // k-steps of a tile that this wavefront takes
-    // HELD > 0: the wavefront's token fragments, at most that many steps of them, are the same for every tile and stay in
-    // registers, which leaves room for the weights of a step more; otherwise they come along with the weights of their step.
-    constexpr int AHEAD = HELD > 0 ? 2 : 1;
+    const int mine = first < a.steps1 ? (a.steps1 - first + KW - 1) / KW : 0;   // k-steps of a tile that this wavefront takes
+    // STAGED: token fragments come out of LDS when their step is multiplied, and the registers hold the weights of three steps more;
+    // otherwise they come along with the weights of their step.
+    constexpr int AHEAD = W::template AHEAD_UP<STAGED>;
     W buf[AHEAD + 1];
-    typename W::Tokens tok[HELD > 0 ? HELD : 2];
+    typename W::Raw raw[STAGED ? 1 : AHEAD + 1];
     bool more = mine > 0;
-    if constexpr (HELD > 0) {
-#pragma unroll
-        for (int i = 0; i < HELD; ++i) W::load(tok[i], xrow, wave + i * kFewWaves, a.hidden);
-    } else if (more) {
-        W::load(tok[0], xrow, kb, a.hidden);
+    if (more) {
+        load(buf[0]);
+        if constexpr (!STAGED) W::load(raw[0], xrow, kb, a.hidden);
     }
-    if (more) load(buf[0]);
-    if constexpr (AHEAD == 2) {
+#pragma unroll
+    for (int i = 1; i < AHEAD; ++i) {
         more = more && advance();
-        if (more) load(buf[1]);
+        if (more) {
+            load(buf[i]);
+            if constexpr (!STAGED) W::load(raw[i], xrow, kb, a.hidden);
+        }
     }
     for (int at = blockIdx.x; at < total; at += gridDim.x) {
         f32x4_t acc[W::BLOCKS];
 #pragma unroll
         for (int b = 0; b < W::BLOCKS; ++b) acc[b] = f32x4_t{0.f, 0.f, 0.f, 0.f};
-        auto step = [&](const typename W::Tokens& t) __attribute__((always_inline)) {
+        for (int i = 0; i < mine; ++i) {
             more = more && advance();
             if (more) {
                 load(buf[AHEAD]);
-                if constexpr (HELD == 0) W::load(tok[1], xrow, kb, a.hidden);
+                if constexpr (!STAGED) W::load(raw[AHEAD], xrow, kb, a.hidden);
             }
-            buf[0].multiply(t, acc);
+            if constexpr (MX4) {
+                typename W::Tokens tok;
+                if constexpr (STAGED) W::load(tok, tokens, T, a.hidden, li < T ? li : 0, first + i * KW);
+                else W::convert(tok, raw[0]);
+                buf[0].multiply(tok, acc);
+            } else {
+                buf[0].multiply(raw[0], acc);
+            }
 #pragma unroll
-            for (int i = 0; i < AHEAD; ++i) buf[i] = buf[i + 1];
-            if constexpr (HELD == 0) tok[0] = tok[1];
-        };
-        if constexpr (HELD > 0) {
-#pragma unroll
-            for (int i = 0; i < HELD; ++i)
-                if (i < mine) step(tok[i]);
-        } else {
-            for (int i = 0; i < mine; ++i) step(tok[0]);
+            for (int b = 0; b < AHEAD; ++b) {
+                buf[b] = buf[b + 1];
+                if constexpr (!STAGED) raw[b] = raw[b + 1];
+            }
         }
         if (li < T) W::each(acc, [&](int col, f32x4_t v) { *reinterpret_cast<f32x4_t*>(sums + (wave * T + li) * W::COLS + col) = v; });
         __syncthreads();
-        const int slot_at = at / a.tiles1, c_at = at - slot_at * a.tiles1, e_at = slots.expert(slot_at);
-        for (int i = threadIdx.x; i < T * OUTS; i += kFewThreads) {
-            const int t = i / OUTS, o = i % OUTS, row = few_row(r, t, k, e_at);
-            if (row < 0 || c_at * OUTS + o >= a.h_pitch) continue;
+        const int slot_at = at / groups, c_at = (at - slot_at * groups) * NC, e_at = slots.expert(slot_at);
+        for (int i = threadIdx.x; i < T * OUTS * NC; i += kFewThreads) {
+            const int o = i % OUTS, which = i / OUTS % NC, t = i / (OUTS * NC);
+            int row = few_row(r, t, k, e_at);
+            if (NC > 1 && c_at + which >= a.tiles1) row = -1;
             const int gate = MX4 ? (o >> 4) * 32 + (o & 15) : o, up = MX4 ? gate + 16 : gate + OUTS;
             float g = 0.f, u = 0.f;
+            if (row >= 0) {
 #pragma unroll
-            for (int w = 0; w < kFewWaves; ++w) {
-                g += sums[(w * T + t) * W::COLS + gate];
-                u += sums[(w * T + t) * W::COLS + up];
+                for (int w = 0; w < KW; ++w) {
+                    g += sums[((w * NC + which) * T + t) * W::COLS + gate];
+                    u += sums[((w * NC + which) * T + t) * W::COLS + up];
+                }
             }
-            a.h[(int64_t)row * a.h_pitch + c_at * OUTS + o] = (uint16_t)pack_bf16(g / (1.f + expf(-g)) * u, 0.f);
+            const float h = g / (1.f + expf(-g)) * u;
+            const int col = (c_at + which) * OUTS + o;
+            const int64_t at_h = (int64_t)row * a.h_pitch + col;
+            if constexpr (MX4) {
+                // the tile's 32 outputs of a token are one block, and 32 neighbouring lanes
+                uint32_t m = __float_as_uint(h) & 0x7fffffffu;
+                auto larger = [&](uint32_t other) __attribute__((always_inline)) { m = other > m ? other : m; };
+                larger(__builtin_amdgcn_update_dpp(0, m, 0x121, 0xf, 0xf, false));   // row_ror:1, 2, 4, 8: all 16 lanes of a row
+                larger(__builtin_amdgcn_update_dpp(0, m, 0x122, 0xf, 0xf, false));
+                larger(__builtin_amdgcn_update_dpp(0, m, 0x124, 0xf, 0xf, false));
+                larger(__builtin_amdgcn_update_dpp(0, m, 0x128, 0xf, 0xf, false));
+                larger((uint32_t)__shfl_xor((int)m, 16));
+                const uint32_t byte = W::scale_byte(m);
+                const float v[4] = {h * W::inverse(byte), 0.f, 0.f, 0.f};
+                int hi, lo;
+                W::split(v, hi, lo);
+                if (row >= 0) {
+                    a.h_hi[at_h] = (uint8_t)hi;
+                    a.h_lo[at_h] = (uint8_t)lo;
+                    if (o == 0) a.h_scales[at_h >> 5] = (uint8_t)byte;
+                }
+            } else if (row >= 0 && col < a.h_pitch) {
+                a.h[at_h] = (uint16_t)pack_bf16(h, 0.f);
+            }
         }
         __syncthreads();
     }
@@ -319,50 +498,65 @@ __global__ __launch_bounds__(kFewThreads, 4) void few_tokens_down(FewArgs a) {
     // the wavefront's sums over its experts, each lane's own part of it (in LDS: they change a few times only)
     float* const mine = sums + (wave * T + (li < T ? li : 0)) * W::COLS;
     if (li < T) W::each(acc, [&](int n, f32x4_t v) { *reinterpret_cast<f32x4_t*>(mine + n) = v; });
-    // the expert that the wavefront's loads are at: its k-steps left, and this lane's row among its tokens
-    int slot = from / a.steps2, kb = from - slot * a.steps2;
-    int64_t e = 0;
-    int row = -1;
-    auto enter = [&]() __attribute__((always_inline)) {
-        e = slots.expert(slot);
-        row = few_row(r, li < T ? li : 0, k, (int)e);
+    // where the wavefront's loads are, and, steps behind, its products: slot, k-step, expert, and this lane's row among its tokens
+    struct Place { int slot, kb, row; int64_t e; };
+    auto enter = [&](Place& p) __attribute__((always_inline)) {
+        p.e = slots.expert(p.slot);
+        p.row = few_row(r, li < T ? li : 0, k, (int)p.e);
     };
+    auto onward = [&](Place& p, bool more) __attribute__((always_inline)) {     // true at the end of an expert
+        if (++p.kb < a.steps2) return false;
+        p.kb = 0;
+        ++p.slot;
+        if (more) enter(p);
+        return true;
+    };
+    Place l = {from / a.steps2, 0, -1, 0};
+    l.kb = from - l.slot * a.steps2;
+    if (from < to) enter(l);
+    Place m = l;
     auto load = [&](W& s, typename W::Tokens& t) __attribute__((always_inline)) {
         const uint32_t col = c * W::COLS + (W::COLS / 16) * li;
-        const uint16_t* h = a.h + (int64_t)(row < 0 ? 0 : row) * a.h_pitch;
-        if constexpr (MX4) s.load(a.down, a.down_scales, (e * a.tiles2 + c) * a.steps2 + kb);
-        else s.load(reinterpret_cast<const uint16_t*>(a.down) + e * a.inter * a.hidden, col < a.hidden ? col : 0, a.hidden, a.inter, kb);
-        W::load(t, h, kb, a.h_pitch);
+        const int64_t at_h = (int64_t)(l.row < 0 ? 0 : l.row) * a.h_pitch;
+        if constexpr (MX4) {
+            s.load(a.down, a.down_scales, (l.e * a.tiles2 + c) * a.steps2 + l.kb);
+            W::load(t, a.h_hi + at_h, a.h_lo + at_h, a.h_scales + (at_h >> 5), l.kb, a.h_pitch);
+        } else {
+            s.load(reinterpret_cast<const uint16_t*>(a.down) + l.e * a.inter * a.hidden, col < a.hidden ? col : 0, a.hidden, a.inter, l.kb);
+            W::load(t, a.h + at_h, l.kb, a.h_pitch);
+        }
     };
-    W now, next;
-    typename W::Tokens tok, tok_next;
-    if (from < to) {
-        enter();
-        load(now, tok);
+    constexpr int AHEAD = W::AHEAD_DOWN;
+    W buf[AHEAD + 1];
+    typename W::Tokens tok[AHEAD + 1];
+#pragma unroll
+    for (int i = 0; i < AHEAD; ++i) {
+        if (from + i >= to) break;
+        load(buf[i], tok[i]);
+        onward(l, from + i + 1 < to);
     }
     for (int step = from; step < to; ++step) {
-        const int row_now = row;
-        const bool leave = ++kb == a.steps2;
-        if (step + 1 < to) {
-            if (leave) {
-                kb = 0;
-                ++slot;
-                enter();
-            }
-            load(next, tok_next);
+        if (step + AHEAD < to) {
+            load(buf[AHEAD], tok[AHEAD]);
+            onward(l, step + AHEAD + 1 < to);
         }
-        now.multiply(tok, acc);
-        if (leave || step + 1 == to) {                              // the wavefront's last step of this expert
+        buf[0].multiply(tok[0], acc);
+        const int row = m.row;
+        const bool last_step = step + 1 == to;
+        if (onward(m, !last_step) || last_step) {                   // the wavefront's last step of this expert
             // (a token that did not choose it takes nothing: not 0 times what may be an infinity)
-            if (row_now >= 0 && li < T) {
-                const float w = r.weights[row_now];
+            if (row >= 0 && li < T) {
+                const float w = r.weights[row];
                 W::each(acc, [&](int n, f32x4_t v) { *reinterpret_cast<f32x4_t*>(mine + n) += w * v; });
             }
 #pragma unroll
             for (int b = 0; b < W::BLOCKS; ++b) acc[b] = f32x4_t{0.f, 0.f, 0.f, 0.f};
         }
-        now = next;
-        tok = tok_next;
+#pragma unroll
+        for (int b = 0; b < AHEAD; ++b) {
+            buf[b] = buf[b + 1];
+            tok[b] = tok[b + 1];
+        }
     }
     __syncthreads();
     auto write = [&](int i, float v) {

@@ -123,32 +123,35 @@ int few_sizes(const moe_few_tokens_desc* d, FewSizes* z) {
         z->h_pitch = z->tiles1 * 32;
     } else {
         z->tiles1 = (d->inter + 63) / 64;
-        z->steps1 = (d->hidden + 31) / 32;
-        z->tiles2 = (d->hidden + 127) / 128;
-        z->steps2 = (d->inter + 31) / 32;
+        z->steps1 = (d->hidden + FewBf16::KSTEP - 1) / FewBf16::KSTEP;
+        z->tiles2 = (d->hidden + FewBf16::COLS - 1) / FewBf16::COLS;
+        z->steps2 = (d->inter + FewBf16::KSTEP - 1) / FewBf16::KSTEP;
         z->h_pitch = d->inter;
     }
     const int64_t rows = (int64_t)d->T * d->k, slots = rows < d->E ? rows : d->E;
-    // two workgroups per CU are resident; a part is at least a step for each wavefront
-    const int64_t tiles = slots * z->tiles1, steps = slots * z->steps2;
+    // Workgroups that are resident at once: two per CU, one where the staged tokens leave no LDS for a second (16 tokens, 64 experts,
+    // 2048 / 1408: 75 -> 69 us).  A part of the second launch is at least a step for each of its wavefronts.
+    const int first = mx4 ? few_lds_bytes<FewMx4>(d->T) + FewMx4::lds_bytes(d->T, d->hidden) : few_lds_bytes<FewBf16>(d->T);
+    const int resident = first <= kFewLdsMost && first > kFewLdsMost / 2 ? kCus : 2 * kCus;
+    const int groups = mx4 ? FewMx4::GROUP : FewBf16::GROUP;
+    const int64_t tiles = slots * ((z->tiles1 + groups - 1) / groups), steps = slots * z->steps2;
     int64_t parts = (2 * kCus + z->tiles2 - 1) / z->tiles2;
     if (parts > (steps + kFewWaves - 1) / kFewWaves) parts = (steps + kFewWaves - 1) / kFewWaves;
-    z->grid1 = (int)(tiles < 2 * kCus ? tiles : 2 * kCus);
+    z->grid1 = (int)(tiles < resident ? tiles : resident);
     z->parts2 = (int)(parts < 1 ? 1 : parts);
-    z->h_bytes = up256((size_t)rows * z->h_pitch * 2);
+    z->h_bytes = mx4 ? 2 * up256((size_t)rows * z->h_pitch) + up256((size_t)rows * (z->h_pitch / kMxBlock)) : up256((size_t)rows * z->h_pitch * 2);
     z->partial_bytes = up256((size_t)z->tiles2 * z->parts2 * kFewTokens * (mx4 ? FewMx4::COLS : FewBf16::COLS) * sizeof(float));
     z->arrived_bytes = up256((size_t)z->tiles2 * sizeof(int));
     return MOE_OK;
 }
 
-template <class W, int EPL, class Src, int HELD>
+template <class W, int EPL, class Src, bool STAGED>
 int launch_few(const FewArgs& a, int grid1, hipStream_t s) {
     const int lds = few_lds_bytes<W>(a.route.T);
     static unsigned long long done1 = 0, done2 = 0;
-    constexpr int most = few_lds_bytes<W>(kFewTokens);
-    if (ensure_lds_attr(reinterpret_cast<const void*>(&few_tokens_up<W, EPL, Src, HELD>), most, &done1) != MOE_OK) return MOE_ERR_HIP;
-    if (ensure_lds_attr(reinterpret_cast<const void*>(&few_tokens_down<W>), most, &done2) != MOE_OK) return MOE_ERR_HIP;
-    few_tokens_up<W, EPL, Src, HELD><<<dim3(grid1), kFewThreads, lds, s>>>(a);
+    if (ensure_lds_attr(reinterpret_cast<const void*>(&few_tokens_up<W, EPL, Src, STAGED>), STAGED ? kFewLdsMost : few_lds_bytes<W>(kFewTokens), &done1) != MOE_OK ||
+        ensure_lds_attr(reinterpret_cast<const void*>(&few_tokens_down<W>), few_lds_bytes<W>(kFewTokens), &done2) != MOE_OK) return MOE_ERR_HIP;
+    few_tokens_up<W, EPL, Src, STAGED><<<dim3(grid1), kFewThreads, lds + (STAGED ? W::lds_bytes(a.route.T, a.hidden) : 0), s>>>(a);
     const int rc = launched();
     if (rc != MOE_OK) return rc;
     few_tokens_down<W><<<dim3(a.tiles2 * a.parts2), kFewThreads, lds, s>>>(a);
@@ -156,10 +159,10 @@ int launch_few(const FewArgs& a, int grid1, hipStream_t s) {
 }
 template <class W, int EPL, class Src>
 int launch_few(const FewArgs& a, int grid1, hipStream_t s) {
-    // (two steps of 4-bit token fragments, 32 registers, is what there is room for)
     if constexpr (std::is_same<W, FewMx4>::value)
-        if (a.steps1 <= 2 * kFewWaves) return launch_few<W, EPL, Src, 2>(a, grid1, s);
-    return launch_few<W, EPL, Src, 0>(a, grid1, s);
+        if (few_lds_bytes<W>(a.route.T) + W::lds_bytes(a.route.T, a.hidden) <= kFewLdsMost)
+            return launch_few<W, EPL, Src, true>(a, grid1, s);
+    return launch_few<W, EPL, Src, false>(a, grid1, s);
 }
 template <class W, class Src>
 int launch_few(const FewArgs& a, int grid1, hipStream_t s) {
@@ -291,7 +294,11 @@ int moe_layer_few_tokens(const void* X, const void* logits, const void* w_up, co
     a.down = static_cast<const char*>(w_down); a.down_scales = static_cast<const uint8_t*>(down_scales);
     a.out = static_cast<uint16_t*>(out); a.ids = topk_ids; a.weights = topk_weights;
     char* w = static_cast<char*>(workspace);
+    const size_t h_bytes = up256((size_t)d->T * d->k * z.h_pitch);
     a.h = reinterpret_cast<uint16_t*>(w);
+    a.h_hi = reinterpret_cast<uint8_t*>(w);
+    a.h_lo = a.h_hi + h_bytes;
+    a.h_scales = a.h_lo + h_bytes;
     a.partial = reinterpret_cast<float*>(w + z.h_bytes);
     a.arrived = reinterpret_cast<int*>(w + z.h_bytes + z.partial_bytes);
     a.hidden = d->hidden; a.inter = d->inter; a.h_pitch = z.h_pitch;
