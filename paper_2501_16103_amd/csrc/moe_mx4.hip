@@ -135,7 +135,7 @@ int few_sizes(const moe_few_tokens_desc* d, FewSizes* z) {
     const int resident = first <= kFewLdsMost && first > kFewLdsMost / 2 ? kCus : 2 * kCus;
     const int groups = mx4 ? FewMx4::GROUP : FewBf16::GROUP;
     const int64_t tiles = slots * ((z->tiles1 + groups - 1) / groups), steps = slots * z->steps2;
-    int64_t parts = (2 * kCus + z->tiles2 - 1) / z->tiles2;
+    int64_t parts = (kCus + z->tiles2 - 1) / z->tiles2;
     if (parts > (steps + kFewWaves - 1) / kFewWaves) parts = (steps + kFewWaves - 1) / kFewWaves;
     z->grid1 = (int)(tiles < resident ? tiles : resident);
     z->parts2 = (int)(parts < 1 ? 1 : parts);
