@@ -88,9 +88,8 @@ struct Mx4Tile {
 };
 const Mx4Tile kMx4Tiles[] = {
     {16, 256, &launch_mx4_rows<1>},
-    {64, 256, &launch_mx4_rows<4>},
+    {32, 256, &launch_mx4_rows<2>},
     {128, 256, &launch_mx4_lds<1>},
-    {256, 256, &launch_mx4_lds<2>},
 };
 const Mx4Tile* find_mx4_tile(int tile_m, int tile_n) {
     for (const Mx4Tile& t : kMx4Tiles)
@@ -236,7 +235,12 @@ int moe_mx4_tile_supported(int tile_m, int tile_n) { return find_mx4_tile(tile_m
 
 int moe_mx4_default_tiling(int T, int k, int E, int K, int N, int gated, moe_tiling* out) {
     if (!out || T < 0 || k < 1 || k > E || check_mx4_weights(E, K, N, gated) == MOE_ERR_INVALID_ARG) return MOE_ERR_INVALID_ARG;
-    const moe_tiling g = {(int64_t)T * k > 32 * (int64_t)E ? 128 : (int64_t)T * k > 16 * (int64_t)E ? 64 : 16, 256, MOE_ORDER_ASCENDING, 0, 0, 0};
+    // Rows per expert on average.  us, 16 / 32 / 128 rows a tile, even and skewed routing: 64 experts, 2048 -> 2816, gated, 3 rows 36.9 / 36.7 /
+    // 44.7 and 20.7 / 22.4 / 21.8, 6 rows 38.0 / 38.4 / 45.0 and 22.3 / 25.5 / 24.8, 12 rows 42.3 / 40.6 / 45.8 and 34.1 / 33.9 / 28.2, 19 rows 45.7 / 42.2 /
+    // 46.0 and 39.0 / 37.0 / 30.3, 28 rows 53.9 / 52.3 / 47.0 and 47.4 / 42.3 / 41.1; 8 experts, 4096 -> 28672, 8 rows 95.4 / 95.4 / 90.4 and 82.0 / 79.1 /
+    // 80.9, 16 rows 107.7 / 105.1 / 91.8 and 93.5 / 90.9 / 83.8; 256 experts, 2048 -> 1024, 8 rows 57.3 / 53.9 / 55.1 and 28.7 / 34.9 / 28.0.
+    const int64_t R = (int64_t)T * k;
+    const moe_tiling g = {R > 16 * (int64_t)E ? 128 : R > 8 * (int64_t)E ? 32 : 16, 256, MOE_ORDER_ASCENDING, 0, 0, 0};
     *out = g;
     return MOE_OK;
 }

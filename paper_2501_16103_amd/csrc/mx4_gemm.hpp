@@ -37,53 +37,94 @@ __device__ __forceinline__ void mx4_store4(uint16_t* yrow, int n, int out_n, uin
     }
 }
 
-// Tiles of 16 MB rows x 256 packed columns, four wavefronts of 64 columns; operands straight from memory.
+// Tiles of 16 MB rows x 256 packed columns for few rows per expert: a stream of weights.  Four wavefronts of 64 columns and the whole
+// of K each, which have nothing to wait for in each other: operands go straight from memory to registers, the next steps' loads
+// (of 128 k: 4 KB of codes, 256 bytes of scales, and 64 bytes of each token row) ahead of the product.
 template <int MB>
-__global__ __launch_bounds__(256) void mx4_gemm_rows(Mx4GemmArgs a) {
+__global__ __launch_bounds__(256, 4) void mx4_gemm_rows(Mx4GemmArgs a) {
     MapLayout L;
     TileCoord tc;
     if (!locate_tile<16 * MB, 256, 0, 0>(a, a.map, L, tc)) return;
     const int lane = threadIdx.x & 63, g = lane >> 4, li = lane & 15;
-    const int nt = tc.n_tile * 4 + (threadIdx.x >> 6);
+    const int nt = tc.n_tile * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     if (nt >= a.tiles_n) return;
     const int32_t* rows = a.map + L.off_rows + tc.row_base;
-    const int64_t kp = (int64_t)a.tiles_k * kMxTileK;
-    const char* xp[MB];
-    const uint8_t* sp[MB];
+    const int kp = a.tiles_k * kMxTileK;
+    int id[MB];                             // rows of the tile: asked for in front of the first weights, which do not wait for them
 #pragma unroll
-    for (int mb = 0; mb < MB; ++mb) {
-        const int row = 16 * mb + li, tok = rows[row < tc.rows ? row : 0] / a.k;
-        xp[mb] = static_cast<const char*>(a.X) + tok * (kp / 2) + 16 * g;
-        sp[mb] = a.xs + tok * (kp / kMxBlock) + g;
-    }
+    for (int mb = 0; mb < MB; ++mb) id[mb] = rows[16 * mb + li < tc.rows ? 16 * mb + li : 0];
     const int64_t tile = ((int64_t)tc.e * a.tiles_n + nt) * a.tiles_k;
-    const char* wp = static_cast<const char*>(a.W) + tile * kMxTileBytes + lane * 16;
-    const uint8_t* wsp = a.ws + tile * kMxTileScales + lane * 4;
+    const char* wp = static_cast<const char*>(a.W) + tile * kMxTileBytes;
+    const uint8_t* wsp = a.ws + tile * kMxTileScales;
+    const bool once = tc.m_tiles == 1;      // nobody else reads these weights: they pass L2 by
     f32x4_t acc[4][MB];
 #pragma unroll
     for (int nb = 0; nb < 4; ++nb)
 #pragma unroll
         for (int mb = 0; mb < MB; ++mb) acc[nb][mb] = f32x4_t{0.f, 0.f, 0.f, 0.f};
-    for (int kb = 0; kb < a.tiles_k; ++kb) {
-        u32x4_t w[4];
+    struct Step {
+        u32x4_t w[4], x[MB];
+        uint32_t ws, xs[MB];
+    };
+    uint32_t xp[MB], sp[MB];
+    auto load_w = [&](Step& s, int kb) __attribute__((always_inline)) {
+        const u32x4_t* w = reinterpret_cast<const u32x4_t*>(wp + (int64_t)kb * kMxTileBytes) + lane;
+        const uint32_t* ws = reinterpret_cast<const uint32_t*>(wsp + (int64_t)kb * kMxTileScales) + lane;
+        if (once) {
 #pragma unroll
-        for (int nb = 0; nb < 4; ++nb) w[nb] = *reinterpret_cast<const u32x4_t*>(wp + (int64_t)kb * kMxTileBytes + nb * 1024);
-        const uint32_t ws = *reinterpret_cast<const uint32_t*>(wsp + (int64_t)kb * kMxTileScales);
+            for (int nb = 0; nb < 4; ++nb) s.w[nb] = __builtin_nontemporal_load(w + 64 * nb);
+            s.ws = __builtin_nontemporal_load(ws);
+        } else {
+#pragma unroll
+            for (int nb = 0; nb < 4; ++nb) s.w[nb] = w[64 * nb];
+            s.ws = *ws;
+        }
+    };
+    auto load_x = [&](Step& s, int kb) __attribute__((always_inline)) {
+        const char* x = static_cast<const char*>(a.X) + kb * (kMxTileK / 2);
+        const uint8_t* xs = a.xs + kb * (kMxTileK / kMxBlock);
 #pragma unroll
         for (int mb = 0; mb < MB; ++mb) {
-            const u32x4_t x = *reinterpret_cast<const u32x4_t*>(xp[mb] + kb * (kMxTileK / 2));
-            const uint32_t xs = sp[mb][kb * (kMxTileK / kMxBlock)];
-            acc[0][mb] = mx4_mfma16<0, 0>(w[0], x, acc[0][mb], ws, xs);
-            acc[1][mb] = mx4_mfma16<1, 0>(w[1], x, acc[1][mb], ws, xs);
-            acc[2][mb] = mx4_mfma16<2, 0>(w[2], x, acc[2][mb], ws, xs);
-            acc[3][mb] = mx4_mfma16<3, 0>(w[3], x, acc[3][mb], ws, xs);
+            s.x[mb] = *reinterpret_cast<const u32x4_t*>(x + xp[mb]);
+            s.xs[mb] = xs[sp[mb]];
         }
+    };
+    constexpr int AHEAD = MB == 1 ? 3 : 2;
+    Step buf[AHEAD + 1];
+#pragma unroll
+    for (int i = 0; i < AHEAD; ++i)
+        if (i < a.tiles_k) load_w(buf[i], i);
+    MOE_SCHED_FENCE();
+#pragma unroll
+    for (int mb = 0; mb < MB; ++mb) {
+        const uint32_t tok = (uint32_t)id[mb] / (uint32_t)a.k;
+        xp[mb] = tok * (uint32_t)(kp / 2) + 16 * g;
+        sp[mb] = tok * (uint32_t)(kp / kMxBlock) + g;
+    }
+#pragma unroll
+    for (int i = 0; i < AHEAD; ++i)
+        if (i < a.tiles_k) load_x(buf[i], i);
+    for (int kb = 0; kb < a.tiles_k; ++kb) {
+        if (kb + AHEAD < a.tiles_k) {
+            load_w(buf[AHEAD], kb + AHEAD);
+            load_x(buf[AHEAD], kb + AHEAD);
+        }
+        const Step& s = buf[0];
+#pragma unroll
+        for (int mb = 0; mb < MB; ++mb) {
+            acc[0][mb] = mx4_mfma16<0, 0>(s.w[0], s.x[mb], acc[0][mb], s.ws, s.xs[mb]);
+            acc[1][mb] = mx4_mfma16<1, 0>(s.w[1], s.x[mb], acc[1][mb], s.ws, s.xs[mb]);
+            acc[2][mb] = mx4_mfma16<2, 0>(s.w[2], s.x[mb], acc[2][mb], s.ws, s.xs[mb]);
+            acc[3][mb] = mx4_mfma16<3, 0>(s.w[3], s.x[mb], acc[3][mb], s.ws, s.xs[mb]);
+        }
+#pragma unroll
+        for (int i = 0; i < AHEAD; ++i) buf[i] = buf[i + 1];
     }
 #pragma unroll
     for (int mb = 0; mb < MB; ++mb) {
         const int row = 16 * mb + li;
         if (row >= tc.rows) continue;
-        uint16_t* y = static_cast<uint16_t*>(a.Y) + (int64_t)rows[row] * a.out_n;
+        uint16_t* y = static_cast<uint16_t*>(a.Y) + (int64_t)id[mb] * a.out_n;
 #pragma unroll
         for (int nb = 0; nb < 4; ++nb) {
             if (!a.gated) {
@@ -128,18 +169,22 @@ struct Mx4TileLds {
         const int64_t kp = (int64_t)a.tiles_k * kMxTileK;
         // token rows: 16-byte chunk tid % 8 of rows tid / 8 + 32 WM i
         const int pos = tid & 7;
-        uint32_t xp[4];
+        uint32_t xp[4], sp;                 // their offsets, and that of the scales of row tid: eight bytes of a stage
         // (LDS has 64 banks: rows of 128 bytes alternate between their halves, and 16 rows' chunks spread over both; 32 WM rows further on
         // the swizzle is the same)
         const int x_lds = (tid >> 3) * 128 + ((pos ^ ((tid >> 4) & 7)) << 4);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const int row = (tid >> 3) + 32 * WM * i;
-            xp[i] = (uint32_t)(rows[row < tc.rows ? row : 0] / a.k) * (uint32_t)(kp / 2) + pos * 16;
-        }
-        // their scales: eight bytes of a stage for row tid
         const bool has_scales = tid < ROWS;
-        const uint32_t sp = (uint32_t)(rows[tid < tc.rows ? tid : 0] / a.k) * (uint32_t)(kp / kMxBlock);
+        int id[5];                          // asked for in front of the first weights, which do not wait for them
+#pragma unroll
+        for (int i = 0; i < 5; ++i) {
+            const int row = i < 4 ? (tid >> 3) + 32 * WM * i : tid;
+            id[i] = rows[row < tc.rows ? row : 0];
+        }
+        auto locate_rows = [&]() __attribute__((always_inline)) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) xp[i] = (uint32_t)id[i] / (uint32_t)a.k * (uint32_t)(kp / 2) + pos * 16;
+            sp = (uint32_t)id[4] / (uint32_t)a.k * (uint32_t)(kp / kMxBlock);
+        };
         const int nt_all = tc.n_tile * 4 + wn, nt = nt_all < a.tiles_n ? nt_all : a.tiles_n - 1;
         const int64_t tile = ((int64_t)tc.e * a.tiles_n + nt) * a.tiles_k;
         // lane (h, r32): column r32 % 16 of block r32 / 16 of a 32-column pair, chunk h of the two that a 64 k instruction takes
@@ -231,11 +276,12 @@ struct Mx4TileLds {
         constexpr integral_constant<int, 1> i1{};
         constexpr integral_constant<int, 2> i2{};
         constexpr integral_constant<int, 3> i3{};
+        load_w(0, i0); load_w(0, i1); load_w(0, i2); load_w(0, i3);
+        MOE_SCHED_FENCE();
+        locate_rows();
         load_x(0, 0);
-        load_w(0, i0); load_w(0, i1);
         store_x(0, 0);
         load_x(0, 1);
-        load_w(0, i2); load_w(0, i3);
         store_x(0, 1);
         load_x(stage(1), 0);
         barrier();
