@@ -227,6 +227,12 @@ int moe_mx4_pack_weights(const void* W, int dtype, int w_layout, int E, int K, i
     const int64_t tiles = (int64_t)E * tiles_n * tiles_k;
     const hipStream_t s = static_cast<hipStream_t>(stream);
     const int nk = w_layout == MOE_W_LAYOUT_NK;
+    if (dtype == MOE_DTYPE_BF16 && !nk && N % (gated ? 4 : 2) == 0 && !misaligned(W, 4) && !misaligned(values, 4)) {
+        const dim3 grid((unsigned)((int64_t)E * ((tiles_n + 1) / 2) * tiles_k));
+        mx4_pack_pairs<<<grid, 256, 0, s>>>(static_cast<const uint16_t*>(W), K, N, gated, tiles_n, tiles_k, static_cast<char*>(codes), static_cast<uint8_t*>(scales),
+                                            static_cast<uint16_t*>(values));
+        return launched();
+    }
     return dtype == MOE_DTYPE_FP32 ? launch_pack<float>(W, nk, tiles, K, N, gated, tiles_n, tiles_k, codes, scales, values, s)
                                    : launch_pack<uint16_t>(W, nk, tiles, K, N, gated, tiles_n, tiles_k, codes, scales, values, s);
 }

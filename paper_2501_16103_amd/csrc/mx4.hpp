@@ -161,9 +161,19 @@ __global__ __launch_bounds__(256) void mx4_pack_weights(const Src* __restrict__ 
     const Src* p = W + first;
     float v[kMxBlock];
     uint32_t largest = 0;
+    if (NK && sizeof(Src) == 2 && have == kMxBlock && ((uintptr_t)p & 15) == 0) {
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            const u32x4_t x = reinterpret_cast<const u32x4_t*>(p)[q];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[8 * q + i] = __uint_as_float(i & 1 ? x[i >> 1] & 0xffff0000u : x[i >> 1] << 16);
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < kMxBlock; ++i) v[i] = i < have ? mx4_load(p + i * step) : 0.f;
+    }
 #pragma unroll
     for (int i = 0; i < kMxBlock; ++i) {
-        v[i] = i < have ? mx4_load(p + i * step) : 0.f;
         const uint32_t b = __float_as_uint(v[i]) & 0x7fffffffu;
         largest = b > largest ? b : largest;
     }
@@ -180,9 +190,92 @@ __global__ __launch_bounds__(256) void mx4_pack_weights(const Src* __restrict__ 
 #pragma unroll
         for (int q = 0; q < 4; ++q) {
             const u32x4_t o = mx4_values8(code[q], mx4_scale_or_nan(byte));
+            if (NK && have == kMxBlock && ((uintptr_t)(values + first) & 15) == 0) {
+                reinterpret_cast<u32x4_t*>(values + first)[q] = o;
+                continue;
+            }
 #pragma unroll
             for (int i = 0; i < 8; ++i)
                 if (8 * q + i < have) values[first + (8 * q + i) * step] = (uint16_t)(o[i >> 1] >> (16 * (i & 1)));
+        }
+    }
+}
+
+// The same for bf16 weights [E][K][N] whose rows can be read two columns at a time: one workgroup per two tiles side by side, a thread per 32 k
+// of two neighbouring columns, so that a wavefront reads (and with values writes) 256 bytes of a row, or, gated, 128 bytes of gate columns
+// and 128 of the up columns of the same outputs.
+__global__ __launch_bounds__(256) void mx4_pack_pairs(const uint16_t* __restrict__ W, int K, int N, int gated, int tiles_n, int tiles_k,
+                                                      char* __restrict__ codes, uint8_t* __restrict__ scales, uint16_t* __restrict__ values) {
+    const int pairs_n = (tiles_n + 1) / 2;
+    const int64_t b = blockIdx.x;
+    const int kb = (int)(b % tiles_k), nb = (int)(b / tiles_k % pairs_n);
+    const int64_t e = b / tiles_k / pairs_n;
+    const int lane = threadIdx.x & 63, g = threadIdx.x >> 6;
+    // first of the two columns: in the source, and packed
+    int col, p;
+    bool there;
+    if (gated) {
+        const int half = N >> 1, i = nb * 64 + 2 * (lane & 31), up = lane >> 5;
+        there = i < half;                    // (half is even)
+        col = i + up * half;
+        p = (i >> 4) * 32 + up * 16 + (i & 15);
+    } else {
+        col = p = nb * 128 + 2 * lane;
+        there = col < N;
+    }
+    const int k0 = kb * kMxTileK + g * kMxBlock;
+    const int have = !there || K <= k0 ? 0 : (K - k0 < kMxBlock ? K - k0 : kMxBlock);
+    const int64_t first = (e * K + k0) * N + col;
+    const uint32_t* src = reinterpret_cast<const uint32_t*>(W + first);
+    const int64_t step = N / 2;
+    uint32_t v[kMxBlock];
+    if (have == kMxBlock) {
+#pragma unroll
+        for (int i = 0; i < kMxBlock; ++i) v[i] = __builtin_nontemporal_load(src + i * step);
+    } else {
+#pragma unroll
+        for (int i = 0; i < kMxBlock; ++i) v[i] = i < have ? src[i * step] : 0u;
+    }
+    uint32_t largest[2] = {0u, 0u}, byte[2];
+#pragma unroll
+    for (int i = 0; i < kMxBlock; ++i) {
+        const uint32_t lo = (v[i] << 16) & 0x7fffffffu, hi = v[i] & 0x7fff0000u;
+        largest[0] = lo > largest[0] ? lo : largest[0];
+        largest[1] = hi > largest[1] ? hi : largest[1];
+    }
+    u32x4_t code[2];
+#pragma unroll
+    for (int c = 0; c < 2; ++c) {
+        byte[c] = mx4_scale_byte(largest[c]);
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            float part[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) part[i] = __uint_as_float(c ? v[8 * q + i] & 0xffff0000u : v[8 * q + i] << 16);
+            code[c][q] = mx4_codes8(part, byte[c]);
+        }
+    }
+    const int tile_n = p >> 6, n = p & 63;
+    if (tile_n < tiles_n) {
+        const int64_t tile = (e * tiles_n + tile_n) * tiles_k + kb;
+        u32x4_t* out = reinterpret_cast<u32x4_t*>(codes + tile * kMxTileBytes + (n >> 4) * 1024) + g * 16 + (n & 15);
+        out[0] = code[0];
+        out[1] = code[1];
+        uint8_t* s = scales + tile * kMxTileScales + (g * 16 + (n & 15)) * 4 + (n >> 4);
+        s[0] = (uint8_t)byte[0];
+        s[4] = (uint8_t)byte[1];
+    }
+    if (values && have > 0) {
+        uint32_t* dst = reinterpret_cast<uint32_t*>(values + first);
+        const float s0 = mx4_scale_or_nan(byte[0]), s1 = mx4_scale_or_nan(byte[1]);
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            const u32x4_t a = mx4_values8(code[0][q], s0), c = mx4_values8(code[1][q], s1);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const uint32_t w = __builtin_amdgcn_perm(c[i >> 1], a[i >> 1], i & 1 ? 0x07060302u : 0x05040100u);
+                if (8 * q + i < have) __builtin_nontemporal_store(w, dst + (8 * q + i) * step);
+            }
         }
     }
 }
