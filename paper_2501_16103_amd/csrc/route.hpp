@@ -47,34 +47,60 @@ __device__ __forceinline__ uint32_t wave_max_u32(uint32_t v) {
     return (uint32_t)__builtin_amdgcn_readlane((int)v, 63);
 }
 __device__ __forceinline__ float wave_sum(float v) {
-#pragma unroll
-    for (int d = 1; d < 64; d <<= 1) v += __shfl_xor(v, d);
-    return v;
+    auto step = [&](int o) __attribute__((always_inline)) { v += __int_as_float(o); };
+    step(__builtin_amdgcn_update_dpp(0, __float_as_int(v), 0x111, 0xf, 0xf, false));
+    step(__builtin_amdgcn_update_dpp(0, __float_as_int(v), 0x112, 0xf, 0xf, false));
+    step(__builtin_amdgcn_update_dpp(0, __float_as_int(v), 0x114, 0xf, 0xf, false));
+    step(__builtin_amdgcn_update_dpp(0, __float_as_int(v), 0x118, 0xf, 0xf, false));
+    step(__builtin_amdgcn_update_dpp(0, __float_as_int(v), 0x142, 0xa, 0xf, false));
+    step(__builtin_amdgcn_update_dpp(0, __float_as_int(v), 0x143, 0xc, 0xf, false));
+    return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v), 63));
 }
 
-// One token by one wavefront.  EPL: logits per lane, expert 64 j + lane in slot j.  The i-th choice comes back in slot i / 64 of
+// One token by one wavefront.  EPL: logits per lane, experts EPL * lane + 0 .. EPL - 1.  The i-th choice comes back in slot i / 64 of
 // lane i % 64: its expert and its weight (lanes past the k choices hold nothing of use).  WEIGHTS false: the experts alone.
+// A lane keeps its logits in falling order (equal ones by rising expert), so that a choice only looks at one of them: the largest first
+// one of all lanes, of several the lowest lane's.
 template <int EPL, class Src, bool WEIGHTS = true>
 __device__ __forceinline__ void route_token(const RouteArgs& a, int64_t t, int (&ids)[EPL], float (&weights)[EPL]) {
     const int lane = __lane_id();
     const Src* row = static_cast<const Src*>(a.logits) + t * a.row_stride;
     uint32_t key[EPL];
+    int expert[EPL];
+    float logit[EPL];          // (all loads first and without branches: one trip to memory)
 #pragma unroll
-    for (int j = 0; j < EPL; ++j) key[j] = 64 * j + lane < a.E ? route_key(mx4_load(row + 64 * j + lane)) : 0;
-    auto largest = [&]() {
-        uint32_t m = 0;
+    for (int j = 0; j < EPL; ++j) {
+        expert[j] = EPL * lane + j;
+        logit[j] = mx4_load(row + (expert[j] < a.E ? expert[j] : a.E - 1));
+    }
 #pragma unroll
-        for (int j = 0; j < EPL; ++j) m = key[j] > m ? key[j] : m;
-        return wave_max_u32(m);
-    };
-    uint32_t now = largest();
+    for (int j = 0; j < EPL; ++j) key[j] = expert[j] < a.E ? route_key(logit[j]) : 0;
+    uint32_t first = key[0];
+#pragma unroll
+    for (int j = 1; j < EPL; ++j) first = key[j] > first ? key[j] : first;
+    uint32_t now = wave_max_u32(first);
     const float top = route_logit(now);
     const bool empty = top == -__builtin_inff();
     float total = 0.f;
     if (WEIGHTS && !a.sigmoid && !empty) {
 #pragma unroll
-        for (int j = 0; j < EPL; ++j) total += key[j] != 0 ? expf(route_logit(key[j]) - top) : 0.f;
+        for (int j = 0; j < EPL; ++j) {
+            const float p = expf(logit[j] - top);
+            total += key[j] != 0 ? p : 0.f;
+        }
         total = wave_sum(total);
+    }
+    // insertion sort (in registers): an element moves up past strictly smaller ones only
+#pragma unroll
+    for (int j = 1; j < EPL; ++j) {
+#pragma unroll
+        for (int i = j; i > 0; --i) {
+            const bool up = key[i] > key[i - 1];
+            const uint32_t hi = up ? key[i] : key[i - 1], lo = up ? key[i - 1] : key[i];
+            const int e_hi = up ? expert[i] : expert[i - 1], e_lo = up ? expert[i - 1] : expert[i];
+            key[i - 1] = hi; key[i] = lo;
+            expert[i - 1] = e_hi; expert[i] = e_lo;
+        }
     }
     uint32_t chosen[EPL];
 #pragma unroll
@@ -83,20 +109,21 @@ __device__ __forceinline__ void route_token(const RouteArgs& a, int64_t t, int (
         chosen[s] = 0;
         const int end = a.k - 64 * s < 64 ? a.k - 64 * s : 64;
         for (int i = 0; i < end; ++i) {
-            int e = -1;
-#pragma unroll
-            for (int j = 0; j < EPL; ++j) {
-                const unsigned long long at = __ballot(key[j] == now);
-                if (e < 0 && at != 0) {
-                    e = 64 * j + __builtin_ctzll(at);
-                    if (lane == __builtin_ctzll(at)) key[j] = 0;
-                }
-            }
+            const int owner = __builtin_ctzll(__ballot(key[0] == now));
+            const int e = __builtin_amdgcn_readlane(expert[0], owner);
             if (lane == i) {
                 ids[s] = e;
                 chosen[s] = now;
             }
-            now = largest();
+            if (lane == owner) {
+#pragma unroll
+                for (int j = 0; j + 1 < EPL; ++j) {
+                    key[j] = key[j + 1];
+                    expert[j] = expert[j + 1];
+                }
+                key[EPL - 1] = 0;
+            }
+            now = wave_max_u32(key[0]);
         }
     }
     if (!WEIGHTS) return;
