@@ -529,9 +529,10 @@ def moe_route(logits: torch.Tensor, k: int, topk_ids: torch.Tensor, topk_weights
               renormalize: bool = True, scale: float = 1.0, check: bool = True) -> int:
     """logits [T, E], fp32 or bf16, rows of consecutive elements -> topk_ids int32 [T, k], topk_weights fp32 [T, k]."""
     T, E = logits.shape
-    d = moe_route_desc(T, k, E, _dtype(logits), logits.stride(0), score, int(renormalize), scale)
-    rc = MOE_ERR_INVALID_ARG if E > 1 and logits.stride(1) != 1 else lib().moe_route(_ptr(logits), ctypes.byref(d), _ptr(topk_ids),
-                                                                                     _ptr(topk_weights), _stream())
+    row, step = logits.stride()
+    d = moe_route_desc(T, k, E, _dtype(logits), row, score, renormalize, scale)
+    rc = MOE_ERR_INVALID_ARG if step != 1 and E > 1 else lib().moe_route(logits.data_ptr(), ctypes.byref(d), topk_ids.data_ptr(),
+                                                                         topk_weights.data_ptr(), _stream())
     if check and rc != MOE_OK:
         raise MoeError(rc, "moe_route")
     return rc
@@ -540,8 +541,9 @@ def moe_route(logits: torch.Tensor, k: int, topk_ids: torch.Tensor, topk_weights
 def moe_mx4_quantize(src: torch.Tensor, codes: torch.Tensor, scales: torch.Tensor, values: Optional[torch.Tensor] = None, check: bool = True) -> int:
     """src [rows, cols], fp32 or bf16, rows of consecutive elements; `values` bf16 [rows, cols], contiguous."""
     rows, cols = src.shape
-    rc = MOE_ERR_INVALID_ARG if cols > 1 and src.stride(1) != 1 else lib().moe_mx4_quantize(
-        _ptr(src), _dtype(src), rows, cols, src.stride(0), _ptr(codes), _ptr(scales), _ptr(values), _stream())
+    row, step = src.stride()
+    rc = MOE_ERR_INVALID_ARG if step != 1 and cols > 1 else lib().moe_mx4_quantize(
+        src.data_ptr(), _dtype(src), rows, cols, row, codes.data_ptr(), scales.data_ptr(), _ptr(values), _stream())
     if check and rc != MOE_OK:
         raise MoeError(rc, "moe_mx4_quantize")
     return rc
@@ -591,7 +593,7 @@ def moe_mx4_default_tiling(T: int, k: int, E: int, K: int, N: int, gated: bool =
 
 def _contiguous(where: str, t: torch.Tensor, shape: tuple, dtype: Optional[torch.dtype] = None) -> None:
     """The classes below take tensors whose sizes the C entry points cannot see: what does not fit is refused here."""
-    if tuple(t.shape) != shape or not t.is_contiguous() or (dtype is not None and t.dtype != dtype):
+    if t.shape != shape or not t.is_contiguous() or (dtype is not None and t.dtype != dtype):
         raise MoeError(MOE_ERR_INVALID_ARG, where)
 
 
@@ -606,10 +608,11 @@ class Mx4Rows:
         self.codes, self.scales = (torch.empty(n, dtype=torch.uint8, device=device) for n in sizes)
 
     def quantize(self, src: torch.Tensor, values: Optional[torch.Tensor] = None) -> "Mx4Rows":
-        if src.dim() != 2 or src.shape[0] > self.rows or src.shape[1] != self.cols:
+        shape = src.shape
+        if len(shape) != 2 or shape[0] > self.rows or shape[1] != self.cols:
             raise MoeError(MOE_ERR_INVALID_ARG, "Mx4Rows.quantize")
         if values is not None:
-            _contiguous("Mx4Rows.quantize", values, tuple(src.shape), torch.bfloat16)
+            _contiguous("Mx4Rows.quantize", values, shape, torch.bfloat16)
         moe_mx4_quantize(src, self.codes, self.scales, values)
         return self
 
@@ -629,7 +632,7 @@ class Mx4Weights:
         """W [E, K, N] (or [E, N, K] with MOE_W_LAYOUT_NK), bf16 or fp32; `values`: bf16, of W's shape."""
         _contiguous("Mx4Weights.pack", W, (self.E, self.N, self.K) if w_layout == MOE_W_LAYOUT_NK else (self.E, self.K, self.N))
         if values is not None:
-            _contiguous("Mx4Weights.pack", values, tuple(W.shape), torch.bfloat16)
+            _contiguous("Mx4Weights.pack", values, W.shape, torch.bfloat16)
         moe_mx4_pack_weights(W, w_layout, self.E, self.K, self.N, self.gated, self.codes, self.scales, values)
         return self
 

@@ -259,10 +259,9 @@ struct Mx4TileLds {
             }
             asm volatile("s_nop 1" : "+v"(wsc));      // two wait states between the shifts and what reads them
 #pragma unroll
-            for (int mb = 0; mb < MB; ++mb) {
-                mx4_mfma32<0, JX>(w[I][0], x[I & 1][mb], acc[mb][0], wsc, xs[I / 2][mb]);
-                mx4_mfma32<2, JX>(w[I][1], x[I & 1][mb], acc[mb][1], wsc, xs[I / 2][mb]);
-            }
+            for (int mb = 0; mb < MB; ++mb) mx4_mfma32<0, JX>(w[I][0], x[I & 1][mb], acc[mb][0], wsc, xs[I / 2][mb]);
+#pragma unroll
+            for (int mb = MB - 1; mb >= 0; --mb) mx4_mfma32<2, JX>(w[I][1], x[I & 1][mb], acc[mb][1], wsc, xs[I / 2][mb]);
         };
         auto barrier = []() __attribute__((always_inline)) {
             asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");   // this wavefront's writes (and reads) of LDS are done

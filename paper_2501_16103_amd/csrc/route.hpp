@@ -85,7 +85,8 @@ __device__ __forceinline__ void route_token(const RouteArgs& a, int64_t t, int (
     if (WEIGHTS && !a.sigmoid && !empty) {
 #pragma unroll
         for (int j = 0; j < EPL; ++j) {
-            const float p = expf(logit[j] - top);
+            // (the fast exponential is off by 2^-24 of its argument: x e^-x of that at most in the sum, whose largest term is 1)
+            const float p = __expf(logit[j] - top);
             total += key[j] != 0 ? p : 0.f;
         }
         total = wave_sum(total);
