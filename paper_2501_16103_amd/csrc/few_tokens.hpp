@@ -170,7 +170,7 @@ struct FewMx4 {
     // All of X, split, in LDS: [T][pitch] hi, the same of lo, [T][pitch / 32] scales.  Rows are 16 bytes more than whole steps long, so
     // that the 16 rows of a fragment are spread over the banks.
     static __host__ __device__ constexpr int lds_pitch(int hidden) { return (hidden + KSTEP - 1) / KSTEP * KSTEP + 16; }
-    static __host__ __device__ constexpr int lds_bytes(int T, int hidden) { return T * (2 * lds_pitch(hidden) + lds_pitch(hidden) / 16 * 16); }
+    static __host__ __device__ constexpr int lds_bytes(int T, int hidden) { return T * (2 * lds_pitch(hidden) + lds_pitch(hidden) / 32); }
     // eight elements a thread, four threads a block (all threads; pieces beyond the row are zeros)
     static __device__ __forceinline__ void stage(const uint16_t* X, int T, int hidden, char* lds) {
         const int pitch = lds_pitch(hidden), chunks = (pitch - 16) / 8;
@@ -203,7 +203,7 @@ struct FewMx4 {
             }
             *reinterpret_cast<u32x2_t*>(hi + t * pitch + at) = u32x2_t{(uint32_t)h[0], (uint32_t)h[1]};
             *reinterpret_cast<u32x2_t*>(lo + t * pitch + at) = u32x2_t{(uint32_t)l[0], (uint32_t)l[1]};
-            if ((i & 3) == 0) scales[t * (pitch / 16) + (at >> 5)] = (uint8_t)byte;
+            if ((i & 3) == 0) scales[t * (pitch / 32) + (at >> 5)] = (uint8_t)byte;
         }
     }
     // the fragment of step kb for token row t
@@ -220,7 +220,7 @@ struct FewMx4 {
                 f.lo[4 * half + i] = (int)l[i];
             }
         }
-        const uint32_t b = *reinterpret_cast<const uint8_t*>(lds + 2 * T * pitch + t * (pitch / 16) + kb * 4 + g);
+        const uint32_t b = *reinterpret_cast<const uint8_t*>(lds + 2 * T * pitch + t * (pitch / 32) + kb * 4 + g);
         f.scale = b | (b - 4) << 8;
     }
     // activations that are split already.  valid: elements of a row that were written (a multiple of 32)
