@@ -96,7 +96,7 @@ __device__ __forceinline__ int few_row(const FewRouting& r, int t, int k, int e)
 struct FewMx4 {
     static constexpr int KSTEP = kMxTileK, COLS = kMxTileN, BLOCKS = 4;
     template <bool STAGED> static constexpr int AHEAD_UP = STAGED ? 3 : 1;   // steps that loads are ahead, as far as registers go
-    static constexpr int AHEAD_DOWN = 1, GROUP = 2;   // GROUP: column tiles that a workgroup of the first launch takes at a time
+    static constexpr int AHEAD_DOWN = 1;
     struct Raw { u32x4_t x[4]; };
     struct Tokens {
         i32x8_t hi, lo;
@@ -171,39 +171,53 @@ struct FewMx4 {
     // that the 16 rows of a fragment are spread over the banks.
     static __host__ __device__ constexpr int lds_pitch(int hidden) { return (hidden + KSTEP - 1) / KSTEP * KSTEP + 16; }
     static __host__ __device__ constexpr int lds_bytes(int T, int hidden) { return T * (2 * lds_pitch(hidden) + lds_pitch(hidden) / 32); }
-    // eight elements a thread, four threads a block (all threads; pieces beyond the row are zeros)
+    // eight elements a thread, four threads a block (all threads; pieces beyond the row are zeros); BATCH pieces a thread are asked for at
+    // a time, each batch a trip to memory
     static __device__ __forceinline__ void stage(const uint16_t* X, int T, int hidden, char* lds) {
-        const int pitch = lds_pitch(hidden), chunks = (pitch - 16) / 8;
+        constexpr int BATCH = 4;
+        const int pitch = lds_pitch(hidden), chunks = (pitch - 16) / 8, all = T * chunks;
         uint8_t* hi = reinterpret_cast<uint8_t*>(lds);
         uint8_t* lo = hi + T * pitch;
         uint8_t* scales = lo + T * pitch;
-        for (int i = threadIdx.x; i < T * chunks; i += kFewThreads) {     // (a multiple of 16 a row: the four threads stay together)
-            const int t = i / chunks, at = (i - t * chunks) * 8;
-            const u32x4_t x = at < hidden ? *reinterpret_cast<const u32x4_t*>(X + (int64_t)t * hidden + at) : u32x4_t{0u, 0u, 0u, 0u};
-            uint32_t m = 0;
+        for (int i0 = threadIdx.x; i0 < all; i0 += BATCH * kFewThreads) {     // (a multiple of 16 a row: the four threads stay together)
+            u32x4_t x[BATCH];
+            int t[BATCH], at[BATCH];
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const uint32_t a = (x[j] << 16) & 0x7fffffffu, b = x[j] & 0x7fff0000u;
-                m = a > m ? a : m;
-                m = b > m ? b : m;
+            for (int u = 0; u < BATCH; ++u) {
+                const int i = i0 + u * kFewThreads;
+                t[u] = i / chunks;
+                at[u] = (i - t[u] * chunks) * 8;
+                x[u] = *reinterpret_cast<const u32x4_t*>(X + (i < all && at[u] < hidden ? (int64_t)t[u] * hidden + at[u] : 0));
             }
 #pragma unroll
-            for (int d = 1; d < 4; d <<= 1) {
-                const uint32_t o = (uint32_t)__shfl_xor((int)m, d);
-                m = o > m ? o : m;
-            }
-            const uint32_t byte = scale_byte(m);
-            const float inv = inverse(byte);
-            int h[2], l[2];
+            for (int u = 0; u < BATCH; ++u) {
+                if (i0 + u * kFewThreads >= all) break;
+                const u32x4_t v4 = at[u] < hidden ? x[u] : u32x4_t{0u, 0u, 0u, 0u};
+                uint32_t m = 0;
 #pragma unroll
-            for (int j = 0; j < 2; ++j) {
-                const float v[4] = {__uint_as_float(x[2 * j] << 16) * inv, __uint_as_float(x[2 * j] & 0xffff0000u) * inv, __uint_as_float(x[2 * j + 1] << 16) * inv,
-                                    __uint_as_float(x[2 * j + 1] & 0xffff0000u) * inv};
-                split(v, h[j], l[j]);
+                for (int j = 0; j < 4; ++j) {
+                    const uint32_t a = (v4[j] << 16) & 0x7fffffffu, b = v4[j] & 0x7fff0000u;
+                    m = a > m ? a : m;
+                    m = b > m ? b : m;
+                }
+#pragma unroll
+                for (int d = 1; d < 4; d <<= 1) {
+                    const uint32_t o = (uint32_t)__shfl_xor((int)m, d);
+                    m = o > m ? o : m;
+                }
+                const uint32_t byte = scale_byte(m);
+                const float inv = inverse(byte);
+                int h[2], l[2];
+#pragma unroll
+                for (int j = 0; j < 2; ++j) {
+                    const float v[4] = {__uint_as_float(v4[2 * j] << 16) * inv, __uint_as_float(v4[2 * j] & 0xffff0000u) * inv,
+                                        __uint_as_float(v4[2 * j + 1] << 16) * inv, __uint_as_float(v4[2 * j + 1] & 0xffff0000u) * inv};
+                    split(v, h[j], l[j]);
+                }
+                *reinterpret_cast<u32x2_t*>(hi + t[u] * pitch + at[u]) = u32x2_t{(uint32_t)h[0], (uint32_t)h[1]};
+                *reinterpret_cast<u32x2_t*>(lo + t[u] * pitch + at[u]) = u32x2_t{(uint32_t)l[0], (uint32_t)l[1]};
+                if (((i0 + u * kFewThreads) & 3) == 0) scales[t[u] * (pitch / 32) + (at[u] >> 5)] = (uint8_t)byte;
             }
-            *reinterpret_cast<u32x2_t*>(hi + t * pitch + at) = u32x2_t{(uint32_t)h[0], (uint32_t)h[1]};
-            *reinterpret_cast<u32x2_t*>(lo + t * pitch + at) = u32x2_t{(uint32_t)l[0], (uint32_t)l[1]};
-            if ((i & 3) == 0) scales[t * (pitch / 32) + (at >> 5)] = (uint8_t)byte;
         }
     }
     // the fragment of step kb for token row t
@@ -265,7 +279,7 @@ struct FewMx4 {
 struct FewBf16 {
     static constexpr int KSTEP = 16, COLS = 128, BLOCKS = 8;
     template <bool> static constexpr int AHEAD_UP = 3;
-    static constexpr int AHEAD_DOWN = 3, GROUP = 1;
+    static constexpr int AHEAD_DOWN = 3;
     struct Tokens { u32x2_t x; };
     using Raw = Tokens;
     static __host__ __device__ constexpr int lds_bytes(int, int) { return 0; }
@@ -319,12 +333,12 @@ constexpr int few_lds_bytes(int T) { return kFewWaves * T * W::COLS * (int)sizeo
 constexpr int kFewLdsMost = 160 * 1024 - 4096;      // (the routing takes less than 4 KB)
 static_assert(sizeof(FewRouting) + 64 <= 4096, "routing");
 
-// First launch.  Workgroups take column tiles of the chosen experts one after the other.
-template <class W, int EPL, class Src, bool STAGED>
+// First launch.  Workgroups take column tiles of the chosen experts, NC neighbouring ones at a time, one group after the other.
+template <class W, int NC, int EPL, class Src, bool STAGED>
 __global__ __launch_bounds__(kFewThreads, 4) void few_tokens_up(FewArgs a) {
     constexpr bool MX4 = std::is_same<W, FewMx4>::value;
     constexpr int OUTS = W::COLS / 2;   // outputs of a column tile
-    constexpr int NC = W::GROUP, KW = kFewWaves / NC;  // wavefronts that share a column tile
+    constexpr int KW = kFewWaves / NC;  // wavefronts that share a column tile
     extern __shared__ __attribute__((aligned(16))) float sums[];
     __shared__ FewRouting r;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), li = lane & 15;
@@ -352,9 +366,12 @@ __global__ __launch_bounds__(kFewThreads, 4) void few_tokens_up(FewArgs a) {
     FewSlots slots;
     slots.build(r, T * k);
     const uint16_t* xrow = a.X + (int64_t)(li < T ? li : 0) * a.hidden;
-    // A workgroup takes NC neighbouring column tiles at a time, a wavefront every KW-th k-step of one of them.  Its loads are steps ahead,
+    // A wavefront takes every KW-th k-step of one of a group's tiles.  Its loads are steps ahead,
     // across the tiles too: while the sums of one are added, the weights of the next are on their way.
     const int groups = (a.tiles1 + NC - 1) / NC, total = slots.all * groups, sub = wave % NC, first = wave / NC;
+    // (as few workgroups as the longest share allows: all of them then end together)
+    const int rounds = (total + gridDim.x - 1) / (int)gridDim.x, sharing = (total + rounds - 1) / rounds;
+    if ((int)blockIdx.x >= sharing) return;
     int tile = blockIdx.x, kb = first, c = 0;           // where the loads are
     int64_t e = 0;
     auto enter = [&]() __attribute__((always_inline)) {
@@ -376,12 +393,11 @@ __global__ __launch_bounds__(kFewThreads, 4) void few_tokens_up(FewArgs a) {
         kb += KW;
         if (kb >= a.steps1) {
             kb = first;
-            tile += gridDim.x;
+            tile += sharing;
             if (tile < total) enter();
         }
         return tile < total;
     };
-    if (tile >= total) return;
     enter();
     const int mine = first < a.steps1 ? (a.steps1 - first + KW - 1) / KW : 0;   // k-steps of a tile that this wavefront takes
     // STAGED: token fragments come out of LDS when their step is multiplied, and the registers hold the weights of three steps more;
@@ -402,7 +418,7 @@ __global__ __launch_bounds__(kFewThreads, 4) void few_tokens_up(FewArgs a) {
             if constexpr (!STAGED) W::load(raw[i], xrow, kb, a.hidden);
         }
     }
-    for (int at = blockIdx.x; at < total; at += gridDim.x) {
+    for (int at = blockIdx.x; at < total; at += sharing) {
         f32x4_t acc[W::BLOCKS];
 #pragma unroll
         for (int b = 0; b < W::BLOCKS; ++b) acc[b] = f32x4_t{0.f, 0.f, 0.f, 0.f};

@@ -99,10 +99,23 @@ const Mx4Tile* find_mx4_tile(int tile_m, int tile_n) {
 
 // Sizes of the layer for few tokens that follow from its description.
 struct FewSizes {
-    int tiles1, steps1, tiles2, steps2, parts2, h_pitch, grid1;
+    int tiles1, steps1, tiles2, steps2, parts2, h_pitch, group1, grid1;
     size_t h_bytes, partial_bytes, arrived_bytes;
 };
 constexpr size_t up256(size_t n) { return (n + 255) / 256 * 256; }
+
+// Column tiles of bf16 weights that a workgroup of the first launch takes at a time.  Two read stretches of 512 bytes instead of 256, which
+// memory gives an eighth faster, but a workgroup per CU then takes its tiles by twos: taken where that makes no CU's share longer by more, for
+// the number of experts that evenly spread choices make.  us, one / two: 8 experts, 4096 / 14336, 5 tokens 419 / 361, 16 tokens 505 / 469;
+// 16 experts, 4096 / 2048, 8 tokens 116 / 98; and where the share is longer: 64 experts, 2048 / 1408, 1 token 32.5 / 44.7; 8 experts,
+// 4096 / 7168, 1 token 71 / 95; 64 experts, 2048 / 1024, 16 tokens 102 / 117.
+int few_group(const moe_few_tokens_desc* d, int tiles) {
+    double none = 1.;
+    for (int t = 0; t < d->T; ++t) none *= 1. - (double)d->k / d->E;
+    const int64_t chosen = (int64_t)(d->E * (1. - none) + 0.5);
+    const int64_t by_one = (chosen * tiles + kCus - 1) / kCus, by_two = 2 * ((chosen * ((tiles + 1) / 2) + kCus - 1) / kCus);
+    return 7 * by_two <= 8 * by_one ? 2 : 1;
+}
 
 int few_sizes(const moe_few_tokens_desc* d, FewSizes* z) {
     if (!d) return MOE_ERR_INVALID_ARG;
@@ -128,15 +141,13 @@ int few_sizes(const moe_few_tokens_desc* d, FewSizes* z) {
         z->h_pitch = d->inter;
     }
     const int64_t rows = (int64_t)d->T * d->k, slots = rows < d->E ? rows : d->E;
-    // Workgroups that are resident at once: two per CU, one where the staged tokens leave no LDS for a second (16 tokens, 64 experts,
-    // 2048 / 1408: 75 -> 69 us).  A part of the second launch is at least a step for each of its wavefronts.
-    const int first = mx4 ? few_lds_bytes<FewMx4>(d->T) + FewMx4::lds_bytes(d->T, d->hidden) : few_lds_bytes<FewBf16>(d->T);
-    const int resident = first <= kFewLdsMost && first > kFewLdsMost / 2 ? kCus : 2 * kCus;
-    const int groups = mx4 ? FewMx4::GROUP : FewBf16::GROUP;
-    const int64_t tiles = slots * ((z->tiles1 + groups - 1) / groups), steps = slots * z->steps2;
+    // A workgroup per CU.  (Two, where LDS holds them: 4 bits within 3 % either way; bf16, 8 experts, 4096 / 14336, 5 tokens 404 us instead
+    // of 361.)  A part of the second launch is at least a step for each of its wavefronts.
+    z->group1 = mx4 ? 2 : few_group(d, z->tiles1);
+    const int64_t tiles = slots * ((z->tiles1 + z->group1 - 1) / z->group1), steps = slots * z->steps2;
     int64_t parts = (kCus + z->tiles2 - 1) / z->tiles2;
     if (parts > (steps + kFewWaves - 1) / kFewWaves) parts = (steps + kFewWaves - 1) / kFewWaves;
-    z->grid1 = (int)(tiles < resident ? tiles : resident);
+    z->grid1 = (int)(tiles < kCus ? tiles : kCus);
     z->parts2 = (int)(parts < 1 ? 1 : parts);
     z->h_bytes = mx4 ? 2 * up256((size_t)rows * z->h_pitch) + up256((size_t)rows * (z->h_pitch / kMxBlock)) : up256((size_t)rows * z->h_pitch * 2);
     z->partial_bytes = up256((size_t)z->tiles2 * z->parts2 * kFewTokens * (mx4 ? FewMx4::COLS : FewBf16::COLS) * sizeof(float));
@@ -144,30 +155,33 @@ int few_sizes(const moe_few_tokens_desc* d, FewSizes* z) {
     return MOE_OK;
 }
 
-template <class W, int EPL, class Src, bool STAGED>
+template <class W, int NC, int EPL, class Src, bool STAGED>
 int launch_few(const FewArgs& a, int grid1, hipStream_t s) {
     const int lds = few_lds_bytes<W>(a.route.T);
     static unsigned long long done1 = 0, done2 = 0;
-    if (ensure_lds_attr(reinterpret_cast<const void*>(&few_tokens_up<W, EPL, Src, STAGED>), STAGED ? kFewLdsMost : few_lds_bytes<W>(kFewTokens), &done1) != MOE_OK ||
+    if (ensure_lds_attr(reinterpret_cast<const void*>(&few_tokens_up<W, NC, EPL, Src, STAGED>), STAGED ? kFewLdsMost : few_lds_bytes<W>(kFewTokens), &done1) != MOE_OK ||
         ensure_lds_attr(reinterpret_cast<const void*>(&few_tokens_down<W>), few_lds_bytes<W>(kFewTokens), &done2) != MOE_OK) return MOE_ERR_HIP;
-    few_tokens_up<W, EPL, Src, STAGED><<<dim3(grid1), kFewThreads, lds + (STAGED ? W::lds_bytes(a.route.T, a.hidden) : 0), s>>>(a);
+    few_tokens_up<W, NC, EPL, Src, STAGED><<<dim3(grid1), kFewThreads, lds + (STAGED ? W::lds_bytes(a.route.T, a.hidden) : 0), s>>>(a);
     const int rc = launched();
     if (rc != MOE_OK) return rc;
     few_tokens_down<W><<<dim3(a.tiles2 * a.parts2), kFewThreads, lds, s>>>(a);
     return launched();
 }
 template <class W, int EPL, class Src>
-int launch_few(const FewArgs& a, int grid1, hipStream_t s) {
-    if constexpr (std::is_same<W, FewMx4>::value)
+int launch_few(const FewArgs& a, const FewSizes& z, hipStream_t s) {
+    if constexpr (std::is_same<W, FewMx4>::value) {
         if (few_lds_bytes<W>(a.route.T) + W::lds_bytes(a.route.T, a.hidden) <= kFewLdsMost)
-            return launch_few<W, EPL, Src, true>(a, grid1, s);
-    return launch_few<W, EPL, Src, false>(a, grid1, s);
+            return launch_few<W, 2, EPL, Src, true>(a, z.grid1, s);
+        return launch_few<W, 2, EPL, Src, false>(a, z.grid1, s);
+    } else {
+        return z.group1 == 2 ? launch_few<W, 2, EPL, Src, false>(a, z.grid1, s) : launch_few<W, 1, EPL, Src, false>(a, z.grid1, s);
+    }
 }
 template <class W, class Src>
-int launch_few(const FewArgs& a, int grid1, hipStream_t s) {
-    if (a.route.E <= 64) return launch_few<W, 1, Src>(a, grid1, s);
-    if (a.route.E <= 256) return launch_few<W, 4, Src>(a, grid1, s);
-    return launch_few<W, 16, Src>(a, grid1, s);
+int launch_few(const FewArgs& a, const FewSizes& z, hipStream_t s) {
+    if (a.route.E <= 64) return launch_few<W, 1, Src>(a, z, s);
+    if (a.route.E <= 256) return launch_few<W, 4, Src>(a, z, s);
+    return launch_few<W, 16, Src>(a, z, s);
 }
 
 }  // namespace
@@ -315,8 +329,8 @@ int moe_layer_few_tokens(const void* X, const void* logits, const void* w_up, co
     a.tiles1 = z.tiles1; a.steps1 = z.steps1; a.tiles2 = z.tiles2; a.steps2 = z.steps2; a.parts2 = z.parts2;
     const hipStream_t s = static_cast<hipStream_t>(stream);
     const bool f32 = d->logits_dtype == MOE_DTYPE_FP32;
-    if (mx4) return f32 ? launch_few<FewMx4, float>(a, z.grid1, s) : launch_few<FewMx4, uint16_t>(a, z.grid1, s);
-    return f32 ? launch_few<FewBf16, float>(a, z.grid1, s) : launch_few<FewBf16, uint16_t>(a, z.grid1, s);
+    if (mx4) return f32 ? launch_few<FewMx4, float>(a, z, s) : launch_few<FewMx4, uint16_t>(a, z, s);
+    return f32 ? launch_few<FewBf16, float>(a, z, s) : launch_few<FewBf16, uint16_t>(a, z, s);
 }
 
 }  // extern "C"
