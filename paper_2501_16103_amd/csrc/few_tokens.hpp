@@ -42,6 +42,7 @@ struct FewArgs {
     uint16_t* h;                  // bf16 weights: [T * k][h_pitch] bf16
     uint8_t *h_hi, *h_lo;         // 4-bit weights: [T * k][h_pitch] e4m3, see FewMx4
     uint8_t* h_scales;            // [T * k][h_pitch / 32]
+    char* x_split;                // 4-bit weights, tokens that LDS does not hold: FewMx4::token_bytes each
     float* partial;               // [column tile][part][16][columns of a tile]
     int* arrived;                 // [column tile]
     int hidden, inter, h_pitch;
@@ -97,7 +98,6 @@ struct FewMx4 {
     static constexpr int KSTEP = kMxTileK, COLS = kMxTileN, BLOCKS = 4;
     template <bool STAGED> static constexpr int AHEAD_UP = STAGED ? 3 : 1;   // steps that loads are ahead, as far as registers go
     static constexpr int AHEAD_DOWN = 1;
-    struct Raw { u32x4_t x[4]; };
     struct Tokens {
         i32x8_t hi, lo;
         uint32_t scale;           // byte 0: of hi, byte 1: of lo
@@ -127,56 +127,18 @@ struct FewMx4 {
         for (int i = 0; i < 4; ++i) w[i] = __builtin_nontemporal_load(p + 64 * i);
         scale = __builtin_nontemporal_load(reinterpret_cast<const uint32_t*>(scales + tile * kMxTileScales) + __lane_id());
     }
-    // bf16 tokens.  xrow: this lane's token row; valid: elements of it (a multiple of 8)
-    static __device__ __forceinline__ void load(Raw& t, const uint16_t* xrow, int kb, int valid) {
-#pragma unroll
-        for (int q = 0; q < 4; ++q) {
-            const int k = kb * KSTEP + 16 * (__lane_id() >> 4) + 64 * (q >> 1) + 8 * (q & 1);
-            t.x[q] = k < valid ? *reinterpret_cast<const u32x4_t*>(xrow + k) : u32x4_t{0u, 0u, 0u, 0u};
-        }
-    }
-    static __device__ __forceinline__ void convert(Tokens& t, const Raw& r) {
-        // the lane's two halves belong to blocks g / 2 and 2 + g / 2, which the lanes of g ^ 1 hold the rest of
-        uint32_t byte[2];
-#pragma unroll
-        for (int half = 0; half < 2; ++half) {
-            uint32_t m = 0;
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                const uint32_t v = r.x[2 * half + i / 4][i % 4], a = (v << 16) & 0x7fffffffu, b = v & 0x7fff0000u;
-                m = a > m ? a : m;
-                m = b > m ? b : m;
-            }
-            const uint32_t o = (uint32_t)__shfl_xor((int)m, 16);
-            byte[half] = scale_byte(o > m ? o : m);
-            const float inv = inverse(byte[half]);
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const uint32_t p = r.x[2 * half + i / 2][2 * (i % 2)], q = r.x[2 * half + i / 2][2 * (i % 2) + 1];
-                const float v[4] = {__uint_as_float(p << 16) * inv, __uint_as_float(p & 0xffff0000u) * inv, __uint_as_float(q << 16) * inv,
-                                    __uint_as_float(q & 0xffff0000u) * inv};
-                int h, l;
-                split(v, h, l);
-                t.hi[4 * half + i] = h;
-                t.lo[4 * half + i] = l;
-            }
-        }
-        // block g's byte: lanes of 2 g, first half (g < 2), lanes of 2 g - 4, second half
-        const int lane = __lane_id(), g = lane >> 4, from = ((2 * g) & 3) * 16 + (lane & 15);
-        const uint32_t first = (uint32_t)__shfl((int)byte[0], from), second = (uint32_t)__shfl((int)byte[1], from);
-        const uint32_t b = g < 2 ? first : second;
-        t.scale = b | (b - 4) << 8;
-    }
-    // All of X, split, in LDS: [T][pitch] hi, the same of lo, [T][pitch / 32] scales.  Rows are 16 bytes more than whole steps long, so
+    // T tokens, split: [T][pitch] hi, the same of lo, [T][pitch / 32] scales.  Rows are 16 bytes more than whole steps long, so
     // that the 16 rows of a fragment are spread over the banks.
     static __host__ __device__ constexpr int lds_pitch(int hidden) { return (hidden + KSTEP - 1) / KSTEP * KSTEP + 16; }
     static __host__ __device__ constexpr int lds_bytes(int T, int hidden) { return T * (2 * lds_pitch(hidden) + lds_pitch(hidden) / 32); }
+    // A token alone, in memory (where LDS does not hold them all)
+    static __host__ __device__ constexpr int token_bytes(int hidden) { return (lds_bytes(1, hidden) + 15) / 16 * 16; }
     // eight elements a thread, four threads a block (all threads; pieces beyond the row are zeros); BATCH pieces a thread are asked for at
     // a time, each batch a trip to memory
-    static __device__ __forceinline__ void stage(const uint16_t* X, int T, int hidden, char* lds) {
+    static __device__ __forceinline__ void stage(const uint16_t* X, int T, int hidden, char* to) {
         constexpr int BATCH = 4;
         const int pitch = lds_pitch(hidden), chunks = (pitch - 16) / 8, all = T * chunks;
-        uint8_t* hi = reinterpret_cast<uint8_t*>(lds);
+        uint8_t* hi = reinterpret_cast<uint8_t*>(to);
         uint8_t* lo = hi + T * pitch;
         uint8_t* scales = lo + T * pitch;
         for (int i0 = threadIdx.x; i0 < all; i0 += BATCH * kFewThreads) {     // (a multiple of 16 a row: the four threads stay together)
@@ -221,9 +183,9 @@ struct FewMx4 {
         }
     }
     // the fragment of step kb for token row t
-    static __device__ __forceinline__ void load(Tokens& f, const char* lds, int T, int hidden, int t, int kb) {
+    static __device__ __forceinline__ void load(Tokens& f, const char* from, int T, int hidden, int t, int kb) {
         const int pitch = lds_pitch(hidden), g = __lane_id() >> 4;
-        const char* hi = lds + t * pitch + kb * KSTEP + 16 * g;
+        const char* hi = from + t * pitch + kb * KSTEP + 16 * g;
         const char* lo = hi + T * pitch;
 #pragma unroll
         for (int half = 0; half < 2; ++half) {
@@ -234,7 +196,7 @@ struct FewMx4 {
                 f.lo[4 * half + i] = (int)l[i];
             }
         }
-        const uint32_t b = *reinterpret_cast<const uint8_t*>(lds + 2 * T * pitch + t * (pitch / 32) + kb * 4 + g);
+        const uint32_t b = *reinterpret_cast<const uint8_t*>(from + 2 * T * pitch + t * (pitch / 32) + kb * 4 + g);
         f.scale = b | (b - 4) << 8;
     }
     // activations that are split already.  valid: elements of a row that were written (a multiple of 32)
@@ -281,7 +243,6 @@ struct FewBf16 {
     template <bool> static constexpr int AHEAD_UP = 3;
     static constexpr int AHEAD_DOWN = 3;
     struct Tokens { u32x2_t x; };
-    using Raw = Tokens;
     static __host__ __device__ constexpr int lds_bytes(int, int) { return 0; }
     u32x4_t w[4];
     // base: row k = 0 of the expert; col: this lane's first column; N: columns of a weight row (K is a multiple of 8)
@@ -332,6 +293,11 @@ template <class W>
 constexpr int few_lds_bytes(int T) { return kFewWaves * T * W::COLS * (int)sizeof(float); }
 constexpr int kFewLdsMost = 160 * 1024 - 4096;      // (the routing takes less than 4 KB)
 static_assert(sizeof(FewRouting) + 64 <= 4096, "routing");
+
+// The tokens, split, in memory: a workgroup per token.
+__global__ __launch_bounds__(kFewThreads) void few_tokens_split(FewArgs a) {
+    FewMx4::stage(a.X + (int64_t)blockIdx.x * a.hidden, 1, a.hidden, a.x_split + (int64_t)blockIdx.x * FewMx4::token_bytes(a.hidden));
+}
 
 // First launch.  Workgroups take column tiles of the chosen experts, NC neighbouring ones at a time, one group after the other.
 template <class W, int NC, int EPL, class Src, bool STAGED>
@@ -400,22 +366,27 @@ __global__ __launch_bounds__(kFewThreads, 4) void few_tokens_up(FewArgs a) {
     };
     enter();
     const int mine = first < a.steps1 ? (a.steps1 - first + KW - 1) / KW : 0;   // k-steps of a tile that this wavefront takes
-    // STAGED: token fragments come out of LDS when their step is multiplied, and the registers hold the weights of three steps more;
+    // STAGED: token fragments come out of LDS when their step is multiplied, and the registers hold the weights of three steps;
     // otherwise they come along with the weights of their step.
+    auto load_tokens = [&](typename W::Tokens& t) __attribute__((always_inline)) {
+        if constexpr (STAGED) return;
+        else if constexpr (MX4) W::load(t, a.x_split + (int64_t)(li < T ? li : 0) * W::token_bytes(a.hidden), 1, a.hidden, 0, kb);
+        else W::load(t, xrow, kb, a.hidden);
+    };
     constexpr int AHEAD = W::template AHEAD_UP<STAGED>;
     W buf[AHEAD + 1];
-    typename W::Raw raw[STAGED ? 1 : AHEAD + 1];
+    typename W::Tokens tok[STAGED ? 1 : AHEAD + 1];
     bool more = mine > 0;
     if (more) {
         load(buf[0]);
-        if constexpr (!STAGED) W::load(raw[0], xrow, kb, a.hidden);
+        load_tokens(tok[0]);
     }
 #pragma unroll
     for (int i = 1; i < AHEAD; ++i) {
         more = more && advance();
         if (more) {
             load(buf[i]);
-            if constexpr (!STAGED) W::load(raw[i], xrow, kb, a.hidden);
+            load_tokens(tok[STAGED ? 0 : i]);
         }
     }
     for (int at = blockIdx.x; at < total; at += sharing) {
@@ -426,20 +397,14 @@ __global__ __launch_bounds__(kFewThreads, 4) void few_tokens_up(FewArgs a) {
             more = more && advance();
             if (more) {
                 load(buf[AHEAD]);
-                if constexpr (!STAGED) W::load(raw[AHEAD], xrow, kb, a.hidden);
+                load_tokens(tok[STAGED ? 0 : AHEAD]);
             }
-            if constexpr (MX4) {
-                typename W::Tokens tok;
-                if constexpr (STAGED) W::load(tok, tokens, T, a.hidden, li < T ? li : 0, first + i * KW);
-                else W::convert(tok, raw[0]);
-                buf[0].multiply(tok, acc);
-            } else {
-                buf[0].multiply(raw[0], acc);
-            }
+            if constexpr (STAGED) W::load(tok[0], tokens, T, a.hidden, li < T ? li : 0, first + i * KW);
+            buf[0].multiply(tok[0], acc);
 #pragma unroll
             for (int b = 0; b < AHEAD; ++b) {
                 buf[b] = buf[b + 1];
-                if constexpr (!STAGED) raw[b] = raw[b + 1];
+                if constexpr (!STAGED) tok[b] = tok[b + 1];
             }
         }
         if (li < T) W::each(acc, [&](int col, f32x4_t v) { *reinterpret_cast<f32x4_t*>(sums + (wave * T + li) * W::COLS + col) = v; });

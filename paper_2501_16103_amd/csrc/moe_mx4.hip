@@ -100,7 +100,7 @@ const Mx4Tile* find_mx4_tile(int tile_m, int tile_n) {
 // Sizes of the layer for few tokens that follow from its description.
 struct FewSizes {
     int tiles1, steps1, tiles2, steps2, parts2, h_pitch, group1, grid1;
-    size_t h_bytes, partial_bytes, arrived_bytes;
+    size_t h_bytes, partial_bytes, arrived_bytes, split_bytes;
 };
 constexpr size_t up256(size_t n) { return (n + 255) / 256 * 256; }
 
@@ -116,6 +116,8 @@ int few_group(const moe_few_tokens_desc* d, int tiles) {
     const int64_t by_one = (chosen * tiles + kCus - 1) / kCus, by_two = 2 * ((chosen * ((tiles + 1) / 2) + kCus - 1) / kCus);
     return 7 * by_two <= 8 * by_one ? 2 : 1;
 }
+
+bool few_staged(int T, int hidden) { return few_lds_bytes<FewMx4>(T) + FewMx4::lds_bytes(T, hidden) <= kFewLdsMost; }
 
 int few_sizes(const moe_few_tokens_desc* d, FewSizes* z) {
     if (!d) return MOE_ERR_INVALID_ARG;
@@ -152,6 +154,7 @@ int few_sizes(const moe_few_tokens_desc* d, FewSizes* z) {
     z->h_bytes = mx4 ? 2 * up256((size_t)rows * z->h_pitch) + up256((size_t)rows * (z->h_pitch / kMxBlock)) : up256((size_t)rows * z->h_pitch * 2);
     z->partial_bytes = up256((size_t)z->tiles2 * z->parts2 * kFewTokens * (mx4 ? FewMx4::COLS : FewBf16::COLS) * sizeof(float));
     z->arrived_bytes = up256((size_t)z->tiles2 * sizeof(int));
+    z->split_bytes = mx4 && !few_staged(d->T, d->hidden) ? (size_t)d->T * FewMx4::token_bytes(d->hidden) : 0;
     return MOE_OK;
 }
 
@@ -170,8 +173,10 @@ int launch_few(const FewArgs& a, int grid1, hipStream_t s) {
 template <class W, int EPL, class Src>
 int launch_few(const FewArgs& a, const FewSizes& z, hipStream_t s) {
     if constexpr (std::is_same<W, FewMx4>::value) {
-        if (few_lds_bytes<W>(a.route.T) + W::lds_bytes(a.route.T, a.hidden) <= kFewLdsMost)
-            return launch_few<W, 2, EPL, Src, true>(a, z.grid1, s);
+        if (few_staged(a.route.T, a.hidden)) return launch_few<W, 2, EPL, Src, true>(a, z.grid1, s);
+        few_tokens_split<<<dim3(a.route.T), kFewThreads, 0, s>>>(a);
+        const int rc = launched();
+        if (rc != MOE_OK) return rc;
         return launch_few<W, 2, EPL, Src, false>(a, z.grid1, s);
     } else {
         return z.group1 == 2 ? launch_few<W, 2, EPL, Src, false>(a, z.grid1, s) : launch_few<W, 1, EPL, Src, false>(a, z.grid1, s);
@@ -295,7 +300,7 @@ int moe_mx4_grouped_gemm(const void* x_codes, const void* x_scales, const void* 
 
 size_t moe_few_tokens_workspace_bytes(const moe_few_tokens_desc* d) {
     FewSizes z;
-    return few_sizes(d, &z) != MOE_OK || d->T == 0 ? 0 : z.h_bytes + z.partial_bytes + z.arrived_bytes;
+    return few_sizes(d, &z) != MOE_OK || d->T == 0 ? 0 : z.h_bytes + z.partial_bytes + z.arrived_bytes + z.split_bytes;
 }
 
 int moe_layer_few_tokens(const void* X, const void* logits, const void* w_up, const void* up_scales, const void* w_down, const void* down_scales,
@@ -310,7 +315,7 @@ int moe_layer_few_tokens(const void* X, const void* logits, const void* w_up, co
     if (mx4 && (!up_scales || !down_scales || misaligned(up_scales, 16) || misaligned(down_scales, 16))) return MOE_ERR_INVALID_ARG;
     if (misaligned(X, 16) || misaligned(w_up, 16) || misaligned(w_down, 16) || misaligned(out, 2) || misaligned(workspace, 16) || misaligned(topk_ids, 4) ||
         misaligned(topk_weights, 4) || misaligned(logits, d->logits_dtype == MOE_DTYPE_FP32 ? 4 : 2)) return MOE_ERR_INVALID_ARG;
-    if (workspace_bytes < z.h_bytes + z.partial_bytes + z.arrived_bytes) return MOE_ERR_INVALID_ARG;
+    if (workspace_bytes < z.h_bytes + z.partial_bytes + z.arrived_bytes + z.split_bytes) return MOE_ERR_INVALID_ARG;
     FewArgs a{};
     a.route = RouteArgs{logits, d->E, d->T, d->E, d->k, d->score == MOE_SCORE_SIGMOID, d->renormalize != 0, d->scale};
     a.X = static_cast<const uint16_t*>(X);
@@ -325,6 +330,7 @@ int moe_layer_few_tokens(const void* X, const void* logits, const void* w_up, co
     a.h_scales = a.h_lo + h_bytes;
     a.partial = reinterpret_cast<float*>(w + z.h_bytes);
     a.arrived = reinterpret_cast<int*>(w + z.h_bytes + z.partial_bytes);
+    a.x_split = w + z.h_bytes + z.partial_bytes + z.arrived_bytes;
     a.hidden = d->hidden; a.inter = d->inter; a.h_pitch = z.h_pitch;
     a.tiles1 = z.tiles1; a.steps1 = z.steps1; a.tiles2 = z.tiles2; a.steps2 = z.steps2; a.parts2 = z.parts2;
     const hipStream_t s = static_cast<hipStream_t>(stream);

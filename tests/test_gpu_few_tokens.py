@@ -177,6 +177,18 @@ def test_same_bits_again_on_streams_and_from_a_graph(mx4):
         assert torch.equal(plan.out, first[seed][0]) and torch.equal(plan.ids, first[seed][1])
 
 
+@pytest.mark.parametrize("T,k,E,hidden,inter", [(16, 2, 3, 4712, 40), (16, 3, 300, 4608, 16), (9, 2, 2, 8200, 24)])
+def test_more_token_values_than_lds_holds(T, k, E, hidden, inter):
+    data = _inputs(T, E, hidden, inter, hidden)
+    _check(_run(*data, k, True), _expected(*data, k, True))
+
+
+@pytest.mark.parametrize("T,k,E,hidden,inter", [(8, 2, 16, 72, 2048), (8, 2, 16, 40, 2104), (16, 4, 300, 16, 448)])
+def test_column_tiles_by_twos(T, k, E, hidden, inter):
+    data = _inputs(T, E, hidden, inter, inter)
+    _check(_run(*data, k, False), _expected(*data, k, False))
+
+
 def test_no_tokens():
     plan = mb.MoeFewTokensPlan(0, 2, 4, 64, 64, device=DEV)
     e = lambda *s: torch.empty(*s, dtype=torch.bfloat16, device=DEV)
