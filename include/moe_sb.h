@@ -498,6 +498,10 @@ int moe_route(const void* logits, const moe_route_desc* desc, int32_t* topk_ids,
  * rows * Kp < 2^35, else MOE_ERR_UNSUPPORTED.
  */
 int moe_mx4_quantize(const void* src, int dtype, int64_t rows, int cols, int64_t row_stride, void* codes, void* scales, void* values, void* stream);
+/* What a 4-bit product reads beside its weights, by one launch up to 16384 routed rows: moe_build_task_map_ex(topk_ids, T, k, E, N, tiling,
+ * task_map) and moe_mx4_quantize of the T token rows X of K elements (no values), with the arguments, results and refusals of those two. */
+int moe_mx4_prepare(const int32_t* topk_ids, int T, int k, int E, int N, const moe_tiling* tiling, void* task_map, const void* X, int dtype, int K,
+                    int64_t row_stride, void* codes, void* scales, void* stream);
 /* Bytes of the two buffers (HOST, pure; 0 on invalid arguments). */
 size_t moe_mx4_row_code_bytes(int64_t rows, int cols);
 size_t moe_mx4_row_scale_bytes(int64_t rows, int cols);

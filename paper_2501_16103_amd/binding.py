@@ -65,7 +65,7 @@ EXPORTS = [
     "moe_grouped_gemm_splitk", "moe_splitk_workspace_bytes", "moe_default_k_parts",
     "moe_grouped_gemm_splitk_static", "moe_splitk_static_scratch_bytes",
     "moe_grouped_gemm_batched", "moe_reduce_task_tiles", "moe_grouped_gemm_tail_split", "moe_tail_split_workspace_bytes", "moe_default_tail_split",
-    "moe_route", "moe_mx4_quantize", "moe_mx4_row_code_bytes", "moe_mx4_row_scale_bytes", "moe_mx4_pack_weights",
+    "moe_route", "moe_mx4_quantize", "moe_mx4_prepare", "moe_mx4_row_code_bytes", "moe_mx4_row_scale_bytes", "moe_mx4_pack_weights",
     "moe_mx4_weight_code_bytes", "moe_mx4_weight_scale_bytes", "moe_mx4_packed_columns", "moe_mx4_grouped_gemm",
     "moe_mx4_tile_supported", "moe_mx4_default_tiling", "moe_layer_few_tokens", "moe_few_tokens_workspace_bytes",
     "moe_strerror",
@@ -197,6 +197,9 @@ def lib() -> ctypes.CDLL:
         L.moe_default_k_parts.argtypes = [ctypes.c_int] * 5
         L.moe_route.restype = ctypes.c_int
         L.moe_route.argtypes = [ctypes.c_void_p, ctypes.POINTER(moe_route_desc)] + [ctypes.c_void_p] * 3
+        L.moe_mx4_prepare.restype = ctypes.c_int
+        L.moe_mx4_prepare.argtypes = ([ctypes.c_void_p] + [ctypes.c_int] * 4 + [ctypes.POINTER(moe_tiling), ctypes.c_void_p, ctypes.c_void_p, ctypes.c_int, ctypes.c_int,
+                                      ctypes.c_int64] + [ctypes.c_void_p] * 3)
         L.moe_mx4_quantize.restype = ctypes.c_int
         L.moe_mx4_quantize.argtypes = [ctypes.c_void_p, ctypes.c_int, ctypes.c_int64, ctypes.c_int, ctypes.c_int64] + [ctypes.c_void_p] * 4
         for n in ("moe_mx4_row_code_bytes", "moe_mx4_row_scale_bytes"):
@@ -549,6 +552,18 @@ def moe_mx4_quantize(src: torch.Tensor, codes: torch.Tensor, scales: torch.Tenso
     return rc
 
 
+def moe_mx4_prepare(topk_ids: torch.Tensor, T: int, k: int, E: int, N: int, tiling: Tiling, task_map: torch.Tensor, X: torch.Tensor, codes: torch.Tensor,
+                    scales: torch.Tensor, check: bool = True) -> int:
+    """moe_build_task_map_ex and moe_mx4_quantize of X [T, K] by one launch (N: the weights' packed columns)."""
+    K, (row, step) = X.shape[1], X.stride()
+    g = tiling.c_struct()
+    rc = MOE_ERR_INVALID_ARG if X.shape[0] != T or (step != 1 and K > 1) else lib().moe_mx4_prepare(
+        topk_ids.data_ptr(), T, k, E, N, ctypes.byref(g), task_map.data_ptr(), X.data_ptr(), _dtype(X), K, row, codes.data_ptr(), scales.data_ptr(), _stream())
+    if check and rc != MOE_OK:
+        raise MoeError(rc, "moe_mx4_prepare")
+    return rc
+
+
 def moe_mx4_row_code_bytes(rows: int, cols: int) -> int:
     return int(lib().moe_mx4_row_code_bytes(rows, cols))
 
@@ -655,7 +670,7 @@ def moe_mx4_grouped_gemm(X: Mx4Rows, W: Mx4Weights, T: int, k: int, task_map: to
 
 
 class MoeMx4ProductPlan:
-    """Buffers and tiling of one product over 4-bit experts: quantise the tokens -> task map -> product, on the current stream.
+    """Buffers and tiling of one product over 4-bit experts: task map and tokens in 4 bits -> product, on the current stream.
     gated: the experts' weights are [gate | up] halves and the product ends with the gated activation."""
 
     def __init__(self, T: int, k: int, E: int, K: int, N: int, gated: bool = False, device="cuda:0"):
@@ -673,8 +688,7 @@ class MoeMx4ProductPlan:
         _contiguous("MoeMx4ProductPlan.forward", topk_ids, (self.T, self.k), torch.int32)
         if self.T == 0:
             return self.out
-        moe_build_task_map_ex(topk_ids, self.T, self.k, self.E, self.columns, self.g, self.map)
-        self.rows.quantize(X)
+        moe_mx4_prepare(topk_ids, self.T, self.k, self.E, self.columns, self.g, self.map, X, self.rows.codes, self.rows.scales)
         moe_mx4_grouped_gemm(self.rows, W, self.T, self.k, self.map, self.out, self.g)
         return self.out
 

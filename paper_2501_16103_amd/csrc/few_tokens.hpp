@@ -546,7 +546,8 @@ __global__ __launch_bounds__(kFewThreads, 4) void few_tokens_down(FewArgs a) {
     };
     // Sums that other workgroups read go through to memory, agent-scope stores as they are, and each wavefront waits until its own have
     // arrived there before the barrier in front of the workgroup's arrival; the last one's loads are agent-scope too and do not
-    // look into caches.  (A release and an acquire fence instead write back and invalidate a whole L2: FENCEFIGURE.)
+    // look into caches.  (A release and an acquire fence instead write back and invalidate a whole L2: 2 to 4 us of the second launch
+    // instead of 0.6 to 1, one token, 64 experts.)
     float* const part_sums = a.partial + ((int64_t)c * a.parts2 + part) * (kFewTokens * W::COLS);
     for (int i = tid; i < T * W::COLS; i += kFewThreads) {
         float v = 0.f;

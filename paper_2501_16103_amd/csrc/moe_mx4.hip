@@ -57,6 +57,16 @@ int launch_pack(const void* W, int nk, int64_t tiles, int K, int N, int gated, i
     return launched();
 }
 
+int check_quantize(const void* src, int dtype, int64_t rows, int cols, int64_t row_stride, const void* codes, const void* scales, const void* values) {
+    if (rows < 0 || cols < 1 || (rows > 1 && row_stride < cols)) return MOE_ERR_INVALID_ARG;
+    if (dtype != MOE_DTYPE_FP32 && dtype != MOE_DTYPE_BF16) return MOE_ERR_UNSUPPORTED;
+    if (cols > (1 << 30) || rows > ((int64_t)1 << 32) || rows * (mx4_padded_k(cols) / 8) > 0xffffff00ll) return MOE_ERR_UNSUPPORTED;
+    if (rows == 0) return MOE_OK;
+    if (!src || !codes || !scales || misaligned(codes, 16) || misaligned(scales, 4) || misaligned(values, 2) ||
+        misaligned(src, dtype == MOE_DTYPE_FP32 ? 4 : 2)) return MOE_ERR_INVALID_ARG;
+    return MOE_OK;
+}
+
 template <class Src>
 int launch_quantize(const void* src, int64_t rows, int cols, int64_t row_stride, void* codes, void* scales, void* values, hipStream_t s) {
     const int64_t chunks = rows * (mx4_padded_k(cols) / 8);
@@ -66,6 +76,30 @@ int launch_quantize(const void* src, int64_t rows, int cols, int64_t row_stride,
     if (vec) mx4_quantize_rows<Src, true><<<grid, 256, 0, s>>>(p, rows, cols, row_stride, static_cast<uint32_t*>(codes), static_cast<uint8_t*>(scales), static_cast<uint16_t*>(values));
     else mx4_quantize_rows<Src, false><<<grid, 256, 0, s>>>(p, rows, cols, row_stride, static_cast<uint32_t*>(codes), static_cast<uint8_t*>(scales), static_cast<uint16_t*>(values));
     return launched();
+}
+
+template <class Src, bool VEC, bool SMALL>
+int launch_prepare(const int32_t* ids, int32_t* map, int builders, int threads, size_t lds, int T, int k, int E, int N, const moe_tiling& g, const Src* X, int K,
+                   int64_t row_stride, void* codes, void* scales, hipStream_t s) {
+    static unsigned long long done = 0;
+    if (ensure_lds_attr(reinterpret_cast<const void*>(&mx4_map_and_rows<Src, VEC, SMALL>),
+                        (int)(SMALL ? small_build_lds(kMapThreads, kMaxE) : scan_scatter_lds(kMaxE)), &done) != MOE_OK) return MOE_ERR_HIP;
+    const int64_t pieces = T * (mx4_padded_k(K) / 8), grid = builders + (pieces + threads - 1) / threads;
+    mx4_map_and_rows<Src, VEC, SMALL><<<dim3((unsigned)grid), threads, lds, s>>>(ids, map, builders, T, k, E, N, g, X, K, row_stride, static_cast<uint32_t*>(codes),
+                                                                                 static_cast<uint8_t*>(scales));
+    return launched();
+}
+template <class Src>
+int launch_prepare(const int32_t* ids, int32_t* map, int T, int k, int E, int N, const moe_tiling& g, const void* X, int K, int64_t row_stride, void* codes,
+                   void* scales, hipStream_t s) {
+    const int64_t R = (int64_t)T * k;
+    const bool small = R <= kChunkRows, vec = K % 8 == 0 && row_stride % (16 / (int)sizeof(Src)) == 0 && !misaligned(X, 16);
+    const int E64 = map_layout(E).E64, builders = (int)((R + kChunkRows - 1) / kChunkRows), threads = small ? small_build_threads(R, E64) : kMapThreads;
+    const size_t lds = small ? small_build_lds(threads, E64) : scan_scatter_lds(E64);
+    const Src* x = static_cast<const Src*>(X);
+    const auto launch = vec ? (small ? &launch_prepare<Src, true, true> : &launch_prepare<Src, true, false>)
+                            : (small ? &launch_prepare<Src, false, true> : &launch_prepare<Src, false, false>);
+    return launch(ids, map, builders, threads, lds, T, k, E, N, g, x, K, row_stride, codes, scales, s);
 }
 
 template <int MB>
@@ -213,12 +247,8 @@ size_t moe_mx4_row_scale_bytes(int64_t rows, int cols) {
 }
 
 int moe_mx4_quantize(const void* src, int dtype, int64_t rows, int cols, int64_t row_stride, void* codes, void* scales, void* values, void* stream) {
-    if (rows < 0 || cols < 1 || (rows > 1 && row_stride < cols)) return MOE_ERR_INVALID_ARG;
-    if (dtype != MOE_DTYPE_FP32 && dtype != MOE_DTYPE_BF16) return MOE_ERR_UNSUPPORTED;
-    if (cols > (1 << 30) || rows > ((int64_t)1 << 32) || rows * (mx4_padded_k(cols) / 8) > 0xffffff00ll) return MOE_ERR_UNSUPPORTED;
-    if (rows == 0) return MOE_OK;
-    if (!src || !codes || !scales || misaligned(codes, 16) || misaligned(scales, 4) || misaligned(values, 2) ||
-        misaligned(src, dtype == MOE_DTYPE_FP32 ? 4 : 2)) return MOE_ERR_INVALID_ARG;
+    const int rc = check_quantize(src, dtype, rows, cols, row_stride, codes, scales, values);
+    if (rc != MOE_OK || rows == 0) return rc;
     const hipStream_t s = static_cast<hipStream_t>(stream);
     if (rows == 1) row_stride = 0;
     return dtype == MOE_DTYPE_FP32 ? launch_quantize<float>(src, rows, cols, row_stride, codes, scales, values, s)
@@ -268,6 +298,27 @@ int moe_mx4_default_tiling(int T, int k, int E, int K, int N, int gated, moe_til
     const moe_tiling g = {R > 16 * (int64_t)E ? 128 : R > 8 * (int64_t)E ? 32 : 16, 256, MOE_ORDER_ASCENDING, 0, 0, 0};
     *out = g;
     return MOE_OK;
+}
+
+int moe_mx4_prepare(const int32_t* topk_ids, int T, int k, int E, int N, const moe_tiling* tiling, void* task_map, const void* X, int dtype, int K,
+                    int64_t row_stride, void* codes, void* scales, void* stream) {
+    if (!tiling) return MOE_ERR_INVALID_ARG;
+    const int rcq = check_quantize(X, dtype, T, K, row_stride, codes, scales, nullptr);
+    if (rcq != MOE_OK) return rcq;
+    // One launch: with the tilings of the 4-bit products, and up to kFusedChunks chunks of routed rows (more need a launch of their own
+    // before the map's, and the rows' own time counts there).
+    const bool order = tiling->order == MOE_ORDER_ASCENDING || tiling->order == MOE_ORDER_SPREAD || tiling->order == MOE_ORDER_INTERLEAVE;
+    const bool plain = find_mx4_tile(tiling->tile_m, tiling->tile_n) && order && tiling->tile_m_small == 0 && tiling->small_max_rows == 0 && tiling->tile_m_slack == 0;
+    const bool sizes = T > 0 && E >= 1 && E <= kMaxE && k >= 1 && k <= E && N >= 1 && (int64_t)T * k <= (int64_t)kFusedChunks * kChunkRows &&
+                       T * (mx4_padded_k(K) / 8) <= 0xffffff00ll - (kFusedChunks + 1) * kMapThreads;
+    if (!plain || !sizes || !topk_ids || !task_map || misaligned(topk_ids, 4) || misaligned(task_map, 16)) {
+        const int rc = moe_build_task_map_ex(topk_ids, T, k, E, N, tiling, task_map, stream);   // (what is wrong here is refused there)
+        return rc != MOE_OK ? rc : moe_mx4_quantize(X, dtype, T, K, row_stride, codes, scales, nullptr, stream);
+    }
+    int32_t* map = static_cast<int32_t*>(task_map);
+    if (T == 1) row_stride = 0;
+    return dtype == MOE_DTYPE_FP32 ? launch_prepare<float>(topk_ids, map, T, k, E, N, *tiling, X, K, row_stride, codes, scales, static_cast<hipStream_t>(stream))
+                                   : launch_prepare<uint16_t>(topk_ids, map, T, k, E, N, *tiling, X, K, row_stride, codes, scales, static_cast<hipStream_t>(stream));
 }
 
 int moe_mx4_grouped_gemm(const void* x_codes, const void* x_scales, const void* w_codes, const void* w_scales, const void* task_map, void* Y,

@@ -500,9 +500,9 @@ int build_maps(const int32_t* topk_ids, int T, int k, int E, int N, const moe_ti
         }
         static unsigned long long attr_done2 = 0;
         if (ensure_lds_attr(reinterpret_cast<const void*>(&map_scan_scatter),
-                            (int)(((size_t)(kWaves + 1) * kMaxE + 2 * hist_stride(kMaxE)) * sizeof(int)), &attr_done2) != MOE_OK)
+                            (int)scan_scatter_lds(kMaxE), &attr_done2) != MOE_OK)
             return MOE_ERR_HIP;
-        map_scan_scatter<<<nchunks, kMapThreads, ((size_t)(kWaves + 1) * L.E64 + 2 * hs) * sizeof(int), s>>>(
+        map_scan_scatter<<<nchunks, kMapThreads, scan_scatter_lds(L.E64), s>>>(
             topk_ids, map, chunk_hist, nchunks, T, k, E, N, g, twin);
     }
     return hipGetLastError() == hipSuccess ? MOE_OK : MOE_ERR_HIP;

@@ -78,11 +78,9 @@ __device__ __forceinline__ float mx4_load(const float* p) { return *p; }
 // Token rows.  A lane takes eight elements of a row, four lanes a block.  VEC: rows begin on 16 bytes and are a multiple
 // of eight long, and every lane moves its elements with one or two 16-byte loads.
 template <class Src, bool VEC>
-__global__ __launch_bounds__(256) void mx4_quantize_rows(const Src* __restrict__ src, int64_t rows, int cols, int64_t row_stride,
-                                                         uint32_t* __restrict__ codes, uint8_t* __restrict__ scales,
-                                                         uint16_t* __restrict__ values) {
+__device__ __forceinline__ void mx4_quantize_piece(int64_t c, const Src* __restrict__ src, int64_t rows, int cols, int64_t row_stride,
+                                                   uint32_t* __restrict__ codes, uint8_t* __restrict__ scales, uint16_t* __restrict__ values) {
     const int cpr = (int)(mx4_padded_k(cols) >> 3);   // eight-element chunks of a padded row: a multiple of 16
-    const int64_t c = (int64_t)blockIdx.x * 256 + threadIdx.x;
     const int64_t row = c / cpr;
     if (row >= rows) return;                          // (the four lanes of a block leave together)
     const int at = (int)(c - row * cpr) * 8;
@@ -133,6 +131,13 @@ __global__ __launch_bounds__(256) void mx4_quantize_rows(const Src* __restrict__
             for (int i = 0; i < 8 && at + i < cols; ++i) q[i] = (uint16_t)(o[i >> 1] >> (16 * (i & 1)));
         }
     }
+}
+
+template <class Src, bool VEC>
+__global__ __launch_bounds__(256) void mx4_quantize_rows(const Src* __restrict__ src, int64_t rows, int cols, int64_t row_stride,
+                                                         uint32_t* __restrict__ codes, uint8_t* __restrict__ scales,
+                                                         uint16_t* __restrict__ values) {
+    mx4_quantize_piece<Src, VEC>((int64_t)blockIdx.x * 256 + threadIdx.x, src, rows, cols, row_stride, codes, scales, values);
 }
 
 // Column of the source that packed column p holds, or -1 (padding).

@@ -404,4 +404,20 @@ __global__ __launch_bounds__(256 * WM, 2) void mx4_gemm_lds(Mx4GemmArgs a) {
     }
 }
 
+// A product's task map and its token rows in 4 bits, by one launch: the first `builders` workgroups build the map (one of them up to
+// kChunkRows routed rows, else one per chunk of them), the others quantise.  Both are a few us of latency, which pass side by side (us, two
+// launches / one: 128 tokens of 2048, 6 of 64 experts 5.7 / 3.8; 1111 of 3584, 8 of 64 8.5 / 5.8; 4096 of 4096, 2 of 8 14.2 / 11.1).
+template <class Src, bool VEC, bool SMALL>
+__global__ __launch_bounds__(kMapThreads) void mx4_map_and_rows(const int32_t* __restrict__ ids, int32_t* __restrict__ map, int builders, int T, int k,
+                                                                int E, int N, moe_tiling g, const Src* __restrict__ src, int cols, int64_t row_stride,
+                                                                uint32_t* __restrict__ codes, uint8_t* __restrict__ scales) {
+    extern __shared__ int s_mem[];
+    if ((int)blockIdx.x < builders) {
+        if constexpr (SMALL) build_small(ids, map, T, k, E, N, g, TwinMap{}, s_mem);
+        else scan_scatter(ids, map, nullptr, builders, T, k, E, N, g, TwinMap{}, s_mem);
+        return;
+    }
+    mx4_quantize_piece<Src, VEC>((int64_t)(blockIdx.x - builders) * blockDim.x + threadIdx.x, src, T, cols, row_stride, codes, scales, nullptr);
+}
+
 }  // namespace moe

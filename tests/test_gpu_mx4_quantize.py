@@ -125,3 +125,28 @@ def test_weight_blocks_that_are_not_numbers():
     held.pack(W.to(DEV), values=values)
     assert torch.equal(held.codes.cpu(), codes) and torch.equal(held.scales.cpu(), scales)
     assert torch.equal(torch.isnan(values.cpu()), torch.isnan(val)) and int(torch.isnan(val).sum()) == 32 * 3
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("T,k,E,cols,tile_m", [
+    (1, 1, 1, 1, 16), (1, 6, 64, 2048, 16), (7, 3, 5, 130, 32), (128, 6, 64, 264, 16), (500, 2, 8, 136, 128), (1025, 1, 9, 40, 32), (1111, 8, 64, 96, 128),
+    (4096, 4, 8, 64, 128), (4097, 4, 256, 33, 128), (16385, 1, 1000, 16, 16)])
+def test_map_and_rows_by_one_launch_are_those_of_two(T, k, E, cols, tile_m, dtype):
+    g = torch.Generator().manual_seed(T + E)
+    ids = torch.rand(T, E, generator=g).topk(k, 1).indices.int().to(DEV)
+    if T > 4:
+        ids[T // 2] = -1                 # (an id that is no expert: counted as bad by both)
+    wide = torch.randn(T, cols + 8, generator=g).to(dtype).to(DEV)
+    tiling = mb.Tiling(tile_m, 256)
+    for x in (wide[:, :cols], wide[:, :cols].contiguous(), wide[:, 1:cols + 1]):
+        got, want = [], []
+        for out in (got, want):
+            task_map, rows = mb.alloc_task_map(T, k, E, tile_m, 256, 512, DEV), mb.Mx4Rows(T, cols, DEV)
+            for t in (task_map, rows.codes, rows.scales):
+                t.fill_(77)
+            out += [task_map, rows.codes, rows.scales]
+        mb.moe_mx4_prepare(ids, T, k, E, 512, tiling, got[0], x, *got[1:])
+        mb.moe_build_task_map_ex(ids, T, k, E, 512, tiling, want[0])
+        mb.moe_mx4_quantize(x, *want[1:])
+        for a, b in zip(got, want):
+            assert torch.equal(a, b)

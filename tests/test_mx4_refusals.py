@@ -47,6 +47,21 @@ def test_quantize(kw, rc):
     assert _quantize(**kw) == rc
 
 
+def _prepare(ids=P, T=4, k=2, E=8, N=256, tile=(16, 256, 0, 0, 0, 0), task_map=P, X=P, dtype=mb.MOE_DTYPE_BF16, K=100, stride=100, codes=P, scales=P):
+    g = ctypes.byref(mb.moe_tiling(*tile)) if tile else None
+    return mb.lib().moe_mx4_prepare(ids, T, k, E, N, g, task_map, X, dtype, K, stride, codes, scales, None)
+
+
+@pytest.mark.parametrize("kw,rc", [(dict(tile=None), INVALID), (dict(T=-1), INVALID), (dict(k=0), INVALID), (dict(k=9), INVALID), (dict(E=0), INVALID), (dict(N=0), INVALID),
+                                   (dict(E=1025), UNSUPPORTED), (dict(T=1 << 23, k=8), UNSUPPORTED), (dict(tile=(16, 100, 0, 0, 0, 0)), UNSUPPORTED),
+                                   (dict(tile=(16, 256, 5, 0, 0, 0)), INVALID), (dict(tile=(16, 256, 0, 0, 0, 16)), INVALID), (dict(ids=None), INVALID),
+                                   (dict(ids=P + 2), INVALID), (dict(task_map=None), INVALID), (dict(task_map=P + 8), INVALID), (dict(X=None), INVALID),
+                                   (dict(X=P + 1), INVALID), (dict(dtype=mb.MOE_DTYPE_FP8_E4M3), UNSUPPORTED), (dict(K=0), INVALID), (dict(stride=99), INVALID),
+                                   (dict(codes=P + 8), INVALID), (dict(scales=P + 2), INVALID), (dict(codes=None), INVALID), (dict(scales=None), INVALID)])
+def test_prepare(kw, rc):
+    assert _prepare(**kw) == rc
+
+
 def _pack(W=P, dtype=mb.MOE_DTYPE_BF16, layout=0, E=2, K=64, N=64, gated=0, codes=P, scales=P, values=None):
     return mb.lib().moe_mx4_pack_weights(W, dtype, layout, E, K, N, gated, codes, scales, values, None)
 
