@@ -109,10 +109,9 @@ int launch_mx4_rows(const Mx4GemmArgs& a, int64_t grid, hipStream_t s) {
     return launched();
 }
 
-template <int WM>
 int launch_mx4_lds(const Mx4GemmArgs& a, int64_t grid, hipStream_t s) {
-    if (!work_items_fit(grid, 256 * WM)) return MOE_ERR_UNSUPPORTED;
-    mx4_gemm_lds<WM><<<dim3((unsigned)grid), 256 * WM, 0, s>>>(a);
+    if (!work_items_fit(grid, 256)) return MOE_ERR_UNSUPPORTED;
+    mx4_gemm_lds<<<dim3((unsigned)grid), 256, 0, s>>>(a);
     return launched();
 }
 
@@ -123,7 +122,7 @@ struct Mx4Tile {
 const Mx4Tile kMx4Tiles[] = {
     {16, 256, &launch_mx4_rows<1>},
     {32, 256, &launch_mx4_rows<2>},
-    {128, 256, &launch_mx4_lds<1>},
+    {128, 256, &launch_mx4_lds},
 };
 const Mx4Tile* find_mx4_tile(int tile_m, int tile_n) {
     for (const Mx4Tile& t : kMx4Tiles)

@@ -149,35 +149,35 @@ __device__ __forceinline__ void mx4_mfma32(const u32x4_t w, const u32x4_t x, f32
                  : "+v"(acc) : "v"(w), "v"(x), "v"(wscale), "v"(xscale), "n"(J / 2), "n"(JX / 2));
 }
 
-// Tiles of 128 WM rows x 256 packed columns, 4 WM wavefronts of 128 rows x 64 columns.  Token rows go through LDS, which every
-// wavefront column reads: stages of 256 k (128 bytes a row), two of them, loaded into registers a stage ahead and written behind the
+// Tiles of 128 rows x 256 packed columns, four wavefronts of 128 rows x 64 columns.  Token rows go through LDS, which every
+// wavefront reads: stages of 256 k (128 bytes a row), two of them, loaded into registers a stage ahead and written behind the
 // barrier that frees the other one.  Weights go straight to registers, two k-steps of 128 ahead: packed, a wavefront's step is 4 KB in
-// one piece.  Scales likewise.  Block b of 32 rows belongs to wavefront row b % WM; each wavefront runs the copy of the loop for the
-// blocks it has (MB of them, none included).
-template <int WM>
+// one piece.  Scales likewise.  A tile runs the copy of the loop for the blocks of 32 rows that it has (MB of them).
 struct Mx4TileLds {
-    static constexpr int ROWS = 128 * WM, THREADS = 256 * WM, STAGE = ROWS * 128, SCALES = ROWS * 8, LDS = 2 * (STAGE + SCALES);
+    static constexpr int ROWS = 128, STAGE = ROWS * 128, SCALES = ROWS * 8, LDS = 2 * (STAGE + SCALES);
     const Mx4GemmArgs& a;
     const TileCoord& tc;
     const int32_t* rows;
     char* smem;
-    int wave, lane, wm, wn, h, r32;
+    int wave, lane, h, r32;
 
     template <int MB>
     __device__ __forceinline__ void run() const {
         const int tid = threadIdx.x;
+        int first = 0;                      // the tile's first row; opaque, or addresses that are cheap to make again are kept, and registers spill
+        asm volatile("" : "+s"(first));
         const int64_t kp = (int64_t)a.tiles_k * kMxTileK;
-        // token rows: 16-byte chunk tid % 8 of rows tid / 8 + 32 WM i
+        // token rows: 16-byte chunk tid % 8 of rows tid / 8 + 32 i
         const int pos = tid & 7;
         uint32_t xp[4], sp;                 // their offsets, and that of the scales of row tid: eight bytes of a stage
-        // (LDS has 64 banks: rows of 128 bytes alternate between their halves, and 16 rows' chunks spread over both; 32 WM rows further on
+        // (LDS has 64 banks: rows of 128 bytes alternate between their halves, and 16 rows' chunks spread over both; 32 rows further on
         // the swizzle is the same)
         const int x_lds = (tid >> 3) * 128 + ((pos ^ ((tid >> 4) & 7)) << 4);
         const bool has_scales = tid < ROWS;
         int id[5];                          // asked for in front of the first weights, which do not wait for them
 #pragma unroll
         for (int i = 0; i < 5; ++i) {
-            const int row = i < 4 ? (tid >> 3) + 32 * WM * i : tid;
+            const int row = i < 4 ? (tid >> 3) + 32 * i : tid;
             id[i] = rows[row < tc.rows ? row : 0];
         }
         auto locate_rows = [&]() __attribute__((always_inline)) {
@@ -185,7 +185,7 @@ struct Mx4TileLds {
             for (int i = 0; i < 4; ++i) xp[i] = (uint32_t)id[i] / (uint32_t)a.k * (uint32_t)(kp / 2) + pos * 16;
             sp = (uint32_t)id[4] / (uint32_t)a.k * (uint32_t)(kp / kMxBlock);
         };
-        const int nt_all = tc.n_tile * 4 + wn, nt = nt_all < a.tiles_n ? nt_all : a.tiles_n - 1;
+        const int nt_all = tc.n_tile * 4 + wave, nt = nt_all < a.tiles_n ? nt_all : a.tiles_n - 1;
         const int64_t tile = ((int64_t)tc.e * a.tiles_n + nt) * a.tiles_k;
         // lane (h, r32): column r32 % 16 of block r32 / 16 of a 32-column pair, chunk h of the two that a 64 k instruction takes
         const char* wp = static_cast<const char*>(a.W) + tile * kMxTileBytes;
@@ -194,7 +194,7 @@ struct Mx4TileLds {
         const int wshift = 8 * (r32 >> 4), xshift = 8 * h;
         const int steps = a.tiles_k, stages = (steps + 1) / 2;
 
-        f32x16_t acc[MB > 0 ? MB : 1][2];
+        f32x16_t acc[MB][2];
 #pragma unroll
         for (int mb = 0; mb < MB; ++mb)
 #pragma unroll
@@ -202,12 +202,12 @@ struct Mx4TileLds {
 #pragma unroll
                 for (int i = 0; i < 16; ++i) acc[mb][b][i] = 0.f;
 
-        u32x4_t xr[2], x[2][MB > 0 ? MB : 1], w[4][2];      // x: of this 64 k instruction and the next; w[instruction of a stage][b]
-        uint32_t xsr[2], xs[2][MB > 0 ? MB : 1], ws[4];
+        u32x4_t xr[2], x[2][MB], w[4][2];      // x: of this 64 k instruction and the next; w[instruction of a stage][b]
+        uint32_t xsr[2], xs[2][MB], ws[4];
         // where this lane's chunk of instruction i of a stage is, and its row's scales (of block 0; blocks are a constant apart)
-        uint32_t x_rd[4], s_rd = 2 * STAGE + (32 * wm + r32) * 8;
+        uint32_t x_rd[4], s_rd = 2 * STAGE + (first + r32) * 8;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) x_rd[i] = (32 * wm + r32) * 128 + (((2 * i + h) ^ ((r32 >> 1) & 7)) << 4);
+        for (int i = 0; i < 4; ++i) x_rd[i] = (first + r32) * 128 + (((2 * i + h) ^ ((r32 >> 1) & 7)) << 4);
         // a stage in two halves: rows of i = 0, 1 with the scales, then of i = 2, 3.  (The second half of an odd last step does not exist:
         // its tokens are zeros, against the weights of the step before.)
         auto load_x = [&](int st, int half) __attribute__((always_inline)) {
@@ -226,13 +226,12 @@ struct Mx4TileLds {
             const bool zero = 2 * st + 1 >= steps && pos >= 4;
 #pragma unroll
             for (int i = 0; i < 2; ++i)
-                *reinterpret_cast<u32x4_t*>(smem + (st & 1) * STAGE + x_lds + (2 * half + i) * (32 * WM * 128)) = zero ? u32x4_t{0u, 0u, 0u, 0u} : xr[i];
+                *reinterpret_cast<u32x4_t*>(smem + (st & 1) * STAGE + x_lds + (2 * half + i) * (32 * 128)) = zero ? u32x4_t{0u, 0u, 0u, 0u} : xr[i];
             if (half == 0 && has_scales)
                 *reinterpret_cast<u32x2_t*>(smem + 2 * STAGE + (st & 1) * SCALES + tid * 8) = u32x2_t{xsr[0], 2 * st + 1 < steps ? xsr[1] : 0u};
         };
         auto load_w = [&](int st, auto i_tag) __attribute__((always_inline)) {
             constexpr int I = decltype(i_tag)::value;
-            if (MB == 0) return;
             const int kb = 2 * st + I / 2 < steps ? 2 * st + I / 2 : steps - 1;
 #pragma unroll
             for (int b = 0; b < 2; ++b) w[I][b] = *reinterpret_cast<const u32x4_t*>(wp + (int64_t)kb * kMxTileBytes + (w_off + b * 2048 + (I & 1) * 512));
@@ -241,10 +240,10 @@ struct Mx4TileLds {
         auto read_x = [&](auto i_tag) __attribute__((always_inline)) {
             constexpr int I = decltype(i_tag)::value;
 #pragma unroll
-            for (int mb = 0; mb < MB; ++mb) x[I & 1][mb] = *reinterpret_cast<const u32x4_t*>(smem + x_rd[I] + mb * (WM * 32 * 128));
+            for (int mb = 0; mb < MB; ++mb) x[I & 1][mb] = *reinterpret_cast<const u32x4_t*>(smem + x_rd[I] + mb * (32 * 128));
             if constexpr ((I & 1) == 0) {
 #pragma unroll
-                for (int mb = 0; mb < MB; ++mb) xs[I / 2][mb] = *reinterpret_cast<const uint32_t*>(smem + s_rd + mb * (WM * 32 * 8) + I * 2);
+                for (int mb = 0; mb < MB; ++mb) xs[I / 2][mb] = *reinterpret_cast<const uint32_t*>(smem + s_rd + mb * (32 * 8) + I * 2);
             }
         };
         auto multiply = [&](auto i_tag) __attribute__((always_inline)) {
@@ -325,13 +324,13 @@ struct Mx4TileLds {
         }
         asm volatile("s_nop 7\n\ts_nop 7\n\ts_nop 7");   // the last sums, before an ordinary instruction reads them
         barrier();                              // the stages become the way out
-        if (MB == 0 || nt_all >= a.tiles_n) return;
+        if (nt_all >= a.tiles_n) return;
         uint16_t* y = static_cast<uint16_t*>(a.Y);
         const int n0 = a.gated ? nt * 32 : nt * 64;
-        int rid[MB > 0 ? MB : 1];               // row of Y that this lane's row of block mb is, or -1
+        int rid[MB];               // row of Y that this lane's row of block mb is, or -1
 #pragma unroll
         for (int mb = 0; mb < MB; ++mb) {
-            const int row = 32 * (WM * mb + wm) + r32;
+            const int row = 32 * (mb + first) + r32;
             rid[mb] = rows[row < tc.rows ? row : 0];
             if (row >= tc.rows) rid[mb] = -1;
         }
@@ -385,22 +384,18 @@ struct Mx4TileLds {
     }
 };
 
-template <int WM>
-__global__ __launch_bounds__(256 * WM, 2) void mx4_gemm_lds(Mx4GemmArgs a) {
-    using Tile = Mx4TileLds<WM>;
-    __shared__ __attribute__((aligned(16))) char smem[Tile::LDS];
+__global__ __launch_bounds__(256, 2) void mx4_gemm_lds(Mx4GemmArgs a) {
+    __shared__ __attribute__((aligned(16))) char smem[Mx4TileLds::LDS];
     MapLayout L;
     TileCoord tc;
-    if (!locate_tile<Tile::ROWS, 256, 0, 0>(a, a.map, L, tc)) return;
+    if (!locate_tile<Mx4TileLds::ROWS, 256, 0, 0>(a, a.map, L, tc)) return;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const Tile t = {a, tc, a.map + L.off_rows + tc.row_base, smem, wave, lane, wave >> 2, wave & 3, lane >> 5, lane & 31};
-    const int blocks = (tc.rows + 31) / 32, mine = (blocks - t.wm + WM - 1) / WM;   // blocks wm, wm + WM, ...
-    switch (mine) {
-        case 0: t.template run<0>(); break;
-        case 1: t.template run<1>(); break;
-        case 2: t.template run<2>(); break;
-        case 3: t.template run<3>(); break;
-        default: t.template run<4>(); break;
+    const Mx4TileLds t = {a, tc, a.map + L.off_rows + tc.row_base, smem, wave, lane, lane >> 5, lane & 31};
+    switch ((tc.rows + 31) / 32) {
+        case 1: t.run<1>(); break;
+        case 2: t.run<2>(); break;
+        case 3: t.run<3>(); break;
+        default: t.run<4>(); break;
     }
 }
 
