@@ -549,7 +549,8 @@ int moe_mx4_tile_supported(int tile_m, int tile_n);
 int moe_mx4_default_tiling(int T, int k, int E, int K, int N, int gated, moe_tiling* out);
 
 /*
- * A whole layer for at most 16 tokens, in two launches and without a task map:
+ * A whole layer for at most 16 tokens, in two launches (4-bit weights and more than about 60000 values of X: three) and without a
+ * task map:
  *     topk_ids, topk_weights = moe_route(logits)
  *     h[t, j] = silu(X[t] . W_gate[e]) * (X[t] . W_up[e]),  e = topk_ids[t, j]
  *     out[t]  = sum_j topk_weights[t, j] * (h[t, j] . W_down[e])
@@ -563,7 +564,9 @@ int moe_mx4_default_tiling(int T, int k, int E, int K, int N, int gated, moe_til
  *   out      DEVICE bf16 [T][hidden]
  *   workspace  DEVICE, 16-byte aligned, at least moe_few_tokens_workspace_bytes(desc) bytes, contents undefined before and after;
  *            calls that share one must not overlap.
- * Sums are fp32; h is rounded to bf16 once, out once.  A token is not touched by what is in the weights of experts that it did not
+ * Sums are fp32; out is rounded to bf16 once.  BF16: h is rounded to bf16 once.  MX4: a block of 32 values of X or of h is two 8-bit
+ * halves under one exponent: exact for X's values down to 2^-13 of the block's largest; a smaller one is off by at most 2^-21 of the largest, one of h by
+ * that or 2^-8 of itself, whichever is more.  A block with an infinity or NaN makes that token's products NaN.  A token is not touched by what is in the weights of experts that it did not
  * choose, nor by other tokens.  Deterministic.
  * T <= 16, k <= 16, hidden a multiple of 8 (BF16: inter too), both at most 2^20, else MOE_ERR_UNSUPPORTED; limits of moe_route.
  */

@@ -8,7 +8,7 @@
 // streams of weights through registers: a wavefront loads its share straight in the layout of the matrix operand (bf16:
 // 16 k x 128 columns of [K][N] weights, turned in registers; 4 bits: the packed tiles of mx4.hpp), multiplies it with all
 // tokens at once (they are the 16 columns of the other operand, token t is column t for every expert), and the
-// wavefronts of a workgroup, which share a column tile and split its k, add their sums in LDS.  A token that an expert
+// wavefronts of a workgroup, which share a column tile (or two neighbouring ones) and split its k, add their sums in LDS.  A token that an expert
 // was not chosen for is a column whose result is dropped (never a product with zero: such an expert's infinities must not
 // reach it).
 //
