@@ -75,7 +75,8 @@ __device__ __forceinline__ u32x4_t mx4_values8(uint32_t codes, float scale) {
 __device__ __forceinline__ float mx4_load(const uint16_t* p) { return __uint_as_float((uint32_t)*p << 16); }
 __device__ __forceinline__ float mx4_load(const float* p) { return *p; }
 
-// Token rows.  A lane takes eight elements of a row, four lanes a block.  VEC: rows begin on 16 bytes and are a multiple
+// Token rows.  A lane takes eight elements of a row, four lanes a block: a stream of bytes, 4096 rows of 7168 bf16 with values in 24.8 us, 5.4 TB/s read
+// and written (a large copy: 5.0).  128 rows of 2048 are a launch's latency, 2.6 us back to back.  VEC: rows begin on 16 bytes and are a multiple
 // of eight long, and every lane moves its elements with one or two 16-byte loads.
 template <class Src, bool VEC>
 __device__ __forceinline__ void mx4_quantize_piece(int64_t c, const Src* __restrict__ src, int64_t rows, int cols, int64_t row_stride,
@@ -208,7 +209,8 @@ __global__ __launch_bounds__(256) void mx4_pack_weights(const Src* __restrict__ 
 
 // The same for bf16 weights [E][K][N] whose rows can be read two columns at a time: one workgroup per two tiles side by side, a thread per 32 k
 // of two neighbouring columns, so that a wavefront reads (and with values writes) 256 bytes of a row, or, gated, 128 bytes of gate columns
-// and 128 of the up columns of the same outputs.
+// and 128 of the up columns of the same outputs.  64 experts of 2048 x 2816, gated, with values: 282 to 306 us, 5.5 to 5.9 TB/s read and written (a
+// thread for a column each, 64 bytes of a row a wavefront: 626).
 __global__ __launch_bounds__(256) void mx4_pack_pairs(const uint16_t* __restrict__ W, int K, int N, int gated, int tiles_n, int tiles_k,
                                                       char* __restrict__ codes, uint8_t* __restrict__ scales, uint16_t* __restrict__ values) {
     const int pairs_n = (tiles_n + 1) / 2;

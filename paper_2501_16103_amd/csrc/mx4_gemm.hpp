@@ -39,7 +39,8 @@ __device__ __forceinline__ void mx4_store4(uint16_t* yrow, int n, int out_n, uin
 
 // Tiles of 16 MB rows x 256 packed columns for few rows per expert: a stream of weights.  Four wavefronts of 64 columns and the whole
 // of K each, which have nothing to wait for in each other: operands go straight from memory to registers, the next steps' loads
-// (of 128 k: 4 KB of codes, 256 bytes of scales, and 64 bytes of each token row) ahead of the product.
+// (of 128 k: 4 KB of codes, 256 bytes of scales, and 64 bytes of each token row) ahead of the product.  Bound by memory: 64 experts, 2048 -> 2816,
+// gated, 128 tokens of 6 experts (12 rows an expert) 40 to 41 us with cold weights, 5 TB/s of them (one step ahead: 43.8).
 template <int MB>
 __global__ __launch_bounds__(256, 4) void mx4_gemm_rows(Mx4GemmArgs a) {
     MapLayout L;
@@ -152,7 +153,10 @@ __device__ __forceinline__ void mx4_mfma32(const u32x4_t w, const u32x4_t x, f32
 // Tiles of 128 rows x 256 packed columns, four wavefronts of 128 rows x 64 columns.  Token rows go through LDS, which every
 // wavefront reads: stages of 256 k (128 bytes a row), two of them, loaded into registers a stage ahead and written behind the
 // barrier that frees the other one.  Weights go straight to registers, two k-steps of 128 ahead: packed, a wavefront's step is 4 KB in
-// one piece.  Scales likewise.  A tile runs the copy of the loop for the blocks of 32 rows that it has (MB of them).
+// one piece.  Scales likewise.  4096 tokens, 2 of 8 experts, 4096 -> 28672, gated: 600 us, 3.2 PFLOP/s, the matrix pipes busy 39 % of the time at 1.96 GHz (nothing
+// but those instructions on such data: 6.2 PFLOP/s, which the power limit sets).  Without the fetches of weights in the loop it would be 467, without
+// those of tokens 481, without either 388, without the way out 538: the rate at which a CU is given operands (16 KB of weights and 4 of
+// tokens a wavefront and stage) bounds it more than the instructions do.  A tile runs the copy of the loop for the blocks of 32 rows that it has (MB of them).
 struct Mx4TileLds {
     static constexpr int ROWS = 128, STAGE = ROWS * 128, SCALES = ROWS * 8, LDS = 2 * (STAGE + SCALES);
     const Mx4GemmArgs& a;
