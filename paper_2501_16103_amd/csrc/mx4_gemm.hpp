@@ -40,9 +40,10 @@ __device__ __forceinline__ void mx4_store4(uint16_t* yrow, int n, int out_n, uin
 // Tiles of 16 MB rows x 256 packed columns for few rows per expert: a stream of weights.  Four wavefronts of 64 columns and the whole
 // of K each, which have nothing to wait for in each other: operands go straight from memory to registers, the next steps' loads
 // (of 128 k: 4 KB of codes, 256 bytes of scales, and 64 bytes of each token row) ahead of the product.  Bound by memory: 64 experts, 2048 -> 2816,
-// gated, 128 tokens of 6 experts (12 rows an expert) 40 to 41 us with cold weights, 5 TB/s of them (one step ahead: 43.8).
+// gated, 128 tokens of 6 experts (12 rows an expert) 41 us with cold weights, 5 TB/s of them (one step ahead: 43.8).  Tiles of 32 rows have a step
+// in registers more than four wavefronts a SIMD leave room for (spilling: 43.2; 100 tokens, 8 of 64 experts, 3584 -> 2560 49.7 against 47.1).
 template <int MB>
-__global__ __launch_bounds__(256, 4) void mx4_gemm_rows(Mx4GemmArgs a) {
+__global__ __launch_bounds__(256, MB == 1 ? 4 : 3) void mx4_gemm_rows(Mx4GemmArgs a) {
     MapLayout L;
     TileCoord tc;
     if (!locate_tile<16 * MB, 256, 0, 0>(a, a.map, L, tc)) return;
