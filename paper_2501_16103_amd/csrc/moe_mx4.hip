@@ -289,12 +289,18 @@ int moe_mx4_tile_supported(int tile_m, int tile_n) { return find_mx4_tile(tile_m
 
 int moe_mx4_default_tiling(int T, int k, int E, int K, int N, int gated, moe_tiling* out) {
     if (!out || T < 0 || k < 1 || k > E || check_mx4_weights(E, K, N, gated) == MOE_ERR_INVALID_ARG) return MOE_ERR_INVALID_ARG;
-    // Rows per expert on average.  us, 16 / 32 / 128 rows a tile, even and skewed routing: 64 experts, 2048 -> 2816, gated, 3 rows 36.9 / 36.7 /
-    // 44.7 and 20.7 / 22.4 / 21.8, 6 rows 38.0 / 38.4 / 45.0 and 22.3 / 25.5 / 24.8, 12 rows 42.3 / 40.6 / 45.8 and 34.1 / 33.9 / 28.2, 19 rows 45.7 / 42.2 /
-    // 46.0 and 39.0 / 37.0 / 30.3, 28 rows 53.9 / 52.3 / 47.0 and 47.4 / 42.3 / 41.1; 8 experts, 4096 -> 28672, 8 rows 95.4 / 95.4 / 90.4 and 82.0 / 79.1 /
-    // 80.9, 16 rows 107.7 / 105.1 / 91.8 and 93.5 / 90.9 / 83.8; 256 experts, 2048 -> 1024, 8 rows 57.3 / 53.9 / 55.1 and 28.7 / 34.9 / 28.0.
-    const int64_t R = (int64_t)T * k;
-    const moe_tiling g = {R > 16 * (int64_t)E ? 128 : R > 8 * (int64_t)E ? 32 : 16, 256, MOE_ORDER_ASCENDING, 0, 0, 0};
+    // By rows per expert on average; between 8 and 16 also by whether an expert's one tile of each column stripe finds a place at once (three of
+    // the 32-row ones a CU).  us, 16 / 32 / 128 rows a tile, even and skewed routing:
+    //   64 experts, 2048 -> 2816, gated (704 stripes): 3 rows 35.8 / 36.7 / 44.3 and 20.8 / 21.5 / 21.0, 6 rows 37.6 / 38.7 / 44.1 and 21.7 / 25.6 / 24.4,
+    //   12 rows 41.9 / 40.8 / 44.5 and 33.7 / 35.0 / 28.5, 19 rows 45.8 / 42.3 / 45.0 and 39.0 / 36.2 / 31.1, 28 rows 53.5 / 51.9 / 46.4 and 48.0 / 46.9 / 40.0;
+    //   64 experts, 1408 -> 2048 (512): 12 rows 25.1 / 21.3 / 22.0 and 16.8 / 15.4 / 16.3, 28 rows 31.2 / 29.5 / 23.1 and 26.3 / 23.3 / 20.8;
+    //   8 experts, 4096 -> 28672 (896): 7 rows 95.0 / 98.4 / 89.4 and 64.6 / 72.0 / 74.0, 10 rows 97.0 / 100.7 / 89.2 and 81.4 / 83.9 / 78.3, 16 rows 108.0 /
+    //   104.6 / 89.8 and 94.0 / 94.1 / 82.4; 16 experts, 4096 -> 14336 (896): 4 rows 92.4 / 96.9 / 88.3 and 71.9 / 73.5 / 79.8, 12 rows 94.1 / 104.0 / 89.1 and
+    //   91.5 / 95.7 / 81.8; 64 experts, 2048 -> 4096 (1024): 12 rows 58.2 / 60.5 / 54.5 and 43.1 / 47.5 / 46.7; 256 experts, 2048 -> 1024 (1024): 16 rows 62.5 /
+    //   62.6 / 55.2 and 45.3 / 43.0 / 37.5; 64 experts, 2048 -> 3500 (896): 12 rows 48.6 / 53.7 / 50.1 and 36.8 / 38.5 / 43.8 (the one that loses).
+    const int64_t R = (int64_t)T * k, stripes = E * ((mx4_packed_columns(N, gated) + 255) / 256);
+    const int middle = stripes > 3 * kCus ? 128 : 32;
+    const moe_tiling g = {R > 16 * (int64_t)E ? 128 : R > 8 * (int64_t)E ? middle : 16, 256, MOE_ORDER_ASCENDING, 0, 0, 0};
     *out = g;
     return MOE_OK;
 }
