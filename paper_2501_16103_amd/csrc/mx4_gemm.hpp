@@ -23,6 +23,7 @@ __device__ __forceinline__ f32x4_t mx4_mfma16(const u32x4_t w, const u32x4_t x, 
     return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, b, acc, 4, 4, J, (int)wscale, JX, (int)xscale);
 }
 
+// (the hardware's exponential and reciprocal: a few units in the last place of 32 bits, in front of the rounding to bf16)
 __device__ __forceinline__ float silu_times(float gate, float up) { return gate * __builtin_amdgcn_rcpf(1.f + __expf(-gate)) * up; }
 
 // Four consecutive values of a row of Y from column n on; columns at and beyond out_n are padding.
