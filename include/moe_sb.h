@@ -469,7 +469,7 @@ int moe_grouped_gemm_batched(const void* X, const void* W, const void* task_map,
  *   topk_weights  DEVICE fp32 [T, k]:  softmax p_e = exp(l_e - max) / sum over all E;  sigmoid p_e = 1 / (1 + exp(-l_e));
  *                 with `renormalize` divided by their sum over the k chosen ones (0 where that is 0); times `scale`.
  * An expert whose logit is -inf is masked: weight 0, chosen only where fewer than k are left.  A row of nothing but -inf has
- * weights 0 (its ids are still experts, 0 .. k-1).  A NaN or +inf in a softmax row makes its weights NaN.
+ * weights 0 (its ids are still experts, 0 .. k-1; moe_combine multiplies their products by 0, so what they hold has to be finite).  A NaN or +inf in a softmax row makes its weights NaN.
  * 1 <= k <= E <= 1024, T*k <= 2^24, T = 0 does nothing; other types MOE_ERR_UNSUPPORTED.  Deterministic.
  */
 enum { MOE_SCORE_SOFTMAX = 0, MOE_SCORE_SIGMOID = 1 };
@@ -567,7 +567,8 @@ int moe_mx4_default_tiling(int T, int k, int E, int K, int N, int gated, moe_til
  * Sums are fp32; out is rounded to bf16 once.  BF16: h is rounded to bf16 once.  MX4: a block of 32 values of X or of h is two 8-bit
  * halves under one exponent: exact for X's values down to 2^-13 of the block's largest; a smaller one is off by at most 2^-21 of the largest, one of h by
  * that or 2^-8 of itself, whichever is more.  A block with an infinity or NaN makes that token's products NaN.  A token is not touched by what is in the weights of experts that it did not
- * choose, nor by other tokens.  Deterministic.
+ * choose, nor by other tokens.  A choice of weight 0 adds nothing, whatever X and that expert's weights hold: a row whose experts are all masked is
+ * zeros.  Deterministic.
  * T <= 16, k <= 16, hidden a multiple of 8 (BF16: inter too), both at most 2^20, else MOE_ERR_UNSUPPORTED; limits of moe_route.
  */
 typedef struct moe_few_tokens_desc {

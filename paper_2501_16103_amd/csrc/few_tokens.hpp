@@ -10,7 +10,8 @@
 // tokens at once (they are the 16 columns of the other operand, token t is column t for every expert), and the
 // wavefronts of a workgroup, which share a column tile (or two neighbouring ones) and split its k, add their sums in LDS.  A token that an expert
 // was not chosen for is a column whose result is dropped (never a product with zero: such an expert's infinities must not
-// reach it).
+// reach it).  A choice of weight 0 (a masked expert's, or one whose weight underflows) is no choice for the sum, by the same rule, and one whose
+// logit is -inf makes the first launch read nothing either: empty slots of a batch cost no weights.
 //
 // The second launch's sum runs over all experts and the whole of their k, in parts by several workgroups per column tile;
 // each leaves its fp32 sums in the workspace, and the last one to arrive adds them in the order of the parts, so the result
@@ -57,7 +58,7 @@ struct FewArgs {
 
 // Who was chosen, as a workgroup keeps it.  Slots are the chosen experts by rising index.
 struct FewRouting {
-    int ids[kFewRows];
+    int ids[kFewRows];             // -1: a choice that does not count
     float weights[kFewRows];
     uint32_t chosen[kMaxE / 32];   // a bit for each expert
 };
@@ -67,9 +68,10 @@ struct FewRouting {
 struct FewSlots {
     uint32_t bits;
     int upto, all;
-    // all threads, behind a barrier; r.chosen is zeroed, r.ids (n of them, valid) are there.  Ends behind a barrier.
+    // all threads, behind a barrier; r.chosen is zeroed, r.ids (n of them, experts or -1) are there.  Ends behind a barrier.
     __device__ __forceinline__ void build(FewRouting& r, int n) {
-        for (int i = threadIdx.x; i < n; i += kFewThreads) atomicOr(&r.chosen[r.ids[i] >> 5], 1u << (r.ids[i] & 31));
+        for (int i = threadIdx.x; i < n; i += kFewThreads)
+            if (r.ids[i] >= 0) atomicOr(&r.chosen[r.ids[i] >> 5], 1u << (r.ids[i] & 31));
         __syncthreads();
         const int lane = __lane_id();
         bits = lane < kMaxE / 32 ? r.chosen[lane] : 0;
@@ -319,17 +321,18 @@ __global__ __launch_bounds__(kFewThreads, 4) void few_tokens_up(FewArgs a) {
     if constexpr (STAGED) W::stage(a.X, T, a.hidden, tokens);
     for (int t = wave; t < T; t += kFewWaves) {
         int id[EPL];
+        uint32_t chosen[EPL];
         float w[EPL];
         if (blockIdx.x == 0) {
-            route_token<EPL, Src>(a.route, t, id, w);
+            route_token<EPL, Src>(a.route, t, id, chosen, w);
             if (lane < k) {      // (k <= 16: slot 0)
                 a.ids[t * k + lane] = id[0];
                 a.weights[t * k + lane] = w[0];
             }
         } else {
-            route_token<EPL, Src, false>(a.route, t, id, w);
+            route_token<EPL, Src, false>(a.route, t, id, chosen, w);
         }
-        if (lane < k) r.ids[t * k + lane] = id[0];
+        if (lane < k) r.ids[t * k + lane] = chosen[0] == kRouteMasked ? -1 : id[0];
     }
     if (blockIdx.x == 0)
         for (int c = threadIdx.x; c < a.tiles2; c += kFewThreads) a.arrived[c] = 0;
@@ -340,6 +343,7 @@ __global__ __launch_bounds__(kFewThreads, 4) void few_tokens_up(FewArgs a) {
     // A wavefront takes every KW-th k-step of one of a group's tiles.  Its loads are steps ahead,
     // across the tiles too: while the sums of one are added, the weights of the next are on their way.
     const int groups = (a.tiles1 + NC - 1) / NC, total = slots.all * groups, sub = wave % NC, first = wave / NC;
+    if (total == 0) return;        // (all masked: the second launch finds nothing to add either)
     // (as few workgroups as the longest share allows: all of them then end together)
     const int rounds = (total + gridDim.x - 1) / (int)gridDim.x, sharing = (total + rounds - 1) / rounds;
     if ((int)blockIdx.x >= sharing) return;
@@ -468,8 +472,9 @@ __global__ __launch_bounds__(kFewThreads, 4) void few_tokens_down(FewArgs a) {
     const int T = a.route.T, k = a.route.k;
     if (tid < kMaxE / 32) r.chosen[tid] = 0;
     if (tid < T * k) {
-        r.ids[tid] = a.ids[tid];
-        r.weights[tid] = a.weights[tid];
+        const float w = a.weights[tid];
+        r.ids[tid] = w == 0.f ? -1 : a.ids[tid];
+        r.weights[tid] = w;
     }
     __syncthreads();
     FewSlots slots;

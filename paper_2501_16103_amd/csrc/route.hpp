@@ -5,8 +5,8 @@
 // the same however they are computed.  Weights are fp32:
 //   softmax  p_e = exp(l_e - max l) / sum over all experts;   sigmoid  p_e = 1 / (1 + exp(-l_e));
 // with `renormalize` divided by the sum over the k chosen ones; times `scale`.  An expert whose logit is -inf has
-// weight 0; a row of nothing else has weights 0 (its ids are 0 .. k-1: still experts, so the row can go on through the
-// layer and comes out as zeros).
+// weight 0; a row of nothing else has weights 0 (its ids are 0 .. k-1: still experts, so that it can go on through products and a
+// weighted sum, and comes out as zeros where its products are numbers; the layer for few tokens leaves choices of weight 0 out).
 #pragma once
 #include <hip/hip_runtime.h>
 #include <stdint.h>
@@ -29,6 +29,7 @@ __device__ __forceinline__ uint32_t route_key(float x) {
     if ((b & 0x7fffffffu) > 0x7f800000u) return 0xffffffffu;
     return b & 0x80000000u ? ~b : b | 0x80000000u;
 }
+constexpr uint32_t kRouteMasked = 0x007fffffu;                 // the key of -inf
 __device__ __forceinline__ float route_logit(uint32_t key) {   // the logit a key stands for
     if (key == 0xffffffffu) return __uint_as_float(0x7fc00000u);
     return __uint_as_float(key & 0x80000000u ? key & 0x7fffffffu : ~key);
@@ -58,11 +59,11 @@ __device__ __forceinline__ float wave_sum(float v) {
 }
 
 // One token by one wavefront.  EPL: logits per lane, experts EPL * lane + 0 .. EPL - 1.  The i-th choice comes back in slot i / 64 of
-// lane i % 64: its expert and its weight (lanes past the k choices hold nothing of use).  WEIGHTS false: the experts alone.
+// lane i % 64: its expert, its logit's key and its weight (lanes past the k choices hold nothing of use).  WEIGHTS false: no weights.
 // A lane keeps its logits in falling order (equal ones by rising expert), so that a choice only looks at one of them: the largest first
 // one of all lanes, of several the lowest lane's.
 template <int EPL, class Src, bool WEIGHTS = true>
-__device__ __forceinline__ void route_token(const RouteArgs& a, int64_t t, int (&ids)[EPL], float (&weights)[EPL]) {
+__device__ __forceinline__ void route_token(const RouteArgs& a, int64_t t, int (&ids)[EPL], uint32_t (&chosen)[EPL], float (&weights)[EPL]) {
     const int lane = __lane_id();
     const Src* row = static_cast<const Src*>(a.logits) + t * a.row_stride;
     uint32_t key[EPL];
@@ -103,7 +104,6 @@ __device__ __forceinline__ void route_token(const RouteArgs& a, int64_t t, int (
             expert[i - 1] = e_hi; expert[i] = e_lo;
         }
     }
-    uint32_t chosen[EPL];
 #pragma unroll
     for (int s = 0; s < EPL; ++s) {
         ids[s] = 0;
@@ -154,8 +154,9 @@ __global__ __launch_bounds__(256) void route_kernel(RouteArgs a, int32_t* __rest
     const int64_t t = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
     if (t >= a.T) return;
     int id[EPL];
+    uint32_t chosen[EPL];
     float w[EPL];
-    route_token<EPL, Src>(a, t, id, w);
+    route_token<EPL, Src>(a, t, id, chosen, w);
 #pragma unroll
     for (int s = 0; s < EPL; ++s) {
         const int i = 64 * s + __lane_id();
