@@ -467,7 +467,8 @@ int moe_grouped_gemm_batched(const void* X, const void* W, const void* task_map,
  *   topk_ids      DEVICE int32 [T, k]: the experts of the k largest logits in falling order, equal logits by rising index
  *                 (NaN counts as larger than every number, +0 and -0 as equal)
  *   topk_weights  DEVICE fp32 [T, k]:  softmax p_e = exp(l_e - max) / sum over all E;  sigmoid p_e = 1 / (1 + exp(-l_e));
- *                 with `renormalize` divided by their sum over the k chosen ones (0 where that is 0); times `scale`.
+ *                 with `renormalize` divided by their sum over the k chosen ones, however small it is (a sigmoid of a logit below -690
+ *                 counts as 0, and where all are, so do the weights); times `scale`.
  * An expert whose logit is -inf is masked: weight 0, chosen only where fewer than k are left.  A row of nothing but -inf has
  * weights 0 (its ids are still experts, 0 .. k-1; moe_combine multiplies their products by 0, so what they hold has to be finite).  A NaN or +inf in a softmax row makes its weights NaN.
  * 1 <= k <= E <= 1024, T*k <= 2^24, T = 0 does nothing; other types MOE_ERR_UNSUPPORTED.  Deterministic.

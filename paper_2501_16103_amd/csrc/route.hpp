@@ -4,7 +4,8 @@
 // larger than every number, +0 and -0 as equal).  Both scores rise with the logit, so the order needs none of them and is
 // the same however they are computed.  Weights are fp32:
 //   softmax  p_e = exp(l_e - max l) / sum over all experts;   sigmoid  p_e = 1 / (1 + exp(-l_e));
-// with `renormalize` divided by the sum over the k chosen ones; times `scale`.  An expert whose logit is -inf has
+// with `renormalize` divided by the sum over the k chosen ones; times `scale`.  Sigmoids of logits far below zero leave fp32 (at -88) though
+// their quotients do not: where all of a row's are below kSigmoidLow, p_e is exp(l_e - max l) times a factor that the quotient drops.  An expert whose logit is -inf has
 // weight 0; a row of nothing else has weights 0 (its ids are 0 .. k-1: still experts, so that it can go on through products and a
 // weighted sum, and comes out as zeros where its products are numbers; the layer for few tokens leaves choices of weight 0 out).
 #pragma once
@@ -29,6 +30,9 @@ __device__ __forceinline__ uint32_t route_key(float x) {
     if ((b & 0x7fffffffu) > 0x7f800000u) return 0xffffffffu;
     return b & 0x80000000u ? ~b : b | 0x80000000u;
 }
+// 1 + exp(l) is 1 in fp32 below kSigmoidLow, and above it a weight that is lost is less than 2^-79 of its row's largest.  Logits below kSigmoidNone are masks (of
+// a type's lowest value, say): their sigmoid is 0, in 64 bits too.
+constexpr float kSigmoidLow = -32.f, kSigmoidNone = -690.f;
 constexpr uint32_t kRouteMasked = 0x007fffffu;                 // the key of -inf
 __device__ __forceinline__ float route_logit(uint32_t key) {   // the logit a key stands for
     if (key == 0xffffffffu) return __uint_as_float(0x7fc00000u);
@@ -128,11 +132,12 @@ __device__ __forceinline__ void route_token(const RouteArgs& a, int64_t t, int (
         }
     }
     if (!WEIGHTS) return;
+    const bool low = a.sigmoid && a.renormalize && top < kSigmoidLow;
     float sum = 0.f;
 #pragma unroll
     for (int s = 0; s < EPL; ++s) {
         const float l = route_logit(chosen[s]);
-        float w = a.sigmoid ? 1.f / (1.f + expf(-l)) : empty ? 0.f : expf(l - top) / total;
+        float w = low ? (l < kSigmoidNone ? 0.f : expf(l - top)) : a.sigmoid ? 1.f / (1.f + expf(-l)) : empty ? 0.f : expf(l - top) / total;
         if (64 * s + lane >= a.k) w = 0.f;
         weights[s] = w;
         sum += w;
