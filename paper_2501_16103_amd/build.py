@@ -117,7 +117,9 @@ def check_mfma_operand_distance(asm_text: str) -> None:
         for k, (is_label, text, by_hand) in enumerate(code):
             if is_label or not by_hand or not text.startswith("v_mfma"):
                 continue
-            reads = set().union(*(_registers(op) for op in text.split(None, 1)[1].split(",")[1:4]))
+            # A, B, C and, of a scaled one, the two registers of scales (modifiers follow the last operand behind a blank)
+            operands = text.split(None, 1)[1].split(",")[1:6 if text.startswith("v_mfma_scale") else 4]
+            reads = set().union(*(_registers(op.split()[0]) for op in operands))
             todo, seen = [(p, 0) for p in before(k)], set()
             while todo:
                 p, waited = todo.pop()
