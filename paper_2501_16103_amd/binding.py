@@ -528,37 +528,71 @@ def _dtype(t: torch.Tensor) -> int:
     return _DTYPES.get(t.dtype, -1)
 
 
+def _holds(t: Optional[torch.Tensor], n: int, dtype: torch.dtype) -> bool:
+    """Whether a call that is given this tensor's address finds n elements of this type there (nothing to find in no tensor)."""
+    return t is None or (t.dtype == dtype and t.numel() >= n and t.is_contiguous())
+
+
+def _holds_bytes(t: torch.Tensor, n: int) -> bool:
+    return t.numel() * t.element_size() >= n and t.is_contiguous()
+
+
 def moe_route(logits: torch.Tensor, k: int, topk_ids: torch.Tensor, topk_weights: torch.Tensor, score: int = MOE_SCORE_SOFTMAX,
               renormalize: bool = True, scale: float = 1.0, check: bool = True) -> int:
     """logits [T, E], fp32 or bf16, rows of consecutive elements -> topk_ids int32 [T, k], topk_weights fp32 [T, k]."""
     T, E = logits.shape
     row, step = logits.stride()
-    d = moe_route_desc(T, k, E, _dtype(logits), row, score, renormalize, scale)
-    rc = MOE_ERR_INVALID_ARG if step != 1 and E > 1 else lib().moe_route(logits.data_ptr(), ctypes.byref(d), topk_ids.data_ptr(),
-                                                                         topk_weights.data_ptr(), _stream())
+    n = T * k
+    rc = MOE_ERR_INVALID_ARG
+    # (as _holds does it; a token's call is its host side)
+    if (topk_ids.numel() >= n and topk_weights.numel() >= n and topk_ids.dtype is torch.int32 and topk_weights.dtype is torch.float32 and
+            topk_ids.is_contiguous() and topk_weights.is_contiguous() and (step == 1 or E <= 1)):
+        d = moe_route_desc(T, k, E, _DTYPES.get(logits.dtype, -1), row, score, renormalize, scale)
+        rc = lib().moe_route(logits.data_ptr(), ctypes.byref(d), topk_ids.data_ptr(), topk_weights.data_ptr(), _stream())
     if check and rc != MOE_OK:
         raise MoeError(rc, "moe_route")
     return rc
 
 
+def _mx4_row_bytes(cols: int) -> tuple:
+    """Bytes of codes and of scales that a row takes."""
+    padded = (cols + 127) // 128 * 128
+    return padded // 2, padded // 32
+
+
+def _mx4_quantize(src: torch.Tensor, codes: torch.Tensor, scales: torch.Tensor, values: Optional[torch.Tensor]) -> int:
+    rows, cols = src.shape
+    row, step = src.stride()
+    return MOE_ERR_INVALID_ARG if step != 1 and cols > 1 else lib().moe_mx4_quantize(
+        src.data_ptr(), _dtype(src), rows, cols, row, codes.data_ptr(), scales.data_ptr(), _ptr(values), _stream())
+
+
 def moe_mx4_quantize(src: torch.Tensor, codes: torch.Tensor, scales: torch.Tensor, values: Optional[torch.Tensor] = None, check: bool = True) -> int:
     """src [rows, cols], fp32 or bf16, rows of consecutive elements; `values` bf16 [rows, cols], contiguous."""
     rows, cols = src.shape
-    row, step = src.stride()
-    rc = MOE_ERR_INVALID_ARG if step != 1 and cols > 1 else lib().moe_mx4_quantize(
-        src.data_ptr(), _dtype(src), rows, cols, row, codes.data_ptr(), scales.data_ptr(), _ptr(values), _stream())
+    code_bytes, scale_bytes = _mx4_row_bytes(cols)
+    fits = _holds_bytes(codes, rows * code_bytes) and _holds_bytes(scales, rows * scale_bytes) and _holds(values, rows * cols, torch.bfloat16)
+    rc = _mx4_quantize(src, codes, scales, values) if fits else MOE_ERR_INVALID_ARG
     if check and rc != MOE_OK:
         raise MoeError(rc, "moe_mx4_quantize")
     return rc
 
 
+def _mx4_prepare(topk_ids: torch.Tensor, T: int, k: int, E: int, N: int, tiling: Tiling, task_map: torch.Tensor, X: torch.Tensor, codes: torch.Tensor,
+                 scales: torch.Tensor) -> int:
+    K, (row, step) = X.shape[1], X.stride()
+    g = tiling.c_struct()
+    return MOE_ERR_INVALID_ARG if step != 1 and K > 1 else lib().moe_mx4_prepare(
+        topk_ids.data_ptr(), T, k, E, N, ctypes.byref(g), task_map.data_ptr(), X.data_ptr(), _dtype(X), K, row, codes.data_ptr(), scales.data_ptr(), _stream())
+
+
 def moe_mx4_prepare(topk_ids: torch.Tensor, T: int, k: int, E: int, N: int, tiling: Tiling, task_map: torch.Tensor, X: torch.Tensor, codes: torch.Tensor,
                     scales: torch.Tensor, check: bool = True) -> int:
     """moe_build_task_map_ex and moe_mx4_quantize of X [T, K] by one launch (N: the weights' packed columns)."""
-    K, (row, step) = X.shape[1], X.stride()
-    g = tiling.c_struct()
-    rc = MOE_ERR_INVALID_ARG if X.shape[0] != T or (step != 1 and K > 1) else lib().moe_mx4_prepare(
-        topk_ids.data_ptr(), T, k, E, N, ctypes.byref(g), task_map.data_ptr(), X.data_ptr(), _dtype(X), K, row, codes.data_ptr(), scales.data_ptr(), _stream())
+    code_bytes, scale_bytes = _mx4_row_bytes(X.shape[1])
+    fits = (X.shape[0] == T and _holds(topk_ids, T * k, torch.int32) and _holds_bytes(codes, T * code_bytes) and _holds_bytes(scales, T * scale_bytes) and
+            _holds(task_map, moe_task_map_bytes(T, k, E, tiling.tile_m, tiling.tile_n, N) // 4, torch.int32))
+    rc = _mx4_prepare(topk_ids, T, k, E, N, tiling, task_map, X, codes, scales) if fits else MOE_ERR_INVALID_ARG
     if check and rc != MOE_OK:
         raise MoeError(rc, "moe_mx4_prepare")
     return rc
@@ -575,8 +609,11 @@ def moe_mx4_row_scale_bytes(rows: int, cols: int) -> int:
 def moe_mx4_pack_weights(W: torch.Tensor, w_layout: int, E: int, K: int, N: int, gated: bool, codes, scales, values: Optional[torch.Tensor] = None,
                          check: bool = True) -> int:
     """W [E, K, N] or [E, N, K], contiguous; `codes`, `scales`: tensors or device addresses."""
+    need = moe_mx4_weight_code_bytes(E, K, N, gated), moe_mx4_weight_scale_bytes(E, K, N, gated)
+    fits = _holds(W, E * K * N, W.dtype) and _holds(values, E * K * N, torch.bfloat16) and all(
+        isinstance(p, int) or _holds_bytes(p, n) for p, n in zip((codes, scales), need))
     at = [p if isinstance(p, int) else _ptr(p) for p in (codes, scales)]
-    rc = lib().moe_mx4_pack_weights(_ptr(W), _dtype(W), w_layout, E, K, N, int(gated), *at, _ptr(values), _stream())
+    rc = lib().moe_mx4_pack_weights(_ptr(W), _dtype(W), w_layout, E, K, N, int(gated), *at, _ptr(values), _stream()) if fits else MOE_ERR_INVALID_ARG
     if check and rc != MOE_OK:
         raise MoeError(rc, "moe_mx4_pack_weights")
     return rc
@@ -628,7 +665,9 @@ class Mx4Rows:
             raise MoeError(MOE_ERR_INVALID_ARG, "Mx4Rows.quantize")
         if values is not None:
             _contiguous("Mx4Rows.quantize", values, shape, torch.bfloat16)
-        moe_mx4_quantize(src, self.codes, self.scales, values)
+        rc = _mx4_quantize(src, self.codes, self.scales, values)
+        if rc != MOE_OK:
+            raise MoeError(rc, "moe_mx4_quantize")
         return self
 
 
@@ -661,9 +700,17 @@ class Mx4Weights:
         return self
 
 
-def moe_mx4_grouped_gemm(X: Mx4Rows, W: Mx4Weights, T: int, k: int, task_map: torch.Tensor, Y: torch.Tensor, tiling: Tiling, check: bool = True) -> int:
+def _mx4_grouped_gemm(X: Mx4Rows, W: Mx4Weights, T: int, k: int, task_map: torch.Tensor, Y: torch.Tensor, tiling: Tiling) -> int:
     d = moe_mx4_gemm_desc(T, k, W.E, W.K, W.N, int(W.gated), tiling.tile_m, tiling.tile_n)
-    rc = lib().moe_mx4_grouped_gemm(_ptr(X.codes), _ptr(X.scales), _ptr(W.codes), _ptr(W.scales), _ptr(task_map), _ptr(Y), ctypes.byref(d), _stream())
+    return lib().moe_mx4_grouped_gemm(_ptr(X.codes), _ptr(X.scales), _ptr(W.codes), _ptr(W.scales), _ptr(task_map), _ptr(Y), ctypes.byref(d), _stream())
+
+
+def moe_mx4_grouped_gemm(X: Mx4Rows, W: Mx4Weights, T: int, k: int, task_map: torch.Tensor, Y: torch.Tensor, tiling: Tiling, check: bool = True) -> int:
+    """X's first T rows times their experts' weights -> Y bf16 [T, k, W.N, or W.N / 2 of gated weights]."""
+    map_bytes = moe_task_map_bytes(T, k, W.E, tiling.tile_m, tiling.tile_n, moe_mx4_packed_columns(W.N, W.gated))
+    fits = (X.rows >= T and X.cols == W.K and _holds(task_map, map_bytes // 4, torch.int32) and
+            _holds(Y, T * k * (W.N // 2 if W.gated else W.N), torch.bfloat16))
+    rc = _mx4_grouped_gemm(X, W, T, k, task_map, Y, tiling) if fits else MOE_ERR_INVALID_ARG
     if check and rc != MOE_OK:
         raise MoeError(rc, "moe_mx4_grouped_gemm")
     return rc
@@ -688,8 +735,12 @@ class MoeMx4ProductPlan:
         _contiguous("MoeMx4ProductPlan.forward", topk_ids, (self.T, self.k), torch.int32)
         if self.T == 0:
             return self.out
-        moe_mx4_prepare(topk_ids, self.T, self.k, self.E, self.columns, self.g, self.map, X, self.rows.codes, self.rows.scales)
-        moe_mx4_grouped_gemm(self.rows, W, self.T, self.k, self.map, self.out, self.g)
+        rc = _mx4_prepare(topk_ids, self.T, self.k, self.E, self.columns, self.g, self.map, X, self.rows.codes, self.rows.scales)
+        if rc != MOE_OK:
+            raise MoeError(rc, "moe_mx4_prepare")
+        rc = _mx4_grouped_gemm(self.rows, W, self.T, self.k, self.map, self.out, self.g)
+        if rc != MOE_OK:
+            raise MoeError(rc, "moe_mx4_grouped_gemm")
         return self.out
 
 
