@@ -99,6 +99,11 @@ __device__ __forceinline__ int few_row(const FewRouting& r, int t, int k, int e)
 // value of x / 2^s and lo that of 16 times what is left.  Exact for bf16 values down to 2^-13 of the block's largest, below that
 // off by at most 2^-21 of the largest.  (Turning the weights into bf16 instead is 64 quarter-rate conversions a step: 64 experts, 2048 /
 // 1408, 16 tokens, 75 us with them.)  A block with an infinity or NaN is NaN.
+// The sum is not fp32's throughout: the instruction aligns the products of 8 consecutive k to the largest of them and drops the bits below
+// 2^(e - 13), e its operands' exponents added; only the groups' sums and the accumulator are added with 24 bits.  (Found with +P, -P and a small
+// product: in their group it survives at 2^-13 of P and vanishes at 2^-14, in another one it survives at 2^-17, the smallest tried, and beside an accumulator
+// at 2^-23.)  That is 7 * 2^-13 of a group's largest product at most.  Apart from sums in 64 bits: normal tokens 1.8e-3 of the norm (with bf16 weights 2.3e-3, for h's rounding), pairs of channels 2^8 above
+// the others that cancel 6e-3, 2^11 above 6.5e-2 (bf16 weights 2.3e-3).
 // The instruction's 8-bit operand: lane 16 g + t holds k = 16 g + 0 .. 15 and 64 + 16 g + 0 .. 15 of token t, and the scale of
 // k = 32 g .. 32 g + 31.
 struct FewMx4 {
