@@ -325,19 +325,18 @@ __global__ __launch_bounds__(kFewThreads, 4) void few_tokens_up(FewArgs a) {
     if (threadIdx.x < kMaxE / 32) r.chosen[threadIdx.x] = 0;
     if constexpr (STAGED) W::stage(a.X, T, a.hidden, tokens);
     for (int t = wave; t < T; t += kFewWaves) {
-        int id[EPL];
-        uint32_t chosen[EPL];
+        int id[EPL], unmasked;
         float w[EPL];
         if (blockIdx.x == 0) {
-            route_token<EPL, Src>(a.route, t, id, chosen, w);
+            unmasked = route_token<EPL, Src>(a.route, t, id, w);
             if (lane < k) {      // (k <= 16: slot 0)
                 a.ids[t * k + lane] = id[0];
                 a.weights[t * k + lane] = w[0];
             }
         } else {
-            route_token<EPL, Src, false>(a.route, t, id, chosen, w);
+            unmasked = route_token<EPL, Src, false>(a.route, t, id, w);
         }
-        if (lane < k) r.ids[t * k + lane] = chosen[0] == kRouteMasked ? -1 : id[0];
+        if (lane < k) r.ids[t * k + lane] = lane < unmasked ? id[0] : -1;
     }
     if (blockIdx.x == 0)
         for (int c = threadIdx.x; c < a.tiles2; c += kFewThreads) a.arrived[c] = 0;

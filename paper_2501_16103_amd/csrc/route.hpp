@@ -63,11 +63,12 @@ __device__ __forceinline__ float wave_sum(float v) {
 }
 
 // One token by one wavefront.  EPL: logits per lane, experts EPL * lane + 0 .. EPL - 1.  The i-th choice comes back in slot i / 64 of
-// lane i % 64: its expert, its logit's key and its weight (lanes past the k choices hold nothing of use).  WEIGHTS false: no weights.
+// lane i % 64: its expert and its weight (lanes past the k choices hold nothing of use).  WEIGHTS false: the experts alone.  Returns how many of
+// the choices are of experts that are not masked; they come first.
 // A lane keeps its logits in falling order (equal ones by rising expert), so that a choice only looks at one of them: the largest first
 // one of all lanes, of several the lowest lane's.
 template <int EPL, class Src, bool WEIGHTS = true>
-__device__ __forceinline__ void route_token(const RouteArgs& a, int64_t t, int (&ids)[EPL], uint32_t (&chosen)[EPL], float (&weights)[EPL]) {
+__device__ __forceinline__ int route_token(const RouteArgs& a, int64_t t, int (&ids)[EPL], float (&weights)[EPL]) {
     const int lane = __lane_id();
     const Src* row = static_cast<const Src*>(a.logits) + t * a.row_stride;
     uint32_t key[EPL];
@@ -108,6 +109,8 @@ __device__ __forceinline__ void route_token(const RouteArgs& a, int64_t t, int (
             expert[i - 1] = e_hi; expert[i] = e_lo;
         }
     }
+    uint32_t chosen[EPL];
+    int unmasked = 0;
 #pragma unroll
     for (int s = 0; s < EPL; ++s) {
         ids[s] = 0;
@@ -116,6 +119,7 @@ __device__ __forceinline__ void route_token(const RouteArgs& a, int64_t t, int (
         for (int i = 0; i < end; ++i) {
             const int owner = __builtin_ctzll(__ballot(key[0] == now));
             const int e = __builtin_amdgcn_readlane(expert[0], owner);
+            unmasked += now > kRouteMasked;
             if (lane == i) {
                 ids[s] = e;
                 chosen[s] = now;
@@ -131,7 +135,7 @@ __device__ __forceinline__ void route_token(const RouteArgs& a, int64_t t, int (
             now = wave_max_u32(key[0]);
         }
     }
-    if (!WEIGHTS) return;
+    if (!WEIGHTS) return unmasked;
     const bool low = a.sigmoid && a.renormalize && top < kSigmoidLow;
     float sum = 0.f;
 #pragma unroll
@@ -149,6 +153,7 @@ __device__ __forceinline__ void route_token(const RouteArgs& a, int64_t t, int (
     }
 #pragma unroll
     for (int s = 0; s < EPL; ++s) weights[s] *= a.scale;
+    return unmasked;
 }
 
 // A wavefront per token, four tokens a workgroup.  What bounds it is latency: the load, k + 1 dependent maxima over the wavefront, the sums; then
@@ -159,9 +164,8 @@ __global__ __launch_bounds__(256) void route_kernel(RouteArgs a, int32_t* __rest
     const int64_t t = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
     if (t >= a.T) return;
     int id[EPL];
-    uint32_t chosen[EPL];
     float w[EPL];
-    route_token<EPL, Src>(a, t, id, chosen, w);
+    route_token<EPL, Src>(a, t, id, w);
 #pragma unroll
     for (int s = 0; s < EPL; ++s) {
         const int i = 64 * s + __lane_id();
