@@ -29,13 +29,19 @@ HIPCC_FLAGS = [
 # third of the throughput gone).  The build therefore reads the device assembly and refuses a GEMM kernel that
 # has a scratch access inside a loop that also holds MFMAs.  (Spills outside the loops only cost their own time;
 # they cannot let a DMA wait pass early: loads retire in order and extra entries in vmcnt make a wait stricter.)
+# The 4-bit products and the layer for few tokens are held to the same: their loops over k, of fewer MFMAs a step, have loads of
+# later steps under way, which the wait for a reload drains as well.
+SPILL_CHECKED = "(?:gemm|few_tokens)"
+
+
 def check_no_spill_in_k_loops(asm_text: str) -> None:
     # accumulators or fragments that were not promoted to registers show up as a large private segment
     for m in re.finditer(r"\.name:\s+(\S+)\n(?:.*\n)*?\s+\.private_segment_fixed_size:\s+(\d+)", asm_text):
-        if "gemm" in m.group(1) and int(m.group(2)) > 256:
+        if re.search(SPILL_CHECKED, m.group(1)) and int(m.group(2)) > 256:
             raise RuntimeError(f"{m.group(1)}: {m.group(2)} bytes of private memory per lane (an array left in memory?)")
-    for m in re.finditer(r"^(_ZN3moe\S*gemm\S*):\s*(?:;.*)?$", asm_text, re.M):
+    for m in re.finditer(rf"^(_ZN3moe\S*{SPILL_CHECKED}\S*):\s*(?:;.*)?$", asm_text, re.M):
         name = m.group(1)
+        least = 4 if "mx4_gemm" in name or "few_tokens" in name else 16   # MFMAs of a k-step
         end = asm_text.find(".Lfunc_end", m.end())
         lines = asm_text[m.end():end].splitlines()
         label_at = {ln.split(":")[0]: k for k, ln in enumerate(lines) if ln.startswith(".LBB")}
@@ -63,15 +69,15 @@ def check_no_spill_in_k_loops(asm_text: str) -> None:
                 continue
             lo, hi = min(around, key=lambda lp: lp[1] - lp[0])          # the innermost loop around the access
             inner = [lp for lp in loops if lo <= lp[0] and lp[1] <= hi and lp != (lo, hi)]
-            if any(mfmas(a, b) >= 16 for a, b in inner):
+            if any(mfmas(a, b) >= least for a, b in inner):
                 # a loop over tiles (resident kernels) with the k loops inside it: a reload between two tiles costs
                 # its own time only -- unless it sits in the middle of a straight run of MFMAs (the unrolled last
                 # iterations of a tile, which still have DMAs in flight)
-                if mfmas(max(lo, k - 40), k) >= 8 and mfmas(k, min(hi, k + 40)) >= 8:
+                if mfmas(max(lo, k - 40), k) >= least // 2 and mfmas(k, min(hi, k + 40)) >= least // 2:
                     raise RuntimeError(f"{name}: register spill among the MFMAs of a tile's last iterations")
                 continue
             own = sum("v_mfma" in lines[x] for x in range(lo, hi + 1) if not any(a <= x <= b for a, b in inner))
-            if own >= 16:
+            if own >= least:
                 raise RuntimeError(f"{name}: register spill inside a k loop (it would drain the DMA ring every iteration)")
 
 
