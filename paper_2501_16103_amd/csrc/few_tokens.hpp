@@ -476,8 +476,9 @@ __global__ __launch_bounds__(kFewThreads, 4) void few_tokens_down(FewArgs a) {
     const int T = a.route.T, k = a.route.k;
     if (tid < kMaxE / 32) r.chosen[tid] = 0;
     if (tid < T * k) {
+        const int id = a.ids[tid];          // (both loads before either is looked at: one trip to memory)
         const float w = a.weights[tid];
-        r.ids[tid] = w == 0.f ? -1 : a.ids[tid];
+        r.ids[tid] = w == 0.f ? -1 : id;
         r.weights[tid] = w;
     }
     __syncthreads();

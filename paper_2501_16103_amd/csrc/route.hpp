@@ -136,16 +136,18 @@ __device__ __forceinline__ int route_token(const RouteArgs& a, int64_t t, int (&
         }
     }
     if (!WEIGHTS) return unmasked;
-    const bool low = a.sigmoid && a.renormalize && top < kSigmoidLow;
     float sum = 0.f;
+    auto weigh = [&](auto score) __attribute__((always_inline)) {
 #pragma unroll
-    for (int s = 0; s < EPL; ++s) {
-        const float l = route_logit(chosen[s]);
-        float w = low ? (l < kSigmoidNone ? 0.f : expf(l - top)) : a.sigmoid ? 1.f / (1.f + expf(-l)) : empty ? 0.f : expf(l - top) / total;
-        if (64 * s + lane >= a.k) w = 0.f;
-        weights[s] = w;
-        sum += w;
-    }
+        for (int s = 0; s < EPL; ++s) {
+            weights[s] = 64 * s + lane < a.k ? score(route_logit(chosen[s])) : 0.f;
+            sum += weights[s];
+        }
+    };
+    // (one branch around all slots: a choice within them costs a token of 512 experts a microsecond)
+    if (!a.sigmoid) weigh([&](float l) { return empty ? 0.f : expf(l - top) / total; });
+    else if (a.renormalize && top < kSigmoidLow) weigh([&](float l) { return l < kSigmoidNone ? 0.f : expf(l - top); });
+    else weigh([&](float l) { return 1.f / (1.f + expf(-l)); });
     if (a.renormalize) {
         sum = wave_sum(sum);
 #pragma unroll
