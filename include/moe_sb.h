@@ -565,11 +565,11 @@ int moe_mx4_default_tiling(int T, int k, int E, int K, int N, int gated, moe_til
  *   out      DEVICE bf16 [T][hidden]
  *   workspace  DEVICE, 16-byte aligned, at least moe_few_tokens_workspace_bytes(desc) bytes, contents undefined before and after;
  *            calls that share one must not overlap.
- * out is rounded to bf16 once.  BF16: sums are fp32; h is rounded to bf16 once.  MX4: a block of 32 values of X or of h is two 8-bit
+ * out is rounded to bf16 once.  BF16: sums are fp32; h is two bf16 halves (off by at most 2^-16 of itself).  MX4: a block of 32 values of X or of h is two 8-bit
  * halves under one exponent: exact for X's values down to 2^-13 of the block's largest; a smaller one is off by at most 2^-21 of the largest, one of h by
  * that or 2^-8 of itself, whichever is more.  Their sums are those of the 8-bit matrix instructions: of the products of k = 8 i .. 8 i + 7 the bits
  * below 2^(e - 13) are dropped, e the largest exponent of a product among them, and the sums of these groups are added in fp32.  With values of one
- * order of magnitude that is far below out's rounding (the whole layer is off by 1.8e-3 of its norm, bf16 weights 2.3e-3); where a channel 2^8 / 2^11 above its
+ * order of magnitude that is far below out's rounding (the whole layer is off by 1.8e-3 of its norm, bf16 weights 1.7e-3); where a channel 2^8 / 2^11 above its
  * neighbours cancels within its group, what the neighbours leave is off by 0.6 % / 6 %.  A block with an infinity or NaN makes that token's products NaN.  A token is not touched by what is in the weights of experts that it did not
  * choose, nor by other tokens.  A choice of weight 0 adds nothing, whatever X and that expert's weights hold: a row whose experts are all masked is
  * zeros.  Deterministic.

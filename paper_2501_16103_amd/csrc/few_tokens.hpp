@@ -45,7 +45,7 @@ struct FewArgs {
     uint16_t* out;                // [T][hidden] bf16
     int32_t* ids;                 // [T][k]
     float* weights;               // [T][k]
-    uint16_t* h;                  // bf16 weights: [T * k][h_pitch] bf16
+    uint16_t* h;                  // bf16 weights: [T * k][h_pitch / 4] runs of four values' high halves and their low ones, see FewBf16
     uint8_t *h_hi, *h_lo;         // 4-bit weights: [T * k][h_pitch] e4m3, see FewMx4
     uint8_t* h_scales;            // [T * k][h_pitch / 32]
     char* x_split;                // 4-bit weights, tokens that LDS does not hold: FewMx4::token_bytes each
@@ -102,8 +102,8 @@ __device__ __forceinline__ int few_row(const FewRouting& r, int t, int k, int e)
 // The sum is not fp32's throughout: the instruction aligns the products of 8 consecutive k to the largest of them and drops the bits below
 // 2^(e - 13), e its operands' exponents added; only the groups' sums and the accumulator are added with 24 bits.  (Found with +P, -P and a small
 // product: in their group it survives at 2^-13 of P and vanishes at 2^-14, in another one it survives at 2^-17, the smallest tried, and beside an accumulator
-// at 2^-23.)  That is 7 * 2^-13 of a group's largest product at most.  Apart from sums in 64 bits: normal tokens 1.8e-3 of the norm (with bf16 weights 2.3e-3, for h's rounding), pairs of channels 2^8 above
-// the others that cancel 6e-3, 2^11 above 6.5e-2 (bf16 weights 2.3e-3).
+// at 2^-23.)  That is 7 * 2^-13 of a group's largest product at most.  Apart from sums in 64 bits: normal tokens 1.8e-3 of the norm (with bf16 weights 1.6e-3, which is out's rounding), pairs of channels 2^8 above
+// the others that cancel 6e-3, 2^11 above 6.5e-2 (bf16 weights 1.7e-3).
 // The instruction's 8-bit operand: lane 16 g + t holds k = 16 g + 0 .. 15 and 64 + 16 g + 0 .. 15 of token t, and the scale of
 // k = 32 g .. 32 g + 31.
 struct FewMx4 {
@@ -114,6 +114,7 @@ struct FewMx4 {
         i32x8_t hi, lo;
         uint32_t scale;           // byte 0: of hi, byte 1: of lo
     };
+    using Activations = Tokens;
     u32x4_t w[4];
     uint32_t scale;
     // Scale byte of a block whose largest magnitude has these fp32 bits; 4 less, that of lo, is a byte too.
@@ -211,8 +212,8 @@ struct FewMx4 {
         const uint32_t b = *reinterpret_cast<const uint8_t*>(from + 2 * T * pitch + t * (pitch / 32) + kb * 4 + g);
         f.scale = b | (b - 4) << 8;
     }
-    // activations that are split already.  valid: elements of a row that were written (a multiple of 32)
-    static __device__ __forceinline__ void load(Tokens& t, const uint8_t* hi, const uint8_t* lo, const uint8_t* scales, int kb, int valid) {
+    // valid: elements of a row that were written (a multiple of 32)
+    static __device__ __forceinline__ void load(Activations& t, const uint8_t* hi, const uint8_t* lo, const uint8_t* scales, int kb, int valid) {
         const int g = __lane_id() >> 4;
         const u32x4_t zero = {0u, 0u, 0u, 0u};
 #pragma unroll
@@ -250,11 +251,16 @@ struct FewMx4 {
 };
 
 // (steps of 16 k: twice as many of them in flight as of 32, in the same registers)
+// h goes into the second launch as two bf16 halves, hi the nearest value and lo that of what is left: off by 2^-16 of itself at most, so that nothing but out is
+// rounded to 8 bits.  (One half: 2.3e-3 to 2.4e-3 of the output's norm from 64 bits instead of 1.7e-3, which is out's rounding.)  The registers hold two steps of
+// the second launch ahead with two halves, three with one.  us, one half / two: 64 experts, 2048 / 1408, 1 token 34.8 / 35.1, 4 tokens 70.3 / 71.6, 16 tokens 163 / 165;
+// 8 experts, 4096 / 14336, 1 token 122 / 124, 5 tokens 370 / 371, 16 tokens 472 / 473; 512 experts, 2048 / 512, 16 tokens 206 / 209.
 struct FewBf16 {
     static constexpr int KSTEP = 16, COLS = 128, BLOCKS = 8;
     template <bool> static constexpr int AHEAD_UP = 3;
-    static constexpr int AHEAD_DOWN = 3;
+    static constexpr int AHEAD_DOWN = 2;
     struct Tokens { u32x2_t x; };
+    struct Activations { u32x2_t hi, lo; };
     static __host__ __device__ constexpr int lds_bytes(int, int) { return 0; }
     u32x4_t w[4];
     // base: row k = 0 of the expert; col: this lane's first column; N: columns of a weight row (K is a multiple of 8)
@@ -277,15 +283,37 @@ struct FewBf16 {
         const int k = kb * KSTEP + 4 * (__lane_id() >> 4);
         t.x = k < valid ? *reinterpret_cast<const u32x2_t*>(xrow + k) : u32x2_t{0u, 0u};
     }
+    static __device__ __forceinline__ void load(Activations& t, const uint16_t* hrow, int kb, int valid) {
+        const int k = kb * KSTEP + 4 * (__lane_id() >> 4);
+        const u32x4_t x = k < valid ? *reinterpret_cast<const u32x4_t*>(hrow + 2 * k) : u32x4_t{0u, 0u, 0u, 0u};
+        t.hi = u32x2_t{x.x, x.y};
+        t.lo = u32x2_t{x.z, x.w};
+    }
+    // value `col` of a row of h
+    static __device__ __forceinline__ void store(uint16_t* hrow, int col, float v) {
+        const uint32_t hi = pack_bf16(v, 0.f) & 0xffffu;
+        const bool number = (hi & 0x7f80u) != 0x7f80u;        // (what is left of an infinity or NaN is nothing)
+        uint16_t* p = hrow + 2 * (col & ~3) + (col & 3);
+        p[0] = (uint16_t)hi;
+        p[4] = number ? (uint16_t)pack_bf16(v - __uint_as_float(hi << 16), 0.f) : (uint16_t)0;
+    }
     // The lane holds 4 rows x 8 columns: words of two columns of a row become words of two rows of a column.
+    __device__ __forceinline__ s16x4_t column(int j) const {
+        u32x2_t a;
+#pragma unroll
+        for (int q = 0; q < 2; ++q) a[q] = __builtin_amdgcn_perm(w[2 * q + 1][j >> 1], w[2 * q][j >> 1], j & 1 ? 0x07060302u : 0x05040100u);
+        return __builtin_bit_cast(s16x4_t, a);
+    }
     __device__ __forceinline__ void multiply(const Tokens& t, f32x4_t (&acc)[BLOCKS]) const {
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            u32x2_t a;
+        for (int j = 0; j < 8; ++j) acc[j] = __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(column(j), __builtin_bit_cast(s16x4_t, t.x), acc[j], 0, 0, 0);
+    }
+    __device__ __forceinline__ void multiply(const Activations& t, f32x4_t (&acc)[BLOCKS]) const {
 #pragma unroll
-            for (int q = 0; q < 2; ++q)
-                a[q] = __builtin_amdgcn_perm(w[2 * q + 1][j >> 1], w[2 * q][j >> 1], j & 1 ? 0x07060302u : 0x05040100u);
-            acc[j] = __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(__builtin_bit_cast(s16x4_t, a), __builtin_bit_cast(s16x4_t, t.x), acc[j], 0, 0, 0);
+        for (int j = 0; j < 8; ++j) {
+            const s16x4_t a = column(j);
+            acc[j] = __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(a, __builtin_bit_cast(s16x4_t, t.hi), acc[j], 0, 0, 0);
+            acc[j] = __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(a, __builtin_bit_cast(s16x4_t, t.lo), acc[j], 0, 0, 0);
         }
     }
     // matrix row i of block j is column 8 i + j: f(column, sums of columns column .. column + 3)
@@ -458,7 +486,7 @@ __global__ __launch_bounds__(kFewThreads, 4) void few_tokens_up(FewArgs a) {
                     if (o == 0) a.h_scales[at_h >> 5] = (uint8_t)byte;
                 }
             } else if (row >= 0 && col < a.h_pitch) {
-                a.h[at_h] = (uint16_t)pack_bf16(h, 0.f);
+                W::store(a.h + (int64_t)row * 2 * a.h_pitch, col, h);
             }
         }
         __syncthreads();
@@ -511,7 +539,9 @@ __global__ __launch_bounds__(kFewThreads, 4) void few_tokens_down(FewArgs a) {
     l.kb = from - l.slot * a.steps2;
     if (from < to) enter(l);
     Place m = l;
-    auto load = [&](W& s, typename W::Tokens& t) __attribute__((always_inline)) {
+    // (h along with the weights of its step: loads return in order, and with h asked for a step ahead alone the wait for it is one for weights of later
+    // steps, 5 to 9 % with bf16)
+    auto load = [&](W& s, typename W::Activations& t) __attribute__((always_inline)) {
         const uint32_t col = c * W::COLS + (W::COLS / 16) * li;
         const int64_t at_h = (int64_t)(l.row < 0 ? 0 : l.row) * a.h_pitch;
         if constexpr (MX4) {
@@ -519,12 +549,12 @@ __global__ __launch_bounds__(kFewThreads, 4) void few_tokens_down(FewArgs a) {
             W::load(t, a.h_hi + at_h, a.h_lo + at_h, a.h_scales + (at_h >> 5), l.kb, a.h_pitch);
         } else {
             s.load(reinterpret_cast<const uint16_t*>(a.down) + l.e * a.inter * a.hidden, col < a.hidden ? col : 0, a.hidden, a.inter, l.kb);
-            W::load(t, a.h + at_h, l.kb, a.h_pitch);
+            W::load(t, a.h + 2 * at_h, l.kb, a.h_pitch);
         }
     };
     constexpr int AHEAD = W::AHEAD_DOWN;
     W buf[AHEAD + 1];
-    typename W::Tokens tok[AHEAD + 1];
+    typename W::Activations tok[AHEAD + 1];
 #pragma unroll
     for (int i = 0; i < AHEAD; ++i) {
         if (from + i >= to) break;
@@ -536,10 +566,10 @@ __global__ __launch_bounds__(kFewThreads, 4) void few_tokens_down(FewArgs a) {
             load(buf[AHEAD], tok[AHEAD]);
             onward(l, step + AHEAD + 1 < to);
         }
-        buf[0].multiply(tok[0], acc);
         const int row = m.row;
         const bool last_step = step + 1 == to;
-        if (onward(m, !last_step) || last_step) {                   // the wavefront's last step of this expert
+        buf[0].multiply(tok[0], acc);
+        if (onward(m, !last_step) || last_step) {
             // (a token that did not choose it takes nothing: not 0 times what may be an infinity)
             if (row >= 0 && li < T) {
                 const float w = r.weights[row];

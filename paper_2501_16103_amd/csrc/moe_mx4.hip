@@ -184,7 +184,7 @@ int few_sizes(const moe_few_tokens_desc* d, FewSizes* z) {
     if (parts > (steps + kFewWaves - 1) / kFewWaves) parts = (steps + kFewWaves - 1) / kFewWaves;
     z->grid1 = (int)(tiles < kCus ? tiles : kCus);
     z->parts2 = (int)(parts < 1 ? 1 : parts);
-    z->h_bytes = mx4 ? 2 * up256((size_t)rows * z->h_pitch) + up256((size_t)rows * (z->h_pitch / kMxBlock)) : up256((size_t)rows * z->h_pitch * 2);
+    z->h_bytes = mx4 ? 2 * up256((size_t)rows * z->h_pitch) + up256((size_t)rows * (z->h_pitch / kMxBlock)) : up256((size_t)rows * z->h_pitch * 4);
     z->partial_bytes = up256((size_t)z->tiles2 * z->parts2 * kFewTokens * (mx4 ? FewMx4::COLS : FewBf16::COLS) * sizeof(float));
     z->arrived_bytes = up256((size_t)z->tiles2 * sizeof(int));
     z->split_bytes = mx4 && !few_staged(d->T, d->hidden) ? (size_t)d->T * FewMx4::token_bytes(d->hidden) : 0;
