@@ -150,6 +150,10 @@ int few_group(const moe_few_tokens_desc* d, int tiles) {
     return 7 * by_two <= 8 * by_one ? 2 : 1;
 }
 
+// Tokens in LDS, split by every workgroup of the first launch, wherever it holds them; else split once by a launch of their own and read from
+// memory, with a step of weights ahead instead of three.  4 bits, us, in LDS / by a launch: 64 experts, 2048 / 1408, 1 token 16.6 / 18.2, 4 tokens 29.5 / 31.1, 16 tokens
+// 61.7 / 70.1; 32 experts, 3584 / 1280, 1 token 19.1 / 21.0, 16 tokens 64.6 / 73.8; 128 experts, 2048 / 512, 1 token 16.3 / 17.8; 8 experts, 4096 / 14336, 1 token
+// 41.0 / 43.5, 8 tokens 125 / 134.
 bool few_staged(int T, int hidden) { return few_lds_bytes<FewMx4>(T) + FewMx4::lds_bytes(T, hidden) <= kFewLdsMost; }
 
 int few_sizes(const moe_few_tokens_desc* d, FewSizes* z) {
@@ -178,6 +182,10 @@ int few_sizes(const moe_few_tokens_desc* d, FewSizes* z) {
     const int64_t rows = (int64_t)d->T * d->k, slots = rows < d->E ? rows : d->E;
     // A workgroup per CU.  (Two, where LDS holds them: 4 bits within 3 % either way; bf16, 8 experts, 4096 / 14336, 5 tokens 404 us instead
     // of 361.)  A part of the second launch is at least a step for each of its wavefronts.
+    // Column tiles of 4-bit weights are taken by twos throughout.  us, one / two: 64 experts, 2048 / 1408, 1 token 17.8 / 16.6, 4 tokens 30.9 / 29.5, 16 tokens 65.9 / 61.7;
+    // 8 experts, 4096 / 14336, 1 token 41.7 / 41.0, 8 tokens 126 / 125, 16 tokens 176 / 157; 32 experts, 3584 / 1280, 16 tokens 65.1 / 64.6; 128 experts,
+    // 2048 / 512, 4 tokens 22.7 / 21.5.  Where that leaves most of the CUs without a workgroup it loses: one token, 32 experts, 3584 / 1280 (80 workgroups) 16.6 /
+    // 19.1, 128 experts, 2048 / 512 (64) 14.7 / 16.3.
     z->group1 = mx4 ? 2 : few_group(d, z->tiles1);
     const int64_t tiles = slots * ((z->tiles1 + z->group1 - 1) / z->group1), steps = slots * z->steps2;
     int64_t parts = (kCus + z->tiles2 - 1) / z->tiles2;
@@ -297,7 +305,9 @@ int moe_mx4_default_tiling(int T, int k, int E, int K, int N, int gated, moe_til
     //   8 experts, 4096 -> 28672 (896): 7 rows 95.0 / 98.4 / 89.4 and 64.6 / 72.0 / 74.0, 10 rows 97.0 / 100.7 / 89.2 and 81.4 / 83.9 / 78.3, 16 rows 108.0 /
     //   104.6 / 89.8 and 94.0 / 94.1 / 82.4; 16 experts, 4096 -> 14336 (896): 4 rows 92.4 / 96.9 / 88.3 and 71.9 / 73.5 / 79.8, 12 rows 94.1 / 104.0 / 89.1 and
     //   91.5 / 95.7 / 81.8; 64 experts, 2048 -> 4096 (1024): 12 rows 58.2 / 60.5 / 54.5 and 43.1 / 47.5 / 46.7; 256 experts, 2048 -> 1024 (1024): 16 rows 62.5 /
-    //   62.6 / 55.2 and 45.3 / 43.0 / 37.5; 64 experts, 2048 -> 3500 (896): 12 rows 48.6 / 53.7 / 50.1 and 36.8 / 38.5 / 43.8 (the one that loses).
+    //   62.6 / 55.2 and 45.3 / 43.0 / 37.5; 64 experts, 2048 -> 3500 (896): 12 rows 48.6 / 53.7 / 50.1 and 36.8 / 38.5 / 43.8.
+    // An average says nothing of how rows are spread, and the rule loses by that: with 704 stripes a skewed routing of 12 rows (35.0, the slowest of the three; 128 rows
+    // 28.5) and an even one of 19 (45.0 against 42.3), with 896 the skewed 12 of 2048 -> 3500 (43.8 against 36.8).
     const int64_t R = (int64_t)T * k, stripes = E * ((mx4_packed_columns(N, gated) + 255) / 256);
     const int middle = stripes > 3 * kCus ? 128 : 32;
     const moe_tiling g = {R > 16 * (int64_t)E ? 128 : R > 8 * (int64_t)E ? middle : 16, 256, MOE_ORDER_ASCENDING, 0, 0, 0};
