@@ -17,7 +17,7 @@
 // each leaves its fp32 sums in the workspace, and the last one to arrive adds them in the order of the parts, so the result
 // does not depend on who that is.
 //
-// What bounds it: with many weights memory (8 experts, 4096 / 14336, bf16: 5 tokens 333 to 390 us by the experts chosen, 5.5 to 5.9 TB/s; 4 bits: 8 tokens
+// What bounds it: with many weights memory (8 experts, 4096 / 14336, bf16: 5 tokens 311 to 373 us by the experts chosen, 5.5 to 5.9 TB/s; 4 bits: 8 tokens
 // 124 us, 5.4 TB/s, 16 tokens 149); with few the chain of the two launches.  One token, 6 of 64 experts, 2048 / 1408, in us from the first launch's start: routed at
 // 2.2, weights there at 5 to 6 (bf16: 16 to 20), h written at 7.7 (22), the second launch begins at 8.9 (23.5), its weights are there at 11.5 to 12.5
 // (31.6 to 33.6), sums of the parts at 14.5 (36), done at 15.5 (37.5).
