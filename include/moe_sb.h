@@ -37,9 +37,9 @@ enum {
     MOE_ERR_TOO_LARGE = -5    /* the problem needs more scratch memory than the library's static array holds */
 };
 
-/* (FP32 and MX4 are types of the router's logits, of what is quantised and of the weights of moe_layer_few_tokens; the products over
- * [E][K][N] weights take BF16 and FP8_E4M3.) */
-enum { MOE_DTYPE_BF16 = 0, MOE_DTYPE_FP8_E4M3 = 1, MOE_DTYPE_FP32 = 2, MOE_DTYPE_MX4 = 3 };
+/* (FP32 and MX4 are types of the router's logits, of what is quantised and of the weights of moe_layer_few_tokens, FP16 one of the scales of
+ * moe_w4_pack_weights; the products over [E][K][N] weights take BF16 and FP8_E4M3.) */
+enum { MOE_DTYPE_BF16 = 0, MOE_DTYPE_FP8_E4M3 = 1, MOE_DTYPE_FP32 = 2, MOE_DTYPE_MX4 = 3, MOE_DTYPE_FP16 = 4 };
 
 /* Storage order of the expert weights (moe_gemm_desc.w_layout).  KN is the layout of the problem statement:
  * W[e][k][n], n contiguous.  NK is a pre-packed alternative, W[e][n][k], k contiguous (the order in which
@@ -587,6 +587,91 @@ int moe_layer_few_tokens(const void* X, const void* logits, const void* w_up, co
                          void* stream);
 /* HOST, pure; 0 on invalid or unsupported arguments and for T = 0. */
 size_t moe_few_tokens_workspace_bytes(const moe_few_tokens_desc* desc);
+
+/*
+ * The router of layers whose experts come in groups and whose load a bias evens out:
+ *     s_e = p_e + bias_e      p_e: softmax or sigmoid of the logits, as for moe_route
+ *     a group's score: its largest s (MOE_GROUP_MAX), or the sum of its two largest (MOE_GROUP_TOP2; of the one there is, where only one is unmasked)
+ *     the `kept` groups of the largest scores stay, equal ones by rising index; group g is experts g * E / groups ..
+ *   topk_ids      the k largest s within them in falling order, equal ones by falling logit, equal ones by rising index
+ *   topk_weights  p of these (without the bias), `renormalize` and `scale` as for moe_route
+ *   bias          DEVICE fp32 [E], or NULL for none
+ * Scores are computed and compared in 64 bits, weights rounded to fp32 once.  An expert whose logit or bias is -inf is masked: it has no part in
+ * the softmax, its weight is 0, and it is chosen only where the groups that stay have fewer than k others (by rising index, after them); a group
+ * of nothing else comes after all others.  A row of nothing but masked experts has ids 0 .. k-1 and weights 0.  A NaN score counts as larger than
+ * every number; a NaN or +inf logit in a softmax row makes all its scores NaN.  With one group and no bias these are moe_route's choices.
+ * logits, desc, topk_ids, topk_weights: as for moe_route.  groups divides E, 1 <= kept <= groups, k <= kept * (E / groups), else
+ * MOE_ERR_INVALID_ARG; groups <= 64, else MOE_ERR_UNSUPPORTED.  Deterministic.
+ */
+enum { MOE_GROUP_MAX = 0, MOE_GROUP_TOP2 = 1 };
+int moe_route_grouped(const void* logits, const float* bias, const moe_route_desc* desc, int groups, int kept, int group_score, int32_t* topk_ids,
+                      float* topk_weights, void* stream);
+
+/*
+ * The way into a layer: the residual's addition, the root-mean-square norm, and the normed rows as the products take them.
+ *     h = x + residual, rounded to the residual's type (h = x without one)
+ *     y = h / sqrt(mean of h^2 + eps) * weight
+ *   x             DEVICE [rows][cols] x_dtype, rows x_stride elements apart
+ *   residual      DEVICE [rows][cols] residual_dtype, rows residual_stride elements apart, or NULL
+ *   weight        DEVICE [cols] weight_dtype, or NULL for ones
+ *   residual_out  DEVICE [rows][cols] residual_dtype: h, or NULL; may be `residual` or x itself where type and row stride (cols) are the same
+ *   y             DEVICE [rows][cols] bf16, or NULL
+ *   codes         DEVICE [rows][cols] e4m3, with
+ *   scales        DEVICE fp32 [rows]: what moe_grouped_gemm takes as X and x_scale; or both NULL.  scale = max |y| of the row / 448, at least
+ *                 2^-126; a code is the e4m3 value nearest to y / scale (ties to even).  A row with an infinity or NaN in h or y has the scale
+ *                 NaN and codes of NaN.
+ * At least one output.  Outputs are contiguous and overlap nothing else.  Types FP32 and BF16, eps >= 0 (a row of zeros with eps 0 gives zeros).  Sums of squares, the
+ * norm and y are fp32 (64 bits where squares leave fp32's range); y and codes are rounded from y in fp32 each.
+ * cols <= 65536, rows <= 2^24, else MOE_ERR_UNSUPPORTED.  rows = 0 does nothing.  Any alignment of the types; rows on 16 bytes and cols a multiple of 8 are
+ * the fast case.  Deterministic.
+ */
+typedef struct moe_norm_desc {
+    int64_t rows;
+    int64_t x_stride, residual_stride;   /* elements */
+    int32_t cols;
+    int32_t x_dtype, residual_dtype, weight_dtype;
+    float eps;
+} moe_norm_desc;
+int moe_add_norm(const void* x, const void* residual, const void* weight, const moe_norm_desc* desc, void* residual_out, void* y, void* codes, float* scales,
+                 void* stream);
+/* The same codes and scales of rows as they are (the second fp8 product's activations): src DEVICE [rows][cols] fp32 or bf16, rows row_stride elements apart. */
+int moe_fp8_quantize(const void* src, int dtype, int64_t rows, int cols, int64_t row_stride, void* codes, float* scales, void* stream);
+
+/*
+ * At most 16 tokens times a dense weight in 4 bits with a scale, and a zero point, for every `group` elements along K (the shared expert beside the
+ * routed ones):
+ *     out[t][n] = (add[t][n] +) sum_k X[t][k] * (q[k][n] - zero[k / group][n]) * scale[k / group][n]
+ * gated = 1: N = [gate | up] halves, out[t][i] = (add +) silu(gate_i) * up_i is [T][N / 2].
+ *
+ * Packing, once for a weight:
+ *   q        DEVICE bytes [K][N] (MOE_W_LAYOUT_KN) or [N][K] (MOE_W_LAYOUT_NK), the code 0 .. 15 in the low four bits
+ *   scales   DEVICE bf16 or fp16 (scale_dtype) [ceil(K / group)][N], or [N][ceil(K / group)]
+ *   zeros    DEVICE bytes of the scales' layout, 0 .. 15 in the low four bits, or NULL: 8 throughout
+ *   codes, words   DEVICE, 16-byte aligned, moe_w4_code_bytes / moe_w4_word_bytes bytes
+ * group 32, 64 or 128 (the last one may be shorter), K and N at most 2^20, else MOE_ERR_UNSUPPORTED.
+ */
+int moe_w4_pack_weights(const uint8_t* q, const void* scales, const uint8_t* zeros, int scale_dtype, int w_layout, int K, int N, int group, int gated, void* codes,
+                        void* words, void* stream);
+/* HOST, pure; 0 on invalid or unsupported arguments. */
+size_t moe_w4_code_bytes(int K, int N, int gated);
+size_t moe_w4_word_bytes(int K, int N, int group, int gated);
+
+/*
+ * The product.
+ *   X      DEVICE bf16 [T][K], rows x_stride elements apart (16-byte aligned rows and K a multiple of 8 are the fast case)
+ *   codes, words   what moe_w4_pack_weights wrote for this K, N, group and gated
+ *   add    DEVICE bf16, of out's shape, or NULL; may be out itself
+ *   out    DEVICE bf16 [T][N], or [T][N / 2] of gated weights; overlaps X nowhere
+ * Products are exact, sums, activation and addition fp32, one rounding to bf16.  A sum over a group of q - z is formed as one over 128 + q less one of
+ * 128 + z: it is off by about 2^-24 of 144 times the sum of |X| there.  An infinity or NaN in a token's X makes all its outputs NaN; tokens do not
+ * touch each other.  T <= 16, else MOE_ERR_UNSUPPORTED; T = 0 does nothing.  Deterministic.
+ */
+typedef struct moe_w4_desc {
+    int32_t T, K, N;
+    int32_t group;
+    int32_t gated;
+} moe_w4_desc;
+int moe_w4_matvec(const void* X, int64_t x_stride, const void* codes, const void* words, const moe_w4_desc* desc, const void* add, void* out, void* stream);
 
 /* Static string for a return code. */
 const char* moe_strerror(int code);

@@ -28,12 +28,15 @@ MOE_DTYPE_BF16 = 0
 MOE_DTYPE_FP8_E4M3 = 1
 MOE_DTYPE_FP32 = 2
 MOE_DTYPE_MX4 = 3
+MOE_DTYPE_FP16 = 4
 MOE_W_LAYOUT_KN = 0
 MOE_W_LAYOUT_NK = 1
 MOE_EPILOGUE_NONE = 0
 MOE_EPILOGUE_SWIGLU = 1
 MOE_SCORE_SOFTMAX = 0
 MOE_SCORE_SIGMOID = 1
+MOE_GROUP_MAX = 0
+MOE_GROUP_TOP2 = 1
 MOE_ORDER_ASCENDING = 0
 MOE_ORDER_SPREAD = 1
 MOE_ORDER_INTERLEAVE = 2
@@ -68,6 +71,7 @@ EXPORTS = [
     "moe_route", "moe_mx4_quantize", "moe_mx4_prepare", "moe_mx4_row_code_bytes", "moe_mx4_row_scale_bytes", "moe_mx4_pack_weights",
     "moe_mx4_weight_code_bytes", "moe_mx4_weight_scale_bytes", "moe_mx4_packed_columns", "moe_mx4_grouped_gemm",
     "moe_mx4_tile_supported", "moe_mx4_default_tiling", "moe_layer_few_tokens", "moe_few_tokens_workspace_bytes",
+    "moe_route_grouped", "moe_add_norm", "moe_fp8_quantize", "moe_w4_code_bytes", "moe_w4_word_bytes", "moe_w4_pack_weights", "moe_w4_matvec",
     "moe_strerror",
 ]
 
@@ -110,6 +114,15 @@ class moe_mx4_gemm_desc(ctypes.Structure):
 class moe_few_tokens_desc(ctypes.Structure):
     _fields_ = [(n, ctypes.c_int32) for n in ("T", "k", "E", "hidden", "inter", "w_dtype", "logits_dtype", "score", "renormalize")] + [
         ("scale", ctypes.c_float)]
+
+
+class moe_norm_desc(ctypes.Structure):
+    _fields_ = [("rows", ctypes.c_int64), ("x_stride", ctypes.c_int64), ("residual_stride", ctypes.c_int64), ("cols", ctypes.c_int32),
+                ("x_dtype", ctypes.c_int32), ("residual_dtype", ctypes.c_int32), ("weight_dtype", ctypes.c_int32), ("eps", ctypes.c_float)]
+
+
+class moe_w4_desc(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("T", "K", "N", "group", "gated")]
 
 
 _lib = None
@@ -223,6 +236,20 @@ def lib() -> ctypes.CDLL:
             ctypes.c_size_t, ctypes.c_void_p]
         L.moe_few_tokens_workspace_bytes.restype = ctypes.c_size_t
         L.moe_few_tokens_workspace_bytes.argtypes = [ctypes.POINTER(moe_few_tokens_desc)]
+        L.moe_route_grouped.restype = ctypes.c_int
+        L.moe_route_grouped.argtypes = [ctypes.c_void_p, ctypes.c_void_p, ctypes.POINTER(moe_route_desc)] + [ctypes.c_int] * 3 + [ctypes.c_void_p] * 3
+        L.moe_add_norm.restype = ctypes.c_int
+        L.moe_add_norm.argtypes = [ctypes.c_void_p] * 3 + [ctypes.POINTER(moe_norm_desc)] + [ctypes.c_void_p] * 5
+        L.moe_fp8_quantize.restype = ctypes.c_int
+        L.moe_fp8_quantize.argtypes = [ctypes.c_void_p, ctypes.c_int, ctypes.c_int64, ctypes.c_int, ctypes.c_int64] + [ctypes.c_void_p] * 3
+        L.moe_w4_code_bytes.restype = ctypes.c_size_t
+        L.moe_w4_code_bytes.argtypes = [ctypes.c_int] * 3
+        L.moe_w4_word_bytes.restype = ctypes.c_size_t
+        L.moe_w4_word_bytes.argtypes = [ctypes.c_int] * 4
+        L.moe_w4_pack_weights.restype = ctypes.c_int
+        L.moe_w4_pack_weights.argtypes = [ctypes.c_void_p] * 3 + [ctypes.c_int] * 6 + [ctypes.c_void_p] * 3
+        L.moe_w4_matvec.restype = ctypes.c_int
+        L.moe_w4_matvec.argtypes = [ctypes.c_void_p, ctypes.c_int64] + [ctypes.c_void_p] * 2 + [ctypes.POINTER(moe_w4_desc)] + [ctypes.c_void_p] * 3
         L.moe_strerror.restype = ctypes.c_char_p
         L.moe_strerror.argtypes = [ctypes.c_int]
         _lib = L
@@ -787,6 +814,149 @@ class MoeFewTokensPlan:
         return self.out, self.ids, self.weights
 
 
+def _here(*tensors) -> bool:
+    """Whether a launch on the current device's stream may touch all of these (None is no tensor)."""
+    device = -1
+    for t in tensors:
+        if t is not None:
+            at = t.get_device()
+            if at < 0 or (device >= 0 and at != device):
+                return False
+            device = at
+    return device < 0 or device == torch.cuda.current_device()
+
+
+def moe_route_grouped(logits: torch.Tensor, k: int, topk_ids: torch.Tensor, topk_weights: torch.Tensor, groups: int, kept: int,
+                      group_score: int = MOE_GROUP_MAX, bias: Optional[torch.Tensor] = None, score: int = MOE_SCORE_SOFTMAX, renormalize: bool = True,
+                      scale: float = 1.0, check: bool = True) -> int:
+    """moe_route among the experts of the `kept` best of `groups` groups, by score + bias (fp32 [E])."""
+    T, E = logits.shape
+    row, step = logits.stride()
+    n = T * k
+    rc = MOE_ERR_INVALID_ARG
+    if (topk_ids.numel() >= n and topk_weights.numel() >= n and topk_ids.dtype is torch.int32 and topk_weights.dtype is torch.float32 and
+            topk_ids.is_contiguous() and topk_weights.is_contiguous() and (step == 1 or E <= 1) and _holds(bias, E, torch.float32) and
+            _here(logits, topk_ids, topk_weights, bias)):
+        d = moe_route_desc(T, k, E, _DTYPES.get(logits.dtype, -1), row, score, renormalize, scale)
+        rc = lib().moe_route_grouped(logits.data_ptr(), _ptr(bias), ctypes.byref(d), groups, kept, group_score, topk_ids.data_ptr(),
+                                     topk_weights.data_ptr(), _stream())
+    if check and rc != MOE_OK:
+        raise MoeError(rc, "moe_route_grouped")
+    return rc
+
+
+class Fp8Rows:
+    """Up to `rows` rows of `cols` e4m3 values, `codes` (bytes), with a scale each, `scales`: X and x_scale of an fp8 product."""
+
+    def __init__(self, rows: int, cols: int, device="cuda:0"):
+        if rows < 0 or cols < 1:
+            raise MoeError(MOE_ERR_INVALID_ARG, "Fp8Rows")
+        self.rows, self.cols = rows, cols
+        self.codes = torch.empty((rows, cols), dtype=torch.uint8, device=device)
+        self.scales = torch.empty(rows, dtype=torch.float32, device=device)
+
+    def quantize(self, src: torch.Tensor) -> "Fp8Rows":
+        """src [up to rows, cols], fp32 or bf16, rows of consecutive elements."""
+        moe_fp8_quantize(src, self)
+        return self
+
+
+def moe_fp8_quantize(src: torch.Tensor, out: Fp8Rows, check: bool = True) -> int:
+    """Rows of src [rows, cols] -> out's first rows."""
+    rows, cols = src.shape
+    row, step = src.stride()
+    rc = MOE_ERR_INVALID_ARG
+    if rows <= out.rows and cols == out.cols and (step == 1 or cols <= 1) and _here(src, out.codes):
+        rc = lib().moe_fp8_quantize(src.data_ptr(), _DTYPES.get(src.dtype, -1), rows, cols, row, out.codes.data_ptr(), out.scales.data_ptr(), _stream())
+    if check and rc != MOE_OK:
+        raise MoeError(rc, "moe_fp8_quantize")
+    return rc
+
+
+def moe_add_norm(x: torch.Tensor, weight: Optional[torch.Tensor], eps: float, residual: Optional[torch.Tensor] = None,
+                 residual_out: Optional[torch.Tensor] = None, y: Optional[torch.Tensor] = None, rows: Optional[Fp8Rows] = None, check: bool = True) -> int:
+    """x + residual -> residual_out; its root-mean-square norm times weight -> y (bf16), rows (e4m3 with scales), or both.  x and residual
+    [T, H] with rows of consecutive elements, outputs contiguous."""
+    T, H = x.shape
+    x_row, x_step = x.stride()
+    fits = (x_step == 1 or H <= 1) and _here(x, weight, residual, residual_out, y, None if rows is None else rows.codes)
+    fits = fits and (weight is None or (weight.shape == (H,) and weight.is_contiguous())) and _holds(y, T * H, torch.bfloat16)
+    r_row, r_type = 0, MOE_DTYPE_FP32
+    if residual is not None:
+        fits = fits and residual.shape == x.shape and (residual.stride(1) == 1 or H <= 1) and _holds(residual_out, T * H, residual.dtype)
+        r_row, r_type = residual.stride(0), _DTYPES.get(residual.dtype, -1)
+    if rows is not None:
+        fits = fits and T <= rows.rows and rows.cols == H
+    rc = MOE_ERR_INVALID_ARG
+    if fits:
+        d = moe_norm_desc(T, x_row, r_row, H, _DTYPES.get(x.dtype, -1), r_type, MOE_DTYPE_FP32 if weight is None else _DTYPES.get(weight.dtype, -1), eps)
+        rc = lib().moe_add_norm(x.data_ptr(), _ptr(residual), _ptr(weight), ctypes.byref(d), _ptr(residual_out), _ptr(y),
+                                None if rows is None else rows.codes.data_ptr(), None if rows is None else rows.scales.data_ptr(), _stream())
+    if check and rc != MOE_OK:
+        raise MoeError(rc, "moe_add_norm")
+    return rc
+
+
+def moe_w4_code_bytes(K: int, N: int, gated: bool = False) -> int:
+    return int(lib().moe_w4_code_bytes(K, N, int(gated)))
+
+
+def moe_w4_word_bytes(K: int, N: int, group: int, gated: bool = False) -> int:
+    return int(lib().moe_w4_word_bytes(K, N, group, int(gated)))
+
+
+class W4Weights:
+    """A dense weight [K, N] in 4 bits with a scale and a zero point for every `group` elements along K, as moe_w4_matvec takes it.  gated: N =
+    [gate | up] halves."""
+
+    def __init__(self, K: int, N: int, group: int, gated: bool = False, device="cuda:0"):
+        self.K, self.N, self.group, self.gated = K, N, group, bool(gated)
+        nbytes = moe_w4_word_bytes(K, N, group, gated)
+        if nbytes == 0:
+            raise MoeError(MOE_ERR_INVALID_ARG, "moe_w4_word_bytes")
+        self.codes = torch.empty(moe_w4_code_bytes(K, N, gated), dtype=torch.uint8, device=device)
+        self.words = torch.empty(nbytes, dtype=torch.uint8, device=device)
+
+    def pack(self, q: torch.Tensor, scales: torch.Tensor, zeros: Optional[torch.Tensor] = None, w_layout: int = MOE_W_LAYOUT_KN) -> "W4Weights":
+        """q uint8 [K, N], codes 0 .. 15; scales bf16 or fp16 [ceil(K / group), N]; zeros uint8 of the scales' shape, or None for 8 throughout.  With
+        MOE_W_LAYOUT_NK all of them transposed."""
+        moe_w4_pack_weights(q, scales, zeros, w_layout, self)
+        return self
+
+
+_SCALE_DTYPES = {torch.bfloat16: MOE_DTYPE_BF16, torch.float16: MOE_DTYPE_FP16}
+
+
+def moe_w4_pack_weights(q: torch.Tensor, scales: torch.Tensor, zeros: Optional[torch.Tensor], w_layout: int, W: W4Weights, check: bool = True) -> int:
+    shape, small = (W.K, W.N), (-(-W.K // W.group), W.N)
+    if w_layout == MOE_W_LAYOUT_NK:
+        shape, small = shape[::-1], small[::-1]
+    fits = (q.shape == shape and q.dtype == torch.uint8 and q.is_contiguous() and scales.shape == small and scales.is_contiguous() and
+            (zeros is None or (zeros.shape == small and zeros.dtype == torch.uint8 and zeros.is_contiguous())) and _here(q, scales, zeros, W.codes))
+    rc = MOE_ERR_INVALID_ARG
+    if fits:
+        rc = lib().moe_w4_pack_weights(_ptr(q), _ptr(scales), _ptr(zeros), _SCALE_DTYPES.get(scales.dtype, -1), w_layout, W.K, W.N, W.group, int(W.gated),
+                                       _ptr(W.codes), _ptr(W.words), _stream())
+    if check and rc != MOE_OK:
+        raise MoeError(rc, "moe_w4_pack_weights")
+    return rc
+
+
+def moe_w4_matvec(X: torch.Tensor, W: W4Weights, out: torch.Tensor, add: Optional[torch.Tensor] = None, check: bool = True) -> int:
+    """X bf16 [T, W.K], T <= 16, rows of consecutive elements -> out bf16 [T, W.N, or W.N / 2 of gated weights], with `add` (of its shape) added."""
+    T, K = X.shape
+    row, step = X.stride()
+    n = T * (W.N // 2 if W.gated else W.N)
+    rc = MOE_ERR_INVALID_ARG
+    if (K == W.K and X.dtype is torch.bfloat16 and (step == 1 or K <= 1) and out.dtype is torch.bfloat16 and out.numel() >= n and out.is_contiguous() and
+            _holds(add, n, torch.bfloat16) and _here(X, W.codes, out, add)):
+        d = moe_w4_desc(T, K, W.N, W.group, W.gated)
+        rc = lib().moe_w4_matvec(X.data_ptr(), row, W.codes.data_ptr(), W.words.data_ptr(), ctypes.byref(d), _ptr(add), out.data_ptr(), _stream())
+    if check and rc != MOE_OK:
+        raise MoeError(rc, "moe_w4_matvec")
+    return rc
+
+
 class MoeLayerPlan:
     """Buffers and tilings for one bf16 MoE feed-forward layer (Sec. 2.2) run with the library's calls only:
 
@@ -882,5 +1052,60 @@ class MoeLayerPlan:
             moe_grouped_gemm_splitk(self.act, W_down, self.map2, self.down, self.d2, self.k_parts, self.workspace)
         else:
             moe_grouped_gemm(self.act, W_down, flat, self.map2, self.down, self.d2)
+        moe_combine(self.down, topk_weights, T, k, self.hidden, self.out)
+        return self.out
+
+
+class MoeFp8LayerPlan:
+    """Buffers and tilings of one MoE feed-forward layer over fp8 weights, tokens and activations (each row of them with a scale):
+
+        rows in 8 bits (moe_add_norm's, or Fp8Rows.quantize's) -> maps of both products -> gate+up product with the fused gated activation
+        -> its rows in 8 bits -> down product -> weighted sum.
+
+    hidden and inter are multiples of 128."""
+
+    def __init__(self, T: int, k: int, E: int, hidden: int, inter: int, device="cuda:0"):
+        self.T, self.k, self.E, self.hidden, self.inter = T, k, E, hidden, inter
+        R = T * k
+        if hidden % 128 != 0 or inter % 128 != 0:
+            raise MoeError(MOE_ERR_UNSUPPORTED, "MoeFp8LayerPlan")
+        self.g1 = moe_default_tiling(MOE_DTYPE_FP8_E4M3, T, k, E, hidden, 2 * inter)
+        self.g2 = moe_default_tiling(MOE_DTYPE_FP8_E4M3, R, 1, E, inter, hidden)
+        self.map1 = alloc_task_map(T, k, E, self.g1.tile_m, self.g1.tile_n, 2 * inter, device)
+        self.map2 = alloc_task_map(R, 1, E, self.g2.tile_m, self.g2.tile_n, hidden, device)
+        self.rows = Fp8Rows(T, hidden, device)                                        # for a caller's tokens
+        self.act = torch.empty((R, inter), dtype=torch.bfloat16, device=device)       # [T, k, inter]
+        self.act_rows = Fp8Rows(R, inter, device)
+        self.down = torch.empty((R, hidden), dtype=torch.bfloat16, device=device)     # [T, k, hidden]
+        self.out = torch.empty((T, hidden), dtype=torch.bfloat16, device=device)
+
+    def forward(self, X: Fp8Rows, W_gate_up: torch.Tensor, up_scale: torch.Tensor, W_down: torch.Tensor, down_scale: torch.Tensor, topk_ids: torch.Tensor,
+                topk_weights: Optional[torch.Tensor]) -> torch.Tensor:
+        """X: T rows of hidden; W_gate_up [E, hidden, 2 * inter] (gate columns first) and W_down [E, inter, hidden] e4m3 bytes with fp32 scales [E];
+        topk_ids int32 [T, k]; topk_weights fp32 [T, k] or None.  Returns out [T, hidden] (the plan's buffer)."""
+        T, k, E, R, where = self.T, self.k, self.E, self.T * self.k, "MoeFp8LayerPlan.forward"
+        if X.rows < T or X.cols != self.hidden or not _here(X.codes, W_gate_up, up_scale, W_down, down_scale, topk_ids, topk_weights, self.out):
+            raise MoeError(MOE_ERR_INVALID_ARG, where)
+        _contiguous(where, W_gate_up, (E, self.hidden, 2 * self.inter))
+        _contiguous(where, W_down, (E, self.inter, self.hidden))
+        if W_gate_up.element_size() != 1 or W_down.element_size() != 1:
+            raise MoeError(MOE_ERR_INVALID_ARG, where)
+        _contiguous(where, up_scale, (E,), torch.float32)
+        _contiguous(where, down_scale, (E,), torch.float32)
+        _contiguous(where, topk_ids, (T, k), torch.int32)
+        if topk_weights is not None:
+            _contiguous(where, topk_weights, (T, k), torch.float32)
+        if T == 0:
+            return self.out
+
+        def desc(g: Tiling, T: int, k: int, K: int, N: int, rows: Fp8Rows, w_scale: torch.Tensor, epilogue: int) -> GemmDesc:
+            return GemmDesc(MOE_DTYPE_FP8_E4M3, T, k, E, K, N, g.tile_m, g.tile_n, rows.scales, w_scale, g.tile_m_small, g.small_max_rows,
+                            g.tile_m_slack, epilogue)
+
+        moe_build_task_map_pair_gemm(topk_ids, T, k, E, 2 * self.inter, self.g1, self.map1, self.hidden, self.g2, self.map2, X.codes, W_gate_up,
+                                     self.act, desc(self.g1, T, k, self.hidden, 2 * self.inter, X, up_scale, MOE_EPILOGUE_SWIGLU))
+        moe_fp8_quantize(self.act, self.act_rows)
+        moe_grouped_gemm(self.act_rows.codes, W_down, None, self.map2, self.down,
+                         desc(self.g2, R, 1, self.inter, self.hidden, self.act_rows, down_scale, MOE_EPILOGUE_NONE))
         moe_combine(self.down, topk_weights, T, k, self.hidden, self.out)
         return self.out

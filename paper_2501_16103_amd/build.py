@@ -9,7 +9,7 @@ import tempfile
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 LIB = os.path.join(HERE, "libmoe_sb.so")
-SRCS = [os.path.join(HERE, "csrc", f) for f in ("moe_sb.hip", "moe_mx4.hip")]
+SRCS = [os.path.join(HERE, "csrc", f) for f in ("moe_sb.hip", "moe_mx4.hip", "moe_block.hip")]
 # measurement kernels, kept out of the product library
 PROBE_LIB = os.path.join(HERE, "libmoe_probe.so")
 PROBE_SRCS = [os.path.join(HERE, "csrc", "moe_probe.hip")]

@@ -9,9 +9,6 @@
 
 namespace moe {
 
-__device__ __forceinline__ float bf16_lo(uint32_t v) { return __uint_as_float(v << 16); }
-__device__ __forceinline__ float bf16_hi(uint32_t v) { return __uint_as_float(v & 0xffff0000u); }
-
 // Chunks (8 columns) [c_begin, c_end) of all tokens, walked by `nthreads` threads of which this is number `tid`:
 // chunk index c -> token c / (N/8), column 8 * (c % (N/8)).
 // KU > 0: k is the compile-time KU and all k loads of a chunk are issued before the first is used.

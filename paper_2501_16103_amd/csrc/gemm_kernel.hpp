@@ -23,18 +23,9 @@
 
 #include "launch_rules.hpp"
 #include "task_map.hpp"
+#include "values.hpp"
 
 namespace moe {
-
-typedef __attribute__((ext_vector_type(8))) __bf16 bf16x8_t;
-typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2_t;
-typedef __attribute__((ext_vector_type(4))) float f32x4_t;
-typedef __attribute__((ext_vector_type(16))) float f32x16_t;
-typedef __attribute__((ext_vector_type(4))) short s16x4_t;
-typedef __attribute__((ext_vector_type(8))) short s16x8_t;
-typedef __attribute__((ext_vector_type(2))) int i32x2_t;
-typedef __attribute__((ext_vector_type(4))) unsigned int u32x4_t;
-typedef __attribute__((ext_vector_type(2))) unsigned int u32x2_t;
 
 #define MOE_LDS(T) __attribute__((address_space(3))) T
 
@@ -64,11 +55,6 @@ struct GemmArgs {
     void* red_out;                     // [red_T][red_N] bf16
     int red_T, red_k, red_N, red_tiles;
 };
-
-__device__ __forceinline__ uint32_t pack_bf16(float a, float b) {
-    bf16x2_t p = {(__bf16)a, (__bf16)b};  // hardware round-to-nearest-even
-    return __builtin_bit_cast(uint32_t, p);
-}
 
 // ---------------------------------------------------------------------------
 // The tile function (all tile shapes, bf16 and fp8)

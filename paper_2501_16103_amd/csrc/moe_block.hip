@@ -1,0 +1,175 @@
+// C-ABI entry points of the operators around a block's experts (the grouped router, norm and rows in 8 bits, the 4-bit product for few tokens):
+// argument checks and launches.  Everything that computes lives in route_grouped.hpp / norm_rows.hpp / w4.hpp.
+#include <hip/hip_runtime.h>
+#include <math.h>
+#include <stdint.h>
+
+#include "../../include/moe_sb.h"
+#include "launch_attr.hpp"
+#include "launch_rules.hpp"
+#include "norm_rows.hpp"
+#include "route_grouped.hpp"
+#include "task_map.hpp"
+#include "w4.hpp"
+
+using namespace moe;
+
+namespace {
+
+int launched() { return hipGetLastError() == hipSuccess ? MOE_OK : MOE_ERR_HIP; }
+bool misaligned(const void* p, int bytes) { return ((uintptr_t)p & (bytes - 1)) != 0; }
+int bytes_of(int dtype) { return dtype == MOE_DTYPE_FP32 ? 4 : 2; }
+bool fp32_or_bf16(int dtype) { return dtype == MOE_DTYPE_FP32 || dtype == MOE_DTYPE_BF16; }
+
+template <int EPL>
+int launch_grouped(const GroupedRouteArgs& a, bool f32, int32_t* ids, float* weights, hipStream_t s) {
+    const dim3 grid((a.T + 3) / 4);
+    if (f32) route_grouped_kernel<EPL, float><<<grid, 256, 0, s>>>(a, ids, weights);
+    else route_grouped_kernel<EPL, uint16_t><<<grid, 256, 0, s>>>(a, ids, weights);
+    return launched();
+}
+
+constexpr int kNormCols = 65536;
+
+template <bool VEC, bool NORM>
+int launch_norm_rows(const NormArgs& a, int64_t rows, hipStream_t s) {
+    const int chunks = (a.cols + 7) / 8;
+    int threads = (chunks + 63) / 64 * 64;
+    threads = threads < 256 ? threads : chunks <= 2048 ? 256 : 1024;
+    const dim3 grid((unsigned)rows);
+    const int each = (chunks + threads - 1) / threads;
+    if (each <= 1) norm_rows_kernel<1, VEC, NORM><<<grid, threads, 0, s>>>(a);
+    else if (each <= 2) norm_rows_kernel<2, VEC, NORM><<<grid, threads, 0, s>>>(a);
+    else if (each <= 4) norm_rows_kernel<4, VEC, NORM><<<grid, threads, 0, s>>>(a);
+    else norm_rows_kernel<8, VEC, NORM><<<grid, threads, 0, s>>>(a);
+    return launched();
+}
+
+int check_w4(int K, int N, int group, int gated) {
+    if (K < 1 || N < 1 || (gated != 0 && gated != 1) || (gated && N % 2 != 0)) return MOE_ERR_INVALID_ARG;
+    if (group != 32 && group != 64 && group != 128) return MOE_ERR_UNSUPPORTED;
+    if (K > (1 << 20) || N > (1 << 20)) return MOE_ERR_UNSUPPORTED;
+    return MOE_OK;
+}
+int64_t w4_tiles(int K, int N, int gated) { return w4_tiles_n(N, gated) * w4_tiles_k(K); }
+
+template <int NT, int PER, bool VEC, bool GATED>
+int launch_w4(const W4Args& a, hipStream_t s) {
+    const int waves = a.tiles_k < 16 ? a.tiles_k : 16;
+    const int lds = waves * NT * 256 * (int)sizeof(float);
+    w4_matvec_kernel<NT, PER, VEC, GATED><<<dim3((a.tiles_n + NT - 1) / NT), waves * 64, lds, s>>>(a);
+    return launched();
+}
+template <int PER, bool VEC>
+int launch_w4(const W4Args& a, bool gated, hipStream_t s) {
+    return gated ? launch_w4<2, PER, VEC, true>(a, s) : launch_w4<1, PER, VEC, false>(a, s);
+}
+template <int PER>
+int launch_w4(const W4Args& a, bool gated, bool vec, hipStream_t s) {
+    return vec ? launch_w4<PER, true>(a, gated, s) : launch_w4<PER, false>(a, gated, s);
+}
+
+}  // namespace
+
+extern "C" {
+
+int moe_route_grouped(const void* logits, const float* bias, const moe_route_desc* d, int groups, int kept, int group_score, int32_t* topk_ids,
+                      float* topk_weights, void* stream) {
+    if (!d || d->T < 0 || d->E < 1 || d->k < 1 || d->k > d->E) return MOE_ERR_INVALID_ARG;
+    if (d->score != MOE_SCORE_SOFTMAX && d->score != MOE_SCORE_SIGMOID) return MOE_ERR_INVALID_ARG;
+    if (groups < 1 || d->E % groups != 0 || kept < 1 || kept > groups || (int64_t)d->k > (int64_t)kept * (d->E / groups)) return MOE_ERR_INVALID_ARG;
+    if (group_score != MOE_GROUP_MAX && group_score != MOE_GROUP_TOP2) return MOE_ERR_INVALID_ARG;
+    if (!fp32_or_bf16(d->dtype)) return MOE_ERR_UNSUPPORTED;
+    if (d->E > kMaxE || groups > 64 || (int64_t)d->T * d->k > (1 << 24)) return MOE_ERR_UNSUPPORTED;
+    if (d->T == 0) return MOE_OK;
+    if (!logits || !topk_ids || !topk_weights || (d->T > 1 && d->row_stride < d->E)) return MOE_ERR_INVALID_ARG;
+    if (misaligned(logits, bytes_of(d->dtype)) || misaligned(bias, 4) || misaligned(topk_ids, 4) || misaligned(topk_weights, 4)) return MOE_ERR_INVALID_ARG;
+    const int each = d->E / groups, lanes = 64 / groups;
+    const GroupedRouteArgs a = {logits, bias, d->row_stride, d->T, d->E, d->k, groups, kept, each, lanes, d->score == MOE_SCORE_SIGMOID,
+                                group_score == MOE_GROUP_TOP2, d->renormalize != 0, d->scale};
+    const hipStream_t s = static_cast<hipStream_t>(stream);
+    const bool f32 = d->dtype == MOE_DTYPE_FP32;
+    const int per_lane = (each + lanes - 1) / lanes;
+    if (per_lane <= 1) return launch_grouped<1>(a, f32, topk_ids, topk_weights, s);
+    if (per_lane <= 2) return launch_grouped<2>(a, f32, topk_ids, topk_weights, s);
+    if (per_lane <= 4) return launch_grouped<4>(a, f32, topk_ids, topk_weights, s);
+    if (per_lane <= 8) return launch_grouped<8>(a, f32, topk_ids, topk_weights, s);
+    if (per_lane <= 16) return launch_grouped<16>(a, f32, topk_ids, topk_weights, s);
+    return launch_grouped<32>(a, f32, topk_ids, topk_weights, s);
+}
+
+int moe_add_norm(const void* x, const void* residual, const void* weight, const moe_norm_desc* d, void* residual_out, void* y, void* codes, float* scales,
+                 void* stream) {
+    if (!d || d->rows < 0 || d->cols < 1 || !(d->eps >= 0.f) || d->eps > 3.4028235e38f) return MOE_ERR_INVALID_ARG;
+    if (!fp32_or_bf16(d->x_dtype) || (residual && !fp32_or_bf16(d->residual_dtype)) || (weight && !fp32_or_bf16(d->weight_dtype))) return MOE_ERR_UNSUPPORTED;
+    if (d->cols > kNormCols || d->rows > (1 << 24)) return MOE_ERR_UNSUPPORTED;
+    if (d->rows == 0) return MOE_OK;
+    if ((residual_out && !residual) || (codes && !scales) || (scales && !codes) || (!residual_out && !y && !codes)) return MOE_ERR_INVALID_ARG;
+    if (!x || (d->rows > 1 && (d->x_stride < d->cols || (residual && d->residual_stride < d->cols)))) return MOE_ERR_INVALID_ARG;
+    const int xb = bytes_of(d->x_dtype), rb = bytes_of(d->residual_dtype), wb = bytes_of(d->weight_dtype);
+    if (misaligned(x, xb) || (residual && (misaligned(residual, rb) || misaligned(residual_out, rb))) || (weight && misaligned(weight, wb)) || misaligned(y, 2) ||
+        misaligned(scales, 4)) return MOE_ERR_INVALID_ARG;
+    const int64_t xs = d->rows > 1 ? d->x_stride : 0, rs = d->rows > 1 ? d->residual_stride : 0;
+    const NormArgs a = {x, residual, weight, xs, rs, d->cols, d->x_dtype == MOE_DTYPE_FP32, d->residual_dtype == MOE_DTYPE_FP32, d->weight_dtype == MOE_DTYPE_FP32,
+                        d->eps, residual_out, static_cast<uint16_t*>(y), static_cast<uint8_t*>(codes), scales};
+    bool vec = d->cols % 8 == 0 && !misaligned(x, 16) && xs * xb % 16 == 0 && !misaligned(weight, 16) && !misaligned(y, 16) && !misaligned(codes, 8);
+    if (residual) vec = vec && !misaligned(residual, 16) && rs * rb % 16 == 0 && !misaligned(residual_out, 16);
+    const hipStream_t s = static_cast<hipStream_t>(stream);
+    return vec ? launch_norm_rows<true, true>(a, d->rows, s) : launch_norm_rows<false, true>(a, d->rows, s);
+}
+
+int moe_fp8_quantize(const void* src, int dtype, int64_t rows, int cols, int64_t row_stride, void* codes, float* scales, void* stream) {
+    if (rows < 0 || cols < 1) return MOE_ERR_INVALID_ARG;
+    if (!fp32_or_bf16(dtype) || cols > kNormCols || rows > (1 << 24)) return MOE_ERR_UNSUPPORTED;
+    if (rows == 0) return MOE_OK;
+    const int b = bytes_of(dtype);
+    if (!src || !codes || !scales || misaligned(src, b) || misaligned(scales, 4) || (rows > 1 && row_stride < cols)) return MOE_ERR_INVALID_ARG;
+    if (rows == 1) row_stride = 0;
+    NormArgs a{};
+    a.x = src; a.x_stride = row_stride; a.cols = cols; a.x_f32 = dtype == MOE_DTYPE_FP32;
+    a.codes = static_cast<uint8_t*>(codes); a.scales = scales;
+    const bool vec = cols % 8 == 0 && !misaligned(src, 16) && row_stride * b % 16 == 0 && !misaligned(codes, 8);
+    const hipStream_t s = static_cast<hipStream_t>(stream);
+    return vec ? launch_norm_rows<true, false>(a, rows, s) : launch_norm_rows<false, false>(a, rows, s);
+}
+
+size_t moe_w4_code_bytes(int K, int N, int gated) { return check_w4(K, N, 128, gated) != MOE_OK ? 0 : (size_t)w4_tiles(K, N, gated) * kW4TileBytes; }
+size_t moe_w4_word_bytes(int K, int N, int group, int gated) {
+    return check_w4(K, N, group, gated) != MOE_OK ? 0 : (size_t)w4_tiles(K, N, gated) * (kW4TileK / group) * kW4TileN * 4;
+}
+
+int moe_w4_pack_weights(const uint8_t* q, const void* scales, const uint8_t* zeros, int scale_dtype, int w_layout, int K, int N, int group, int gated, void* codes,
+                        void* words, void* stream) {
+    const int rc = check_w4(K, N, group, gated);
+    if (rc != MOE_OK) return rc;
+    if (w_layout != MOE_W_LAYOUT_KN && w_layout != MOE_W_LAYOUT_NK) return MOE_ERR_INVALID_ARG;
+    if (scale_dtype != MOE_DTYPE_BF16 && scale_dtype != MOE_DTYPE_FP16) return MOE_ERR_UNSUPPORTED;
+    if (!q || !scales || !codes || !words || misaligned(scales, 2) || misaligned(codes, 16) || misaligned(words, 16)) return MOE_ERR_INVALID_ARG;
+    const int64_t tiles = w4_tiles(K, N, gated);
+    const W4PackArgs a = {q, static_cast<const uint16_t*>(scales), zeros, K, N, group, gated, w_layout == MOE_W_LAYOUT_NK, scale_dtype == MOE_DTYPE_FP16,
+                          (int)w4_tiles_k(K), static_cast<uint32_t*>(codes), static_cast<uint32_t*>(words)};
+    if (!work_items_fit((tiles + 3) / 4, 256)) return MOE_ERR_UNSUPPORTED;
+    w4_pack_kernel<<<dim3((unsigned)((tiles + 3) / 4)), 256, 0, static_cast<hipStream_t>(stream)>>>(a, tiles);
+    return launched();
+}
+
+int moe_w4_matvec(const void* X, int64_t x_stride, const void* codes, const void* words, const moe_w4_desc* d, const void* add, void* out, void* stream) {
+    if (!d || d->T < 0) return MOE_ERR_INVALID_ARG;
+    const int rc = check_w4(d->K, d->N, d->group, d->gated);
+    if (rc != MOE_OK) return rc;
+    if (d->T > kW4Tokens) return MOE_ERR_UNSUPPORTED;
+    if (d->T == 0) return MOE_OK;
+    if (!X || !codes || !words || !out || (d->T > 1 && x_stride < d->K)) return MOE_ERR_INVALID_ARG;
+    if (misaligned(X, 2) || misaligned(codes, 16) || misaligned(words, 16) || misaligned(add, 2) || misaligned(out, 2)) return MOE_ERR_INVALID_ARG;
+    if (d->T == 1) x_stride = 0;
+    const W4Args a = {static_cast<const uint16_t*>(X), x_stride, static_cast<const char*>(codes), static_cast<const uint32_t*>(words),
+                      static_cast<const uint16_t*>(add), static_cast<uint16_t*>(out), d->T, d->K, d->N, d->gated ? d->N / 2 : d->N,
+                      (int)w4_tiles_n(d->N, d->gated), (int)w4_tiles_k(d->K)};
+    const bool vec = d->K % 8 == 0 && x_stride % 8 == 0 && !misaligned(X, 16);
+    const hipStream_t s = static_cast<hipStream_t>(stream);
+    if (d->group == 128) return launch_w4<1>(a, d->gated, vec, s);
+    if (d->group == 64) return launch_w4<2>(a, d->gated, vec, s);
+    return launch_w4<4>(a, d->gated, vec, s);
+}
+
+}  // extern "C"

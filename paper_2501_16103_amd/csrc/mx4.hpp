@@ -72,9 +72,6 @@ __device__ __forceinline__ u32x4_t mx4_values8(uint32_t codes, float scale) {
     return o;
 }
 
-__device__ __forceinline__ float mx4_load(const uint16_t* p) { return __uint_as_float((uint32_t)*p << 16); }
-__device__ __forceinline__ float mx4_load(const float* p) { return *p; }
-
 // Token rows.  A lane takes eight elements of a row, four lanes a block: a stream of bytes, 4096 rows of 7168 bf16 with values in 24.8 us, 5.4 TB/s read
 // and written (a large copy: 5.0).  128 rows of 2048 are a launch's latency, 2.6 us back to back.  VEC: rows begin on 16 bytes and are a multiple
 // of eight long, and every lane moves its elements with one or two 16-byte loads.
@@ -107,7 +104,7 @@ __device__ __forceinline__ void mx4_quantize_piece(int64_t c, const Src* __restr
         }
     } else {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = at + i < cols ? mx4_load(p + i) : 0.f;
+        for (int i = 0; i < 8; ++i) v[i] = at + i < cols ? load_value(p + i) : 0.f;
     }
     uint32_t largest = 0;                             // (as integers: a NaN is above every number)
 #pragma unroll
@@ -176,7 +173,7 @@ __global__ __launch_bounds__(256) void mx4_pack_weights(const Src* __restrict__ 
         }
     } else {
 #pragma unroll
-        for (int i = 0; i < kMxBlock; ++i) v[i] = i < have ? mx4_load(p + i * step) : 0.f;
+        for (int i = 0; i < kMxBlock; ++i) v[i] = i < have ? load_value(p + i * step) : 0.f;
     }
 #pragma unroll
     for (int i = 0; i < kMxBlock; ++i) {

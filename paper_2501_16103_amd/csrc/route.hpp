@@ -12,7 +12,7 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
-#include "mx4.hpp"
+#include "values.hpp"
 
 namespace moe {
 
@@ -77,7 +77,7 @@ __device__ __forceinline__ int route_token(const RouteArgs& a, int64_t t, int (&
 #pragma unroll
     for (int j = 0; j < EPL; ++j) {
         expert[j] = EPL * lane + j;
-        logit[j] = mx4_load(row + (expert[j] < a.E ? expert[j] : a.E - 1));
+        logit[j] = load_value(row + (expert[j] < a.E ? expert[j] : a.E - 1));
     }
 #pragma unroll
     for (int j = 0; j < EPL; ++j) key[j] = expert[j] < a.E ? route_key(logit[j]) : 0;

@@ -1,0 +1,125 @@
+"""What the grouped router, the norm, the row quantiser and the 4-bit product refuse.  Addresses are made up: nothing is launched before a check."""
+import ctypes
+
+import pytest
+import torch
+
+from paper_2501_16103_amd import binding as mb
+
+P = 1 << 20          # an aligned address that nobody reads
+OK, INVALID, UNSUPPORTED = mb.MOE_OK, mb.MOE_ERR_INVALID_ARG, mb.MOE_ERR_UNSUPPORTED
+FP32, BF16, FP16, FP8 = mb.MOE_DTYPE_FP32, mb.MOE_DTYPE_BF16, mb.MOE_DTYPE_FP16, mb.MOE_DTYPE_FP8_E4M3
+
+
+def _route(logits=P, bias=P, groups=4, kept=2, group_score=0, ids=P, weights=P, **kw):
+    d = dict(T=4, k=2, E=8, dtype=FP32, row_stride=8, score=0, renormalize=1, scale=1.0)
+    d.update(kw)
+    return mb.lib().moe_route_grouped(logits, bias, ctypes.byref(mb.moe_route_desc(**d)), groups, kept, group_score, ids, weights, None)
+
+
+@pytest.mark.parametrize("kw,rc", [
+    (dict(T=-1), INVALID), (dict(k=0), INVALID), (dict(k=5), INVALID), (dict(k=9), INVALID), (dict(E=0), INVALID), (dict(score=2), INVALID),
+    (dict(groups=0), INVALID), (dict(groups=3), INVALID), (dict(groups=16), INVALID), (dict(kept=0), INVALID), (dict(kept=5), INVALID), (dict(group_score=2), INVALID),
+    (dict(group_score=-1), INVALID), (dict(dtype=FP8), UNSUPPORTED), (dict(dtype=FP16), UNSUPPORTED), (dict(dtype=-1), UNSUPPORTED),
+    (dict(E=1028, row_stride=1028), UNSUPPORTED), (dict(E=130, groups=65, row_stride=130), UNSUPPORTED), (dict(T=1 << 24), UNSUPPORTED), (dict(row_stride=7), INVALID),
+    (dict(logits=None), INVALID), (dict(ids=None), INVALID), (dict(weights=None), INVALID), (dict(logits=P + 2), INVALID), (dict(bias=P + 2), INVALID),
+    (dict(ids=P + 1), INVALID), (dict(weights=P + 2), INVALID), (dict(dtype=BF16, logits=P + 1), INVALID), (dict(T=0, logits=None), OK)])
+def test_route_grouped(kw, rc):
+    assert _route(**kw) == rc
+
+
+def _norm(x=P, residual=P, weight=P, residual_out=P, y=P, codes=P, scales=P, **kw):
+    d = dict(rows=4, x_stride=64, residual_stride=64, cols=64, x_dtype=BF16, residual_dtype=BF16, weight_dtype=BF16, eps=1e-6)
+    d.update(kw)
+    return mb.lib().moe_add_norm(x, residual, weight, ctypes.byref(mb.moe_norm_desc(**d)), residual_out, y, codes, scales, None)
+
+
+@pytest.mark.parametrize("kw,rc", [
+    (dict(rows=-1), INVALID), (dict(cols=0), INVALID), (dict(eps=-1e-6), INVALID), (dict(eps=float("nan")), INVALID), (dict(eps=float("inf")), INVALID),
+    (dict(x_dtype=FP16), UNSUPPORTED), (dict(residual_dtype=FP8), UNSUPPORTED), (dict(weight_dtype=-1), UNSUPPORTED),
+    (dict(cols=65537, x_stride=65537, residual_stride=65537), UNSUPPORTED), (dict(rows=(1 << 24) + 1), UNSUPPORTED), (dict(residual=None), INVALID),
+    (dict(codes=None), INVALID), (dict(scales=None), INVALID), (dict(residual_out=None, y=None, codes=None, scales=None), INVALID), (dict(x=None), INVALID),
+    (dict(x_stride=63), INVALID), (dict(residual_stride=63), INVALID), (dict(x=P + 1), INVALID), (dict(residual=P + 1), INVALID), (dict(residual_out=P + 1), INVALID),
+    (dict(weight=P + 1), INVALID), (dict(y=P + 1), INVALID), (dict(scales=P + 2), INVALID), (dict(x_dtype=FP32, x=P + 2), INVALID),
+    (dict(residual_dtype=FP32, residual=P + 2), INVALID), (dict(weight_dtype=FP32, weight=P + 2), INVALID), (dict(rows=0, x=None), OK)])
+def test_add_norm(kw, rc):
+    assert _norm(**kw) == rc
+
+
+def _quantize(src=P, dtype=BF16, rows=4, cols=100, stride=100, codes=P, scales=P):
+    return mb.lib().moe_fp8_quantize(src, dtype, rows, cols, stride, codes, scales, None)
+
+
+@pytest.mark.parametrize("kw,rc", [
+    (dict(rows=-1), INVALID), (dict(cols=0), INVALID), (dict(stride=99), INVALID), (dict(dtype=FP8), UNSUPPORTED), (dict(dtype=FP16), UNSUPPORTED), (dict(dtype=-1), UNSUPPORTED),
+    (dict(cols=65537, stride=65537), UNSUPPORTED), (dict(rows=(1 << 24) + 1), UNSUPPORTED), (dict(src=None), INVALID), (dict(codes=None), INVALID),
+    (dict(scales=None), INVALID), (dict(scales=P + 2), INVALID), (dict(src=P + 1), INVALID), (dict(dtype=FP32, src=P + 2), INVALID), (dict(rows=0, src=None), OK)])
+def test_quantize(kw, rc):
+    assert _quantize(**kw) == rc
+
+
+def _pack(q=P, scales=P, zeros=P, dtype=BF16, layout=0, K=64, N=32, group=32, gated=0, codes=P, words=P):
+    return mb.lib().moe_w4_pack_weights(q, scales, zeros, dtype, layout, K, N, group, gated, codes, words, None)
+
+
+@pytest.mark.parametrize("kw,rc", [
+    (dict(K=0), INVALID), (dict(N=0), INVALID), (dict(N=31, gated=1), INVALID), (dict(gated=2), INVALID), (dict(layout=2), INVALID), (dict(group=16), UNSUPPORTED),
+    (dict(group=0), UNSUPPORTED), (dict(group=256), UNSUPPORTED), (dict(dtype=FP32), UNSUPPORTED), (dict(dtype=-1), UNSUPPORTED), (dict(K=(1 << 20) + 1), UNSUPPORTED),
+    (dict(N=(1 << 20) + 2), UNSUPPORTED), (dict(q=None), INVALID), (dict(scales=None), INVALID), (dict(scales=P + 1), INVALID), (dict(codes=None), INVALID),
+    (dict(words=None), INVALID), (dict(codes=P + 8), INVALID), (dict(words=P + 4), INVALID)])
+def test_pack(kw, rc):
+    assert _pack(**kw) == rc
+
+
+def _matvec(X=P, stride=64, codes=P, words=P, add=P, out=P, **kw):
+    d = dict(T=4, K=64, N=32, group=32, gated=0)
+    d.update(kw)
+    return mb.lib().moe_w4_matvec(X, stride, codes, words, ctypes.byref(mb.moe_w4_desc(**d)), add, out, None)
+
+
+@pytest.mark.parametrize("kw,rc", [
+    (dict(T=-1), INVALID), (dict(T=17), UNSUPPORTED), (dict(K=0), INVALID), (dict(N=0), INVALID), (dict(N=31, gated=1), INVALID), (dict(gated=-1), INVALID),
+    (dict(group=48), UNSUPPORTED), (dict(K=(1 << 20) + 1, stride=1 << 21), UNSUPPORTED), (dict(X=None), INVALID), (dict(codes=None), INVALID), (dict(words=None), INVALID),
+    (dict(out=None), INVALID), (dict(stride=63), INVALID), (dict(X=P + 1), INVALID), (dict(codes=P + 8), INVALID), (dict(words=P + 8), INVALID), (dict(add=P + 1), INVALID),
+    (dict(out=P + 1), INVALID), (dict(T=0, X=None), OK)])
+def test_matvec(kw, rc):
+    assert _matvec(**kw) == rc
+
+
+def test_null_descriptions():
+    lib = mb.lib()
+    assert lib.moe_route_grouped(P, None, None, 1, 1, 0, P, P, None) == INVALID
+    assert lib.moe_add_norm(P, None, None, None, None, P, None, None, None) == INVALID
+    assert lib.moe_w4_matvec(P, 64, P, P, None, None, P, None) == INVALID
+
+
+def test_sizes():
+    assert mb.moe_w4_code_bytes(128, 16) == 1024 and mb.moe_w4_code_bytes(129, 17) == 4 * 1024
+    assert mb.moe_w4_code_bytes(128, 34, True) == 4 * 1024                      # 17 columns of each half: two tiles each
+    assert mb.moe_w4_word_bytes(128, 16, 32) == 4 * 64 and mb.moe_w4_word_bytes(128, 16, 128) == 64
+    assert mb.moe_w4_code_bytes(0, 16) == mb.moe_w4_word_bytes(128, 16, 48) == mb.moe_w4_code_bytes(128, 15, True) == 0
+    assert mb.moe_w4_code_bytes(1 << 20, 1 << 20) == 1 << 39                    # sizes beyond 32 bits
+
+
+def test_bindings_refuse_what_does_not_fit():
+    """Tensors on the host, of the wrong size, type or layout never reach the library."""
+    t = torch.empty
+    cpu = dict(check=False)
+    ids, w = t(4, 2, dtype=torch.int32), t(4, 2)
+    assert mb.moe_route_grouped(t(4, 8), 2, ids, w, 2, 1, **cpu) == INVALID                     # on the host
+    assert mb.moe_route_grouped(t(4, 8), 2, t(3, 2, dtype=torch.int32), w, 2, 1, **cpu) == INVALID
+    assert mb.moe_route_grouped(t(4, 8), 2, ids, w, 2, 1, bias=t(7), **cpu) == INVALID
+    assert mb.moe_route_grouped(t(4, 8), 2, ids, w, 2, 1, bias=t(8, dtype=torch.bfloat16), **cpu) == INVALID
+    assert mb.moe_add_norm(t(4, 8), None, 1e-6, y=t(4, 8, dtype=torch.bfloat16), **cpu) == INVALID
+    rows = mb.Fp8Rows(4, 8, "cpu")
+    assert mb.moe_fp8_quantize(t(4, 8), rows, **cpu) == INVALID
+    assert mb.moe_fp8_quantize(t(5, 8), rows, **cpu) == INVALID
+    assert mb.moe_fp8_quantize(t(4, 7), rows, **cpu) == INVALID
+    W = mb.W4Weights(64, 32, 32, device="cpu")
+    q, s = t(64, 32, dtype=torch.uint8), t(2, 32, dtype=torch.float16)
+    assert mb.moe_w4_pack_weights(q, s, None, 0, W, **cpu) == INVALID
+    assert mb.moe_w4_matvec(t(4, 64, dtype=torch.bfloat16), W, t(4, 32, dtype=torch.bfloat16), **cpu) == INVALID
+    for make in (lambda: mb.Fp8Rows(-1, 8, "cpu"), lambda: mb.Fp8Rows(4, 0, "cpu"), lambda: mb.W4Weights(64, 31, 32, True, "cpu"), lambda: mb.W4Weights(64, 32, 48, device="cpu"),
+                 lambda: mb.MoeFp8LayerPlan(4, 2, 8, 130, 128, "cpu")):
+        with pytest.raises(mb.MoeError):
+            make()
