@@ -31,18 +31,26 @@ int launch_grouped(const GroupedRouteArgs& a, bool f32, int32_t* ids, float* wei
 
 constexpr int kNormCols = 65536;
 
-template <bool VEC, bool NORM>
+template <class X, class R, class W>
 int launch_norm_rows(const NormArgs& a, int64_t rows, hipStream_t s) {
-    const int chunks = (a.cols + 7) / 8;
-    int threads = (chunks + 63) / 64 * 64;
-    threads = threads < 256 ? threads : chunks <= 2048 ? 256 : 1024;
+    const int pieces = (a.cols + 7) / 8;
+    const int each = pieces <= 256 ? 1 : pieces <= 2048 ? 2 : pieces <= 4096 ? 4 : 8;
+    const int threads = ((pieces + each - 1) / each + 63) / 64 * 64;
     const dim3 grid((unsigned)rows);
-    const int each = (chunks + threads - 1) / threads;
-    if (each <= 1) norm_rows_kernel<1, VEC, NORM><<<grid, threads, 0, s>>>(a);
-    else if (each <= 2) norm_rows_kernel<2, VEC, NORM><<<grid, threads, 0, s>>>(a);
-    else if (each <= 4) norm_rows_kernel<4, VEC, NORM><<<grid, threads, 0, s>>>(a);
-    else norm_rows_kernel<8, VEC, NORM><<<grid, threads, 0, s>>>(a);
+    if (each == 1) norm_rows_kernel<1, 256, X, R, W><<<grid, threads, 0, s>>>(a);
+    else if (each == 2) norm_rows_kernel<2, 1024, X, R, W><<<grid, threads, 0, s>>>(a);
+    else if (each == 4) norm_rows_kernel<4, 1024, X, R, W><<<grid, threads, 0, s>>>(a);
+    else norm_rows_kernel<8, 1024, X, R, W><<<grid, threads, 0, s>>>(a);
     return launched();
+}
+template <class X, class R>
+int launch_norm_rows(const NormArgs& a, bool weight_f32, int64_t rows, hipStream_t s) {
+    return weight_f32 ? launch_norm_rows<X, R, float>(a, rows, s) : launch_norm_rows<X, R, uint16_t>(a, rows, s);
+}
+template <class X>
+int launch_norm_rows(const NormArgs& a, bool residual_f32, bool weight_f32, int64_t rows, hipStream_t s) {
+    if (!a.residual) return launch_norm_rows<X, void>(a, weight_f32, rows, s);
+    return residual_f32 ? launch_norm_rows<X, float>(a, weight_f32, rows, s) : launch_norm_rows<X, uint16_t>(a, weight_f32, rows, s);
 }
 
 int check_w4(int K, int N, int group, int gated) {
@@ -53,20 +61,23 @@ int check_w4(int K, int N, int group, int gated) {
 }
 int64_t w4_tiles(int K, int N, int gated) { return w4_tiles_n(N, gated) * w4_tiles_k(K); }
 
-template <int NT, int PER, bool VEC, bool GATED>
+template <int NT, int TR, int PER, bool GATED>
 int launch_w4(const W4Args& a, hipStream_t s) {
-    const int waves = a.tiles_k < 16 ? a.tiles_k : 16;
-    const int lds = waves * NT * 256 * (int)sizeof(float);
-    w4_matvec_kernel<NT, PER, VEC, GATED><<<dim3((a.tiles_n + NT - 1) / NT), waves * 64, lds, s>>>(a);
+    const int grid = (a.tiles_n + NT - 1) / NT, most = a.tiles_n >= 4 * kCus ? 4 : grid > kCus || NT == 4 ? 8 : 16;
+    int waves = (a.tiles_k + 1) / 2;
+    waves = waves < most ? waves : most;
+    w4_matvec_kernel<NT, TR, PER, GATED><<<dim3(grid), waves * 64, waves * (TR > NT ? TR : NT) * 1024, s>>>(a);
     return launched();
 }
-template <int PER, bool VEC>
+template <int TR, int PER>
 int launch_w4(const W4Args& a, bool gated, hipStream_t s) {
-    return gated ? launch_w4<2, PER, VEC, true>(a, s) : launch_w4<1, PER, VEC, false>(a, s);
+    if (a.tiles_n >= 4 * kCus || (a.T > 8 && a.tiles_n >= 3 * kCus)) return gated ? launch_w4<4, TR, PER, true>(a, s) : launch_w4<4, TR, PER, false>(a, s);
+    if (gated) return launch_w4<2, TR, PER, true>(a, s);
+    return a.tiles_n > kCus + 32 ? launch_w4<2, TR, PER, false>(a, s) : launch_w4<1, TR, PER, false>(a, s);
 }
 template <int PER>
-int launch_w4(const W4Args& a, bool gated, bool vec, hipStream_t s) {
-    return vec ? launch_w4<PER, true>(a, gated, s) : launch_w4<PER, false>(a, gated, s);
+int launch_w4(const W4Args& a, bool gated, hipStream_t s) {
+    return a.T <= 4 ? launch_w4<1, PER>(a, gated, s) : a.T <= 8 ? launch_w4<2, PER>(a, gated, s) : launch_w4<4, PER>(a, gated, s);
 }
 
 }  // namespace
@@ -110,12 +121,10 @@ int moe_add_norm(const void* x, const void* residual, const void* weight, const 
     if (misaligned(x, xb) || (residual && (misaligned(residual, rb) || misaligned(residual_out, rb))) || (weight && misaligned(weight, wb)) || misaligned(y, 2) ||
         misaligned(scales, 4)) return MOE_ERR_INVALID_ARG;
     const int64_t xs = d->rows > 1 ? d->x_stride : 0, rs = d->rows > 1 ? d->residual_stride : 0;
-    const NormArgs a = {x, residual, weight, xs, rs, d->cols, d->x_dtype == MOE_DTYPE_FP32, d->residual_dtype == MOE_DTYPE_FP32, d->weight_dtype == MOE_DTYPE_FP32,
-                        d->eps, residual_out, static_cast<uint16_t*>(y), static_cast<uint8_t*>(codes), scales};
-    bool vec = d->cols % 8 == 0 && !misaligned(x, 16) && xs * xb % 16 == 0 && !misaligned(weight, 16) && !misaligned(y, 16) && !misaligned(codes, 8);
-    if (residual) vec = vec && !misaligned(residual, 16) && rs * rb % 16 == 0 && !misaligned(residual_out, 16);
+    const NormArgs a = {x, residual, weight, xs, rs, d->cols, d->eps, residual_out, static_cast<uint16_t*>(y), static_cast<uint8_t*>(codes), scales};
     const hipStream_t s = static_cast<hipStream_t>(stream);
-    return vec ? launch_norm_rows<true, true>(a, d->rows, s) : launch_norm_rows<false, true>(a, d->rows, s);
+    const bool r32 = d->residual_dtype == MOE_DTYPE_FP32, w32 = d->weight_dtype == MOE_DTYPE_FP32;
+    return d->x_dtype == MOE_DTYPE_FP32 ? launch_norm_rows<float>(a, r32, w32, d->rows, s) : launch_norm_rows<uint16_t>(a, r32, w32, d->rows, s);
 }
 
 int moe_fp8_quantize(const void* src, int dtype, int64_t rows, int cols, int64_t row_stride, void* codes, float* scales, void* stream) {
@@ -126,11 +135,10 @@ int moe_fp8_quantize(const void* src, int dtype, int64_t rows, int cols, int64_t
     if (!src || !codes || !scales || misaligned(src, b) || misaligned(scales, 4) || (rows > 1 && row_stride < cols)) return MOE_ERR_INVALID_ARG;
     if (rows == 1) row_stride = 0;
     NormArgs a{};
-    a.x = src; a.x_stride = row_stride; a.cols = cols; a.x_f32 = dtype == MOE_DTYPE_FP32;
+    a.x = src; a.x_stride = row_stride; a.cols = cols;
     a.codes = static_cast<uint8_t*>(codes); a.scales = scales;
-    const bool vec = cols % 8 == 0 && !misaligned(src, 16) && row_stride * b % 16 == 0 && !misaligned(codes, 8);
     const hipStream_t s = static_cast<hipStream_t>(stream);
-    return vec ? launch_norm_rows<true, false>(a, rows, s) : launch_norm_rows<false, false>(a, rows, s);
+    return dtype == MOE_DTYPE_FP32 ? launch_norm_rows<float, void, void>(a, rows, s) : launch_norm_rows<uint16_t, void, void>(a, rows, s);
 }
 
 size_t moe_w4_code_bytes(int K, int N, int gated) { return check_w4(K, N, 128, gated) != MOE_OK ? 0 : (size_t)w4_tiles(K, N, gated) * kW4TileBytes; }
@@ -147,7 +155,7 @@ int moe_w4_pack_weights(const uint8_t* q, const void* scales, const uint8_t* zer
     if (!q || !scales || !codes || !words || misaligned(scales, 2) || misaligned(codes, 16) || misaligned(words, 16)) return MOE_ERR_INVALID_ARG;
     const int64_t tiles = w4_tiles(K, N, gated);
     const W4PackArgs a = {q, static_cast<const uint16_t*>(scales), zeros, K, N, group, gated, w_layout == MOE_W_LAYOUT_NK, scale_dtype == MOE_DTYPE_FP16,
-                          (int)w4_tiles_k(K), static_cast<uint32_t*>(codes), static_cast<uint32_t*>(words)};
+                          (int)w4_tiles_n(N, gated), static_cast<uint32_t*>(codes), static_cast<uint32_t*>(words)};
     if (!work_items_fit((tiles + 3) / 4, 256)) return MOE_ERR_UNSUPPORTED;
     w4_pack_kernel<<<dim3((unsigned)((tiles + 3) / 4)), 256, 0, static_cast<hipStream_t>(stream)>>>(a, tiles);
     return launched();
@@ -165,11 +173,10 @@ int moe_w4_matvec(const void* X, int64_t x_stride, const void* codes, const void
     const W4Args a = {static_cast<const uint16_t*>(X), x_stride, static_cast<const char*>(codes), static_cast<const uint32_t*>(words),
                       static_cast<const uint16_t*>(add), static_cast<uint16_t*>(out), d->T, d->K, d->N, d->gated ? d->N / 2 : d->N,
                       (int)w4_tiles_n(d->N, d->gated), (int)w4_tiles_k(d->K)};
-    const bool vec = d->K % 8 == 0 && x_stride % 8 == 0 && !misaligned(X, 16);
     const hipStream_t s = static_cast<hipStream_t>(stream);
-    if (d->group == 128) return launch_w4<1>(a, d->gated, vec, s);
-    if (d->group == 64) return launch_w4<2>(a, d->gated, vec, s);
-    return launch_w4<4>(a, d->gated, vec, s);
+    if (d->group == 128) return launch_w4<1>(a, d->gated, s);
+    if (d->group == 64) return launch_w4<2>(a, d->gated, s);
+    return launch_w4<4>(a, d->gated, s);
 }
 
 }  // extern "C"

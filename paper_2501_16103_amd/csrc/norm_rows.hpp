@@ -10,6 +10,9 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include <type_traits>
+
+#include "lane_sums.hpp"
 #include "values.hpp"
 
 namespace moe {
@@ -22,7 +25,6 @@ struct NormArgs {
     const void* weight;          // or null: 1
     int64_t x_stride, residual_stride;
     int cols;
-    int x_f32, residual_f32, weight_f32;
     float eps;
     void* sum;                   // [rows][cols] of the residual's type, or null
     uint16_t* y;                 // [rows][cols], or null
@@ -30,80 +32,102 @@ struct NormArgs {
     float* scales;               // [rows]
 };
 
-// Eight elements of a row as floats.  VEC: consecutive ones, 16-byte aligned; else `step` apart, the same of neighbouring lanes side by side.
-template <bool VEC>
-struct RowPiece {
-    int at, step, cols;
-    __device__ __forceinline__ bool any() const { return at < cols; }
-    __device__ __forceinline__ int index(int i) const { return VEC ? at + i : at + i * step; }
-    __device__ __forceinline__ bool has(int i) const { return VEC ? at < cols : at + i * step < cols; }
-    __device__ __forceinline__ void load(const void* base, int64_t row_at, int f32, float (&v)[8]) const {
-        if constexpr (VEC) {
-            const int64_t p = row_at + (at < cols ? at : 0);
-            if (f32) {
-                const f32x4_t lo = *reinterpret_cast<const f32x4_t*>(static_cast<const float*>(base) + p);
-                const f32x4_t hi = *reinterpret_cast<const f32x4_t*>(static_cast<const float*>(base) + p + 4);
-#pragma unroll
-                for (int i = 0; i < 4; ++i) { v[i] = lo[i]; v[4 + i] = hi[i]; }
-            } else {
-                const u32x4_t w = *reinterpret_cast<const u32x4_t*>(static_cast<const uint16_t*>(base) + p);
-#pragma unroll
-                for (int i = 0; i < 4; ++i) { v[2 * i] = bf16_lo(w[i]); v[2 * i + 1] = bf16_hi(w[i]); }
-            }
-        } else {
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                const int64_t p = row_at + (has(i) ? index(i) : 0);
-                v[i] = f32 ? static_cast<const float*>(base)[p] : load_value(static_cast<const uint16_t*>(base) + p);
-            }
-        }
+// Eight elements as they are stored.
+template <class T>
+struct Eight {
+    u32x4_t v[sizeof(T) / 2];
+    __device__ __forceinline__ float operator[](int i) const {
+        if constexpr (sizeof(T) == 4) return __uint_as_float(v[i >> 2][i & 3]);
+        else return i & 1 ? bf16_hi(v[0][i >> 1]) : bf16_lo(v[0][i >> 1]);
     }
-    __device__ __forceinline__ void store(void* base, int64_t row_at, int f32, const float (&v)[8]) const {
-        if constexpr (VEC) {
-            if (at >= cols) return;
-            if (f32) {
-                float* p = static_cast<float*>(base) + row_at + at;
-                *reinterpret_cast<f32x4_t*>(p) = f32x4_t{v[0], v[1], v[2], v[3]};
-                *reinterpret_cast<f32x4_t*>(p + 4) = f32x4_t{v[4], v[5], v[6], v[7]};
-            } else {
-                u32x4_t o;
+    __device__ __forceinline__ void set(const float (&f)[8]) {
+        if constexpr (sizeof(T) == 4) {
 #pragma unroll
-                for (int i = 0; i < 4; ++i) o[i] = pack_bf16(v[2 * i], v[2 * i + 1]);
-                *reinterpret_cast<u32x4_t*>(static_cast<uint16_t*>(base) + row_at + at) = o;
-            }
+            for (int i = 0; i < 8; ++i) v[i >> 2][i & 3] = __float_as_uint(f[i]);
         } else {
 #pragma unroll
-            for (int i = 0; i < 8; ++i)
-                if (has(i)) {
-                    if (f32) static_cast<float*>(base)[row_at + index(i)] = v[i];
-                    else static_cast<uint16_t*>(base)[row_at + index(i)] = (uint16_t)pack_bf16(v[i], 0.f);
-                }
-        }
-    }
-    __device__ __forceinline__ void store_codes(uint8_t* base, int64_t row_at, const uint32_t (&c)[2]) const {
-        if constexpr (VEC) {
-            if (at < cols) *reinterpret_cast<uint2*>(base + row_at + at) = make_uint2(c[0], c[1]);
-        } else {
-#pragma unroll
-            for (int i = 0; i < 8; ++i)
-                if (has(i)) base[row_at + index(i)] = (uint8_t)(c[i >> 2] >> (8 * (i & 3)));
+            for (int i = 0; i < 4; ++i) v[0][i] = pack_bf16(f[2 * i], f[2 * i + 1]);
         }
     }
 };
 
+// Eight consecutive elements of a row of `cols`, at any alignment; the last piece of a row may be a part of eight.
+struct RowPiece {
+    int at, cols;
+    __device__ __forceinline__ bool has(int i) const { return at + i < cols; }
+    __device__ __forceinline__ bool whole() const { return at + 8 <= cols; }
+    // Whole pieces; of the others the row's first elements are read (a choice here would wait for what was loaded).  cols >= 8.
+    template <class T>
+    __device__ __forceinline__ void load(const void* base, int64_t row_at, Eight<T>& e) const {
+        const T* p = static_cast<const T*>(base) + row_at + (whole() ? at : 0);
+#pragma unroll
+        for (int i = 0; i < (int)sizeof(T) / 2; ++i) e.v[i] = *reinterpret_cast<const u32x4_any_t*>(reinterpret_cast<const char*>(p) + 16 * i);
+    }
+    // A piece that is not whole: its elements one by one, zeros beyond.
+    template <class T>
+    __device__ __forceinline__ void load_part(const void* base, int64_t row_at, Eight<T>& e) const {
+        float f[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            f[i] = 0.f;
+            if (has(i)) f[i] = load_value(static_cast<const T*>(base) + row_at + at + i);
+        }
+        e.set(f);
+    }
+    template <class T>
+    __device__ __forceinline__ void store(void* base, int64_t row_at, const Eight<T>& e) const {
+        T* p = static_cast<T*>(base) + row_at + at;
+        if (whole()) {
+#pragma unroll
+            for (int i = 0; i < (int)sizeof(T) / 2; ++i) *reinterpret_cast<u32x4_any_t*>(reinterpret_cast<char*>(p) + 16 * i) = e.v[i];
+        } else {
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+                if (has(i)) {
+                    if constexpr (sizeof(T) == 4) p[i] = e[i];
+                    else p[i] = (T)(e.v[0][i >> 1] >> (16 * (i & 1)));
+                }
+        }
+    }
+    __device__ __forceinline__ void store_codes(uint8_t* base, int64_t row_at, const uint32_t (&c)[2]) const {
+        if (whole()) {
+            *reinterpret_cast<u32x2_any_t*>(base + row_at + at) = u32x2_t{c[0], c[1]};
+        } else {
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+                if (has(i)) base[row_at + at + i] = (uint8_t)(c[i >> 2] >> (8 * (i & 3)));
+        }
+    }
+};
+
+__device__ __forceinline__ uint32_t magnitude_bits(float v) { return __float_as_uint(v) & 0x7fffffffu; }
+
 // Sum and largest value over the workgroup, in every thread.
-template <class S, class M>
-__device__ __forceinline__ void block_sum_max(S& sum, M& most, int threads) {
-    __shared__ S sums[16];
-    __shared__ M mosts[16];
+__device__ __forceinline__ void block_sum_max(float& sum, uint32_t& most, int threads) {
+    __shared__ float sums[16];
+    __shared__ uint32_t mosts[16];
+    sum = wave_sum(sum);
+    most = wave_max_u32(most);
+    if (threads <= 64) return;
+    const int lane = threadIdx.x & 63, waves = threads >> 6;
+    if (lane == 0) {
+        sums[threadIdx.x >> 6] = sum;
+        mosts[threadIdx.x >> 6] = most;
+    }
+    __syncthreads();
+    sum = wave_sum(lane < waves ? sums[lane & 15] : 0.f);
+    most = wave_max_u32(lane < waves ? mosts[lane & 15] : 0u);
+}
+// The same of 64-bit values (rare: see where it is called).
+__device__ __forceinline__ void block_sum_max(double& sum, double& most, int threads) {
+    __shared__ double sums[16], mosts[16];
     for (int d = 1; d < 64; d <<= 1) {
         sum += __shfl_xor(sum, d);
-        const M o = __shfl_xor(most, d);
+        const double o = __shfl_xor(most, d);
         most = o > most ? o : most;
     }
     if (threads <= 64) return;
     const int waves = threads >> 6, wave = threadIdx.x >> 6;
-    __syncthreads();                                 // (the arrays may hold what a caller before read)
     if ((threadIdx.x & 63) == 0) {
         sums[wave] = sum;
         mosts[wave] = most;
@@ -117,54 +141,60 @@ __device__ __forceinline__ void block_sum_max(S& sum, M& most, int threads) {
     }
 }
 
-__device__ __forceinline__ uint32_t magnitude_bits(float v) { return __float_as_uint(v) & 0x7fffffffu; }
-
-// A workgroup per row, CH pieces of eight elements a thread.
-template <int CH, bool VEC, bool NORM>
-__global__ __launch_bounds__(1024) void norm_rows_kernel(NormArgs a) {
+// A workgroup per row, CH pieces of eight elements a thread, at most THREADS.  R void: no residual.  W void: the rows as they are, codes and scales only.
+template <int CH, int THREADS, class X, class R, class W>
+__global__ __launch_bounds__(THREADS) void norm_rows_kernel(NormArgs a) {
+    constexpr bool NORM = !std::is_void<W>::value, ADD = !std::is_void<R>::value;
+    using H = std::conditional_t<ADD, R, X>;         // what h is held as
+    using Weight = std::conditional_t<NORM, W, X>;
     const int64_t row = blockIdx.x;
     const int threads = blockDim.x;
-    RowPiece<VEC> piece[CH];
-    float h[CH][8], w[CH][8];
+    const int64_t x_at = row * a.x_stride, r_at = row * a.residual_stride;
+    RowPiece piece[CH];
+    Eight<H> h[CH];
+    Eight<Weight> w[CH];
+    {
+        Eight<X> x[CH];
+        Eight<H> r[CH];
 #pragma unroll
-    for (int c = 0; c < CH; ++c) {
-        const int n = c * threads + threadIdx.x;
-        piece[c] = VEC ? RowPiece<VEC>{8 * n, 0, a.cols} : RowPiece<VEC>{8 * c * threads + (int)threadIdx.x, threads, a.cols};
-        piece[c].load(a.x, row * a.x_stride, a.x_f32, h[c]);
-    }
-    if (NORM && a.residual) {
-        float r[CH][8];
+        for (int c = 0; c < CH; ++c) piece[c] = RowPiece{8 * (c * threads + (int)threadIdx.x), a.cols};
+        if (a.cols >= 8) {
 #pragma unroll
-        for (int c = 0; c < CH; ++c) piece[c].load(a.residual, row * a.residual_stride, a.residual_f32, r[c]);
+            for (int c = 0; c < CH; ++c) piece[c].load(a.x, x_at, x[c]);
+            if constexpr (ADD) {
 #pragma unroll
-        for (int c = 0; c < CH; ++c) {
+                for (int c = 0; c < CH; ++c) piece[c].load(a.residual, r_at, r[c]);
+            }
+            if (NORM && a.weight) {
 #pragma unroll
-            for (int i = 0; i < 8; ++i) h[c][i] += r[c][i];
+                for (int c = 0; c < CH; ++c) piece[c].load(a.weight, 0, w[c]);
+            }
         }
-    }
-    if (NORM) {
 #pragma unroll
         for (int c = 0; c < CH; ++c) {
-            if (a.weight) {
-                piece[c].load(a.weight, 0, a.weight_f32, w[c]);
+            if (!piece[c].whole()) {                 // (a part of a row's end, or nothing)
+                piece[c].load_part(a.x, x_at, x[c]);
+                if constexpr (ADD) piece[c].load_part(a.residual, r_at, r[c]);
+                if (NORM && a.weight) piece[c].load_part(a.weight, 0, w[c]);
+            }
+        }
+#pragma unroll
+        for (int c = 0; c < CH; ++c) {
+            if constexpr (ADD) {
+                float f[8];
+#pragma unroll
+                for (int i = 0; i < 8; ++i) f[i] = x[c][i] + r[c][i];
+                h[c].set(f);
+                if (a.sum) piece[c].store(a.sum, row * a.cols, h[c]);
             } else {
-#pragma unroll
-                for (int i = 0; i < 8; ++i) w[c][i] = 1.f;
+                h[c] = x[c];
             }
         }
-        if (a.residual) {
-            if (!a.residual_f32) {
+    }
+    if (NORM && !a.weight) {
+        const float ones[8] = {1.f, 1.f, 1.f, 1.f, 1.f, 1.f, 1.f, 1.f};
 #pragma unroll
-                for (int c = 0; c < CH; ++c) {
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) h[c][i] = bf16_lo(pack_bf16(h[c][i], 0.f));
-                }
-            }
-            if (a.sum) {
-#pragma unroll
-                for (int c = 0; c < CH; ++c) piece[c].store(a.sum, row * a.cols, a.residual_f32, h[c]);
-            }
-        }
+        for (int c = 0; c < CH; ++c) w[c].set(ones);
     }
     float squares = 0.f;
     uint32_t most = 0;
@@ -172,30 +202,27 @@ __global__ __launch_bounds__(1024) void norm_rows_kernel(NormArgs a) {
     for (int c = 0; c < CH; ++c) {
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-            if (!piece[c].has(i)) { h[c][i] = 0.f; continue; }
-            if (NORM) squares = fmaf(h[c][i], h[c][i], squares);
-            const uint32_t m = magnitude_bits(NORM ? h[c][i] * w[c][i] : h[c][i]);
+            const float v = h[c][i];
+            if (NORM) squares = fmaf(v, v, squares);
+            const uint32_t m = magnitude_bits(NORM ? v * w[c][i] : v);
             most = m > most ? m : most;
         }
     }
     block_sum_max(squares, most, threads);
-    float largest = __uint_as_float(most);
-    if (NORM) {
+    float largest = __uint_as_float(most), factor = 1.f;
+    bool wide = false;                               // squares or products that leave fp32: the same in 64 bits
+    double factor64 = 0.;
+    if constexpr (NORM) {
         if (squares >= 1e-25f && squares <= 1e37f && largest <= 1e37f) {
-            const float factor = 1.f / sqrtf(squares / (float)a.cols + a.eps);
+            factor = 1.f / sqrtf(squares / (float)a.cols + a.eps);
             largest *= factor;
-#pragma unroll
-            for (int c = 0; c < CH; ++c) {
-#pragma unroll
-                for (int i = 0; i < 8; ++i) h[c][i] = h[c][i] * factor * w[c][i];
-            }
-        } else {                                     // squares or products that leave fp32: the same in 64 bits
+        } else {
+            wide = true;
             double s = 0., m = 0., not_finite = 0.;
 #pragma unroll
             for (int c = 0; c < CH; ++c) {
 #pragma unroll
                 for (int i = 0; i < 8; ++i) {
-                    if (!piece[c].has(i)) continue;
                     const double v = (double)h[c][i], y = v * (double)w[c][i];
                     s += v * v;
                     m = fabs(y) > m ? fabs(y) : m;
@@ -205,33 +232,39 @@ __global__ __launch_bounds__(1024) void norm_rows_kernel(NormArgs a) {
             if (!(not_finite == 0.)) m = __longlong_as_double(0x7ff0000000000000ll);
             block_sum_max(s, m, threads);
             const double mean = s / a.cols + (double)a.eps;
-            const double factor = mean == 0. ? 0. : 1. / sqrt(mean);   // (a row of zeros with eps 0 stays zeros)
-            largest = s <= 1.7e308 ? (float)(m * factor) : __builtin_inff();
-#pragma unroll
-            for (int c = 0; c < CH; ++c) {
-#pragma unroll
-                for (int i = 0; i < 8; ++i) h[c][i] = (float)((double)h[c][i] * factor * (double)w[c][i]);
-            }
+            factor64 = mean == 0. ? 0. : 1. / sqrt(mean);   // (a row of zeros with eps 0 stays zeros)
+            largest = s <= 1.7e308 ? (float)(m * factor64) : __builtin_inff();
         }
-        if (a.y) {
-#pragma unroll
-            for (int c = 0; c < CH; ++c) piece[c].store(a.y, row * a.cols, 0, h[c]);
-        }
-        if (!a.codes) return;
     }
+    const bool finite = largest <= 3.4028235e38f;
     float scale = largest / kE4m3Max;
     scale = scale < kLeastScale ? kLeastScale : scale;
-    const bool finite = largest <= 3.4028235e38f;
     if (!finite) scale = __uint_as_float(0x7fc00000u);
     const float inverse = 1.f / scale;
 #pragma unroll
     for (int c = 0; c < CH; ++c) {
+        if (piece[c].at >= a.cols) continue;
+        float y[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) y[i] = NORM ? h[c][i] * factor * w[c][i] : h[c][i];
+        if constexpr (NORM) {
+            if (wide) {
+#pragma unroll
+                for (int i = 0; i < 8; ++i) y[i] = (float)((double)h[c][i] * factor64 * (double)w[c][i]);
+            }
+            if (a.y) {
+                Eight<uint16_t> o;
+                o.set(y);
+                piece[c].store(a.y, row * a.cols, o);
+            }
+            if (!a.codes) continue;
+        }
         float q[8];
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
             // y / scale, its rounding taken back by the remainder
-            const float about = h[c][i] * inverse;
-            q[i] = fmaf(fmaf(-about, scale, h[c][i]), inverse, about);
+            const float about = y[i] * inverse;
+            q[i] = fmaf(fmaf(-about, scale, y[i]), inverse, about);
         }
         uint32_t code[2];
 #pragma unroll
@@ -242,7 +275,7 @@ __global__ __launch_bounds__(1024) void norm_rows_kernel(NormArgs a) {
         }
         piece[c].store_codes(a.codes, row * a.cols, code);
     }
-    if (threadIdx.x == 0) a.scales[row] = scale;
+    if (threadIdx.x == 0 && a.codes) a.scales[row] = scale;
 }
 
 }  // namespace moe

@@ -12,6 +12,7 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include "lane_sums.hpp"
 #include "values.hpp"
 
 namespace moe {
@@ -37,29 +38,6 @@ constexpr uint32_t kRouteMasked = 0x007fffffu;                 // the key of -in
 __device__ __forceinline__ float route_logit(uint32_t key) {   // the logit a key stands for
     if (key == 0xffffffffu) return __uint_as_float(0x7fc00000u);
     return __uint_as_float(key & 0x80000000u ? key & 0x7fffffffu : ~key);
-}
-
-// Largest of the 64 lanes' values, in every lane.  Within the lanes' own registers: the same by shuffles is six round trips through
-// the LDS crossbar, and the choice of k experts is a chain of k + 1 of these.
-__device__ __forceinline__ uint32_t wave_max_u32(uint32_t v) {
-    auto step = [&](uint32_t o) __attribute__((always_inline)) { v = o > v ? o : v; };
-    step(__builtin_amdgcn_update_dpp(0, v, 0x111, 0xf, 0xf, false));   // row_shr:1
-    step(__builtin_amdgcn_update_dpp(0, v, 0x112, 0xf, 0xf, false));   // row_shr:2
-    step(__builtin_amdgcn_update_dpp(0, v, 0x114, 0xf, 0xf, false));   // row_shr:4
-    step(__builtin_amdgcn_update_dpp(0, v, 0x118, 0xf, 0xf, false));   // row_shr:8
-    step(__builtin_amdgcn_update_dpp(0, v, 0x142, 0xa, 0xf, false));   // row_bcast:15 into rows 1 and 3
-    step(__builtin_amdgcn_update_dpp(0, v, 0x143, 0xc, 0xf, false));   // row_bcast:31 into rows 2 and 3
-    return (uint32_t)__builtin_amdgcn_readlane((int)v, 63);
-}
-__device__ __forceinline__ float wave_sum(float v) {
-    auto step = [&](int o) __attribute__((always_inline)) { v += __int_as_float(o); };
-    step(__builtin_amdgcn_update_dpp(0, __float_as_int(v), 0x111, 0xf, 0xf, false));
-    step(__builtin_amdgcn_update_dpp(0, __float_as_int(v), 0x112, 0xf, 0xf, false));
-    step(__builtin_amdgcn_update_dpp(0, __float_as_int(v), 0x114, 0xf, 0xf, false));
-    step(__builtin_amdgcn_update_dpp(0, __float_as_int(v), 0x118, 0xf, 0xf, false));
-    step(__builtin_amdgcn_update_dpp(0, __float_as_int(v), 0x142, 0xa, 0xf, false));
-    step(__builtin_amdgcn_update_dpp(0, __float_as_int(v), 0x143, 0xc, 0xf, false));
-    return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v), 63));
 }
 
 // One token by one wavefront.  EPL: logits per lane, experts EPL * lane + 0 .. EPL - 1.  The i-th choice comes back in slot i / 64 of

@@ -14,6 +14,10 @@ typedef __attribute__((ext_vector_type(8))) short s16x8_t;
 typedef __attribute__((ext_vector_type(2))) int i32x2_t;
 typedef __attribute__((ext_vector_type(4))) unsigned int u32x4_t;
 typedef __attribute__((ext_vector_type(2))) unsigned int u32x2_t;
+// The same at any address: one access as well (the target takes unaligned ones), slower where it crosses a line.
+typedef u32x4_t __attribute__((aligned(1))) u32x4_any_t;
+typedef u32x2_t __attribute__((aligned(1))) u32x2_any_t;
+typedef f32x4_t __attribute__((aligned(1))) f32x4_any_t;
 
 __device__ __forceinline__ uint32_t pack_bf16(float a, float b) {
     bf16x2_t p = {(__bf16)a, (__bf16)b};  // hardware round-to-nearest-even

@@ -3,9 +3,9 @@
 //     out[t][n] = (add[t][n] +) sum_k X[t][k] (q[k][n] - z[g][n]) s[g][n],   g = k / group;   gated: silu(gate) * up of the two halves of N
 //
 // Packed form, tiles of 16 columns x 128 k in one piece, columns and k padded with zeros to whole tiles:
-//   codes   [tiles of columns][tiles of k][64][16 bytes]  lane 16 g + c of a tile holds column c; its word i the eight codes k = 32 i + 8 g ..
+//   codes   [tiles of k][tiles of columns][64][16 bytes]  lane 16 g + c of a tile holds column c; its word i the eight codes k = 32 i + 8 g ..
 //                                                         + 7, the even ones in the low half: nibble p < 4 is k 2 p, nibble 4 + p is k 2 p + 1
-//   words   [tiles of columns][tiles of k][128 / group][16]  the fp32 bits of the scale (bf16 or fp16, exact), the zero point in the four lowest
+//   words   [tiles of k][tiles of columns][128 / group][16]  the fp32 bits of the scale (bf16 or fp16, exact), the zero point in the four lowest
 // `gated`: tiles alternate 16 gate columns and the 16 up columns of the same outputs.
 //
 // A word's codes become bf16 without conversions: 0x4300 | q is 128 + q, two of them by one and-or.  What that adds is taken out as the sum's start:
@@ -39,7 +39,7 @@ struct W4PackArgs {
     const uint16_t* scales;      // [groups][N], or [N][groups]
     const uint8_t* zeros;        // the same, or null: 8
     int K, N, group, gated, nk, f16;
-    int tiles_k;
+    int tiles_n;
     uint32_t* codes;
     uint32_t* words;
 };
@@ -49,8 +49,7 @@ __global__ __launch_bounds__(256) void w4_pack_kernel(W4PackArgs a, int64_t tile
     const int64_t tile = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
     if (tile >= tiles) return;
     const int lane = __lane_id(), c = lane & 15, g = lane >> 4;
-    const int64_t tn = tile / a.tiles_k;
-    const int tk = (int)(tile - tn * a.tiles_k), n = w4_column(tn, c, a.N, a.gated);
+    const int tk = (int)(tile / a.tiles_n), n = w4_column(tile - (int64_t)tk * a.tiles_n, c, a.N, a.gated);
     u32x4_t out = {0u, 0u, 0u, 0u};
     for (int i = 0; i < 4; ++i) {
         uint32_t w = 0;
@@ -86,80 +85,127 @@ struct W4Args {
 };
 
 
-// The tokens' side of a step of 32 k: lane 16 g + t holds k = 8 g .. 8 g + 7 of token t.  Zeros beyond K; tokens beyond T repeat the last one.
-template <bool VEC>
-__device__ __forceinline__ u32x4_t w4_tokens(const uint16_t* row, int k, int K) {
+// Elements k .. k + 7 of a token's row of K, of which not all are there: zeros beyond.
+__device__ __forceinline__ u32x4_t w4_last_tokens(const uint16_t* row, int k, int K) {
     u32x4_t v = {0u, 0u, 0u, 0u};
-    if constexpr (VEC) {
-        if (k < K) v = *reinterpret_cast<const u32x4_t*>(row + k);
-    } else {
 #pragma unroll
-        for (int i = 0; i < 8; ++i)
-            if (k + i < K) v[i >> 1] |= (uint32_t)row[k + i] << (16 * (i & 1));
-    }
+    for (int i = 0; i < 8; ++i)
+        if (k + i < K) v[i >> 1] |= (uint32_t)row[k + i] << (16 * (i & 1));
     return v;
 }
 
-// A workgroup per NT tiles of columns; its wavefronts take the tiles along K in turn and add their sums up through LDS.
-// PER: groups of a tile along K.  VEC: token rows are 16-byte aligned and a multiple of eight long.
-template <int NT, int PER, bool VEC, bool GATED>
-__global__ __launch_bounds__(1024) void w4_matvec_kernel(W4Args a) {
-    extern __shared__ float partial[];               // [wavefronts][NT][4][64]
-    const int lane = __lane_id(), wave = threadIdx.x >> 6, waves = blockDim.x >> 6;
+// A workgroup per NT tiles of columns; its wavefronts take the tiles along K in turn, each asked for before the one in front of it is waited for, and
+// add their sums up through LDS.  TR: four tokens each.  PER: groups of a tile along K.
+//
+// Tokens are read as stretches of 256 bytes, four rows a load, and turned into the matrix operand's order (lane 16 g + t: k = 8 g .. of token t) by a
+// trip through the wavefront's own 1 KB of LDS for each: read straight into that order, a load touches sixteen rows, half a line of each.
+template <int NT, int TR, int PER, bool GATED>
+__global__ __launch_bounds__(NT == 4 ? 512 : 1024) void w4_matvec_kernel(W4Args a) {
+    constexpr int OWN = (TR > NT ? TR : NT) * 1024;  // a wavefront's LDS: tokens, then its sums
+    extern __shared__ char lds[];
+    const int lane = __lane_id(), wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), waves = blockDim.x >> 6;
     const int first = blockIdx.x * NT;
-    const int token = (lane & 15) < a.T ? lane & 15 : a.T - 1;
-    const uint16_t* row = a.x + token * a.x_stride;
+    char* own = lds + wave * OWN;
+    // loading: 16 bytes `lane & 15` of row 4 n + (lane >> 4); they go to piece (lane & 15) ^ row, so that reads of 16 rows meet all banks
+    const int piece = lane & 15;
+    const uint16_t *row[TR], *whole[TR];             // (whole: where 16 bytes can be read, a row of fewer than eight elements has none)
+    int put[TR];
+#pragma unroll
+    for (int n = 0; n < TR; ++n) {
+        const int r = 4 * n + (lane >> 4);
+        row[n] = a.x + (r < a.T ? r : a.T - 1) * a.x_stride;
+        whole[n] = a.K >= 8 ? row[n] : reinterpret_cast<const uint16_t*>(a.codes);
+        put[n] = r * 256 + (piece ^ r) * 16;
+    }
+    const int mine = TR == 4 ? lane & 15 : (lane & 15) < 4 * TR ? lane & 15 : 4 * TR - 1;   // (tokens beyond are dropped)
     f32x4_t acc[NT];
 #pragma unroll
     for (int j = 0; j < NT; ++j) acc[j] = f32x4_t{0.f, 0.f, 0.f, 0.f};
     const u32x4_t ones_bits = {0x3f803f80u, 0x3f803f80u, 0x3f803f80u, 0x3f803f80u};
     const bf16x8_t ones = __builtin_bit_cast(bf16x8_t, ones_bits);
-    for (int tk = wave; tk < a.tiles_k; tk += waves) {
-        u32x4_t code[NT], xv[4];
+    uint32_t codes_mask = 0x000f000fu, magic = 0x43004300u;
+    asm("" : "+s"(codes_mask), "+v"(magic));          // (in registers: one and-or instead of two instructions with literals)
+    const bool tail = a.K % kW4TileK != 0;
+    struct Step {
+        u32x4_t code[NT], x[TR];
         uint32_t word[NT][PER];
+    };
+    auto load = [&](int tk) __attribute__((always_inline)) {
+        Step s;
 #pragma unroll
         for (int j = 0; j < NT; ++j) {
             const int tn = first + j < a.tiles_n ? first + j : a.tiles_n - 1;
-            const int64_t tile = (int64_t)tn * a.tiles_k + tk;
-            code[j] = *reinterpret_cast<const u32x4_t*>(a.codes + tile * kW4TileBytes + lane * 16);
+            const int64_t tile = (int64_t)tk * a.tiles_n + tn;
+            s.code[j] = *reinterpret_cast<const u32x4_t*>(a.codes + tile * kW4TileBytes + lane * 16);
 #pragma unroll
-            for (int p = 0; p < PER; ++p) word[j][p] = a.words[(tile * PER + p) * kW4TileN + (lane & 15)];
+            for (int p = 0; p < PER; ++p) s.word[j][p] = a.words[(tile * PER + p) * kW4TileN + (lane & 15)];
         }
 #pragma unroll
-        for (int i = 0; i < 4; ++i) xv[i] = w4_tokens<VEC>(row, tk * kW4TileK + 32 * i + 8 * (lane >> 4), a.K);
+        for (int n = 0; n < TR; ++n) {
+            const int k = tk * kW4TileK + 8 * piece;     // (pieces that are not all there are read again where they are used: a choice here would wait)
+            s.x[n] = *reinterpret_cast<const u32x4_any_t*>(whole[n] + (k + 8 <= a.K ? k : 0));
+        }
+        return s;
+    };
+    auto multiply = [&](const Step& s, int tk) __attribute__((always_inline)) {
+        bf16x8_t x[4];
+#pragma unroll
+        for (int n = 0; n < TR; ++n) *reinterpret_cast<u32x4_t*>(own + put[n]) = s.x[n];
+        if (tail && tk == a.tiles_k - 1) {
+            const int k = tk * kW4TileK + 8 * piece;
+#pragma unroll
+            for (int n = 0; n < TR; ++n)
+                if (k + 8 > a.K) *reinterpret_cast<u32x4_t*>(own + put[n]) = w4_last_tokens(row[n], k, a.K);
+        }
+        __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+        __builtin_amdgcn_wave_barrier();
+        __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+#pragma unroll
+        for (int i = 0; i < 4; ++i) x[i] = *reinterpret_cast<const bf16x8_t*>(own + mine * 256 + ((4 * i + (lane >> 4)) ^ mine) * 16);
+        __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+        __builtin_amdgcn_wave_barrier();
 #pragma unroll
         for (int p = 0; p < PER; ++p) {
             f32x4_t sum = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-            for (int i = p * 4 / PER; i < (p + 1) * 4 / PER; ++i)
-                sum = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, xv[i]), ones, sum, 0, 0, 0);
+            for (int i = p * 4 / PER; i < (p + 1) * 4 / PER; ++i) sum = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x[i], ones, sum, 0, 0, 0);
 #pragma unroll
             for (int j = 0; j < NT; ++j) {
-                const float start = -128.f - (float)(word[j][p] & 15u), scale = __uint_as_float(word[j][p] & ~15u);
+                const float start = -128.f - (float)(s.word[j][p] & 15u), scale = __uint_as_float(s.word[j][p] & ~15u);
                 f32x4_t d = sum * start;
 #pragma unroll
                 for (int i = p * 4 / PER; i < (p + 1) * 4 / PER; ++i) {
                     u32x4_t w;
 #pragma unroll
-                    for (int s = 0; s < 4; ++s) w[s] = (code[j][i] >> (4 * s) & 0x000f000fu) | 0x43004300u;
-                    d = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, xv[i]), __builtin_bit_cast(bf16x8_t, w), d, 0, 0, 0);
+                    for (int q = 0; q < 4; ++q) w[q] = (s.code[j][i] >> (4 * q) & codes_mask) | magic;
+                    d = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x[i], __builtin_bit_cast(bf16x8_t, w), d, 0, 0, 0);
                 }
 #pragma unroll
                 for (int r = 0; r < 4; ++r) acc[j][r] = fmaf(d[r], scale, acc[j][r]);
             }
         }
+    };
+    int tk = wave;                                   // (a workgroup has no more wavefronts than there are tiles along K)
+    Step now = load(tk);
+    for (; tk + waves < a.tiles_k; tk += waves) {
+        const Step next = load(tk + waves);
+        __builtin_amdgcn_sched_barrier(0);
+        multiply(now, tk);
+        now = next;
     }
+    multiply(now, tk);
+    float* partial = reinterpret_cast<float*>(lds);  // [wavefront: OWN bytes][NT][4][64]
 #pragma unroll
     for (int j = 0; j < NT; ++j) {
 #pragma unroll
-        for (int r = 0; r < 4; ++r) partial[((wave * NT + j) * 4 + r) * 64 + lane] = acc[j][r];
+        for (int r = 0; r < 4; ++r) partial[wave * (OWN / 4) + (j * 4 + r) * 64 + lane] = acc[j][r];
     }
     __syncthreads();
     // element (token 4 g + r, column c) of a tile is register r of lane 16 g + c
     auto total = [&](int j, int t, int c) __attribute__((always_inline)) {
         const int at = (j * 4 + (t & 3)) * 64 + 16 * (t >> 2) + c;
         float v = 0.f;
-        for (int w = 0; w < waves; ++w) v += partial[w * NT * 256 + at];
+        for (int w = 0; w < waves; ++w) v += partial[w * (OWN / 4) + at];
         return v;
     };
     constexpr int OUT = GATED ? NT / 2 : NT;         // tiles of outputs
