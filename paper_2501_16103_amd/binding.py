@@ -814,32 +814,35 @@ class MoeFewTokensPlan:
         return self.out, self.ids, self.weights
 
 
+_current_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
+
+
+def _stream_at(device: int) -> int:
+    return _raw_stream(device) if _raw_stream is not None else torch.cuda.current_stream(device).cuda_stream
+
+
 def _here(*tensors) -> bool:
     """Whether a launch on the current device's stream may touch all of these (None is no tensor)."""
-    device = -1
-    for t in tensors:
-        if t is not None:
-            at = t.get_device()
-            if at < 0 or (device >= 0 and at != device):
-                return False
-            device = at
-    return device < 0 or device == torch.cuda.current_device()
+    at = {t.get_device() for t in tensors if t is not None}
+    return not at or (len(at) == 1 and min(at) >= 0 and min(at) == _current_device())
 
 
+# (The calls of a token's step look at devices in place: what they cost is their host side.)
 def moe_route_grouped(logits: torch.Tensor, k: int, topk_ids: torch.Tensor, topk_weights: torch.Tensor, groups: int, kept: int,
                       group_score: int = MOE_GROUP_MAX, bias: Optional[torch.Tensor] = None, score: int = MOE_SCORE_SOFTMAX, renormalize: bool = True,
                       scale: float = 1.0, check: bool = True) -> int:
     """moe_route among the experts of the `kept` best of `groups` groups, by score + bias (fp32 [E])."""
     T, E = logits.shape
     row, step = logits.stride()
-    n = T * k
+    n, at = T * k, logits.get_device()
     rc = MOE_ERR_INVALID_ARG
     if (topk_ids.numel() >= n and topk_weights.numel() >= n and topk_ids.dtype is torch.int32 and topk_weights.dtype is torch.float32 and
-            topk_ids.is_contiguous() and topk_weights.is_contiguous() and (step == 1 or E <= 1) and _holds(bias, E, torch.float32) and
-            _here(logits, topk_ids, topk_weights, bias)):
+            topk_ids.is_contiguous() and topk_weights.is_contiguous() and (step == 1 or E <= 1) and
+            (bias is None or (_holds(bias, E, torch.float32) and bias.get_device() == at)) and
+            topk_ids.get_device() == at and topk_weights.get_device() == at and at >= 0 and at == _current_device()):
         d = moe_route_desc(T, k, E, _DTYPES.get(logits.dtype, -1), row, score, renormalize, scale)
-        rc = lib().moe_route_grouped(logits.data_ptr(), _ptr(bias), ctypes.byref(d), groups, kept, group_score, topk_ids.data_ptr(),
-                                     topk_weights.data_ptr(), _stream())
+        rc = lib().moe_route_grouped(logits.data_ptr(), None if bias is None else bias.data_ptr(), ctypes.byref(d), groups, kept, group_score,
+                                     topk_ids.data_ptr(), topk_weights.data_ptr(), _stream_at(at))
     if check and rc != MOE_OK:
         raise MoeError(rc, "moe_route_grouped")
     return rc
@@ -865,9 +868,10 @@ def moe_fp8_quantize(src: torch.Tensor, out: Fp8Rows, check: bool = True) -> int
     """Rows of src [rows, cols] -> out's first rows."""
     rows, cols = src.shape
     row, step = src.stride()
+    at = src.get_device()
     rc = MOE_ERR_INVALID_ARG
-    if rows <= out.rows and cols == out.cols and (step == 1 or cols <= 1) and _here(src, out.codes):
-        rc = lib().moe_fp8_quantize(src.data_ptr(), _DTYPES.get(src.dtype, -1), rows, cols, row, out.codes.data_ptr(), out.scales.data_ptr(), _stream())
+    if rows <= out.rows and cols == out.cols and (step == 1 or cols <= 1) and at >= 0 and out.codes.get_device() == at and at == _current_device():
+        rc = lib().moe_fp8_quantize(src.data_ptr(), _DTYPES.get(src.dtype, -1), rows, cols, row, out.codes.data_ptr(), out.scales.data_ptr(), _stream_at(at))
     if check and rc != MOE_OK:
         raise MoeError(rc, "moe_fp8_quantize")
     return rc
@@ -877,21 +881,33 @@ def moe_add_norm(x: torch.Tensor, weight: Optional[torch.Tensor], eps: float, re
                  residual_out: Optional[torch.Tensor] = None, y: Optional[torch.Tensor] = None, rows: Optional[Fp8Rows] = None, check: bool = True) -> int:
     """x + residual -> residual_out; its root-mean-square norm times weight -> y (bf16), rows (e4m3 with scales), or both.  x and residual
     [T, H] with rows of consecutive elements, outputs contiguous."""
-    T, H = x.shape
+    T, H = shape = x.shape
     x_row, x_step = x.stride()
-    fits = (x_step == 1 or H <= 1) and _here(x, weight, residual, residual_out, y, None if rows is None else rows.codes)
-    fits = fits and (weight is None or (weight.shape == (H,) and weight.is_contiguous())) and _holds(y, T * H, torch.bfloat16)
-    r_row, r_type = 0, MOE_DTYPE_FP32
+    n, at = T * H, x.get_device()
+    fits = (x_step == 1 or H <= 1) and at >= 0 and at == _current_device()
+    x_type = w_type = r_type = _DTYPES.get(x.dtype, -1)
+    r_row, w, r, r_out, y_at, codes, scales = 0, None, None, None, None, None, None
+    if weight is not None:
+        fits = fits and weight.numel() == H and weight.dim() == 1 and weight.is_contiguous() and weight.get_device() == at
+        w, w_type = weight.data_ptr(), _DTYPES.get(weight.dtype, -1)
     if residual is not None:
-        fits = fits and residual.shape == x.shape and (residual.stride(1) == 1 or H <= 1) and _holds(residual_out, T * H, residual.dtype)
-        r_row, r_type = residual.stride(0), _DTYPES.get(residual.dtype, -1)
+        r_row, r_step = residual.stride()
+        fits = fits and residual.shape == shape and (r_step == 1 or H <= 1) and residual.get_device() == at
+        r, r_type = residual.data_ptr(), _DTYPES.get(residual.dtype, -1)
+    if residual_out is not None:
+        fits = (fits and residual is not None and residual_out.dtype is residual.dtype and residual_out.numel() >= n and residual_out.is_contiguous() and
+                residual_out.get_device() == at)
+        r_out = residual_out.data_ptr()
+    if y is not None:
+        fits = fits and y.dtype is torch.bfloat16 and y.numel() >= n and y.is_contiguous() and y.get_device() == at
+        y_at = y.data_ptr()
     if rows is not None:
-        fits = fits and T <= rows.rows and rows.cols == H
+        fits = fits and T <= rows.rows and rows.cols == H and rows.codes.get_device() == at
+        codes, scales = rows.codes.data_ptr(), rows.scales.data_ptr()
     rc = MOE_ERR_INVALID_ARG
     if fits:
-        d = moe_norm_desc(T, x_row, r_row, H, _DTYPES.get(x.dtype, -1), r_type, MOE_DTYPE_FP32 if weight is None else _DTYPES.get(weight.dtype, -1), eps)
-        rc = lib().moe_add_norm(x.data_ptr(), _ptr(residual), _ptr(weight), ctypes.byref(d), _ptr(residual_out), _ptr(y),
-                                None if rows is None else rows.codes.data_ptr(), None if rows is None else rows.scales.data_ptr(), _stream())
+        d = moe_norm_desc(T, x_row, r_row, H, x_type, r_type, w_type, eps)
+        rc = lib().moe_add_norm(x.data_ptr(), r, w, ctypes.byref(d), r_out, y_at, codes, scales, _stream_at(at))
     if check and rc != MOE_OK:
         raise MoeError(rc, "moe_add_norm")
     return rc
@@ -946,12 +962,15 @@ def moe_w4_matvec(X: torch.Tensor, W: W4Weights, out: torch.Tensor, add: Optiona
     """X bf16 [T, W.K], T <= 16, rows of consecutive elements -> out bf16 [T, W.N, or W.N / 2 of gated weights], with `add` (of its shape) added."""
     T, K = X.shape
     row, step = X.stride()
-    n = T * (W.N // 2 if W.gated else W.N)
+    gated, at = W.gated, X.get_device()
+    n = T * (W.N // 2 if gated else W.N)
     rc = MOE_ERR_INVALID_ARG
     if (K == W.K and X.dtype is torch.bfloat16 and (step == 1 or K <= 1) and out.dtype is torch.bfloat16 and out.numel() >= n and out.is_contiguous() and
-            _holds(add, n, torch.bfloat16) and _here(X, W.codes, out, add)):
-        d = moe_w4_desc(T, K, W.N, W.group, W.gated)
-        rc = lib().moe_w4_matvec(X.data_ptr(), row, W.codes.data_ptr(), W.words.data_ptr(), ctypes.byref(d), _ptr(add), out.data_ptr(), _stream())
+            (add is None or (_holds(add, n, torch.bfloat16) and add.get_device() == at)) and
+            W.codes.get_device() == at and out.get_device() == at and at >= 0 and at == _current_device()):
+        d = moe_w4_desc(T, K, W.N, W.group, gated)
+        rc = lib().moe_w4_matvec(X.data_ptr(), row, W.codes.data_ptr(), W.words.data_ptr(), ctypes.byref(d), None if add is None else add.data_ptr(),
+                                 out.data_ptr(), _stream_at(at))
     if check and rc != MOE_OK:
         raise MoeError(rc, "moe_w4_matvec")
     return rc

@@ -66,52 +66,26 @@ __device__ __forceinline__ double route_probability(float l, bool sigmoid, float
     return exp((double)l - (double)top) * scale;
 }
 
-// A wavefront per token, four tokens a workgroup.  A group takes `lanes` neighbouring lanes of EPL consecutive experts each, so that lanes and
-// experts rise together.  The i-th choice comes back in slot i / 64 of lane i % 64.
-template <int EPL, class Src>
-__global__ __launch_bounds__(256) void route_grouped_kernel(GroupedRouteArgs a, int32_t* __restrict__ ids, float* __restrict__ weights) {
-    const int64_t t = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
-    if (t >= a.T) return;
-    const int lane = __lane_id();
-    const int group = lane / a.lanes, within = lane - group * a.lanes;
-    const Src* row = static_cast<const Src*>(a.logits) + t * a.row_stride;
-    float logit[EPL], bias[EPL];
-    int expert[EPL];
+// A lane's experts: `lanes` neighbouring lanes hold a group, EPL consecutive experts each, so that lanes and experts rise together.
+template <int EPL>
+struct GroupedRow {
+    int group, first;            // first: its first expert; -1: none
+    int count;                   // experts that are there
+    float logit[EPL], bias[EPL]; // (some other expert's where there is none)
+    uint32_t live;               // bit j: expert first + j is not masked
+    float top;                   // largest logit that is not masked
+};
+
+// The choice in 64 bits.  A round looks at all of a lane's experts: nothing is kept in order, for this is the rare way.
+template <int EPL>
+__device__ __forceinline__ void choose_exactly(const GroupedRouteArgs& a, const GroupedRow<EPL>& r, double per_total, int (&id)[EPL]) {
+    const int lane = __lane_id(), within = lane - r.group * a.lanes;
     uint64_t key[EPL];
 #pragma unroll
     for (int j = 0; j < EPL; ++j) {
-        const int i = within * EPL + j;
-        expert[j] = group < a.groups && i < a.each ? group * a.each + i : -1;
-        const int e = expert[j] < 0 ? 0 : expert[j];
-        logit[j] = load_value(row + e);
-        bias[j] = a.bias ? a.bias[e] : 0.f;
-    }
-    uint32_t first = 0;
-#pragma unroll
-    for (int j = 0; j < EPL; ++j) {
-        const bool masked = expert[j] < 0 || logit[j] == -__builtin_inff() || bias[j] == -__builtin_inff();
-        key[j] = expert[j] < 0 ? 0 : masked ? kScoreMasked : 2;
-        const uint32_t r = masked ? 0 : route_key(logit[j]);
-        first = r > first ? r : first;
-    }
-    first = wave_max_u32(first);                     // (0: every expert is masked, and no probability is asked for)
-    const float top = route_logit(first);
-    double per_total = 0.;
-    if (!a.sigmoid) {
-        double p[EPL], total = 0.;
-#pragma unroll
-        for (int j = 0; j < EPL; ++j) {
-            p[j] = key[j] > kScoreMasked ? route_probability(logit[j], false, top, 1.) : 0.;
-            total += p[j];
-        }
-        per_total = 1. / wave_sum_f64(total);
-#pragma unroll
-        for (int j = 0; j < EPL; ++j)
-            if (key[j] > kScoreMasked) key[j] = score_key(p[j] * per_total + (double)bias[j]);
-    } else {
-#pragma unroll
-        for (int j = 0; j < EPL; ++j)
-            if (key[j] > kScoreMasked) key[j] = score_key(route_probability(logit[j], true, 0.f, 1.) + (double)bias[j]);
+        const bool there = j < r.count, live = r.live >> j & 1;
+        key[j] = !there ? 0 : !live ? kScoreMasked : score_key(route_probability(r.logit[j], a.sigmoid, r.top, per_total) + (double)r.bias[j]);
+        if (EPL > 4) __builtin_amdgcn_sched_barrier(0);   // (one exponential after the other: side by side they take all registers)
     }
     if (a.kept < a.groups) {
         uint64_t one = 0, two = 0;                   // the two largest scores of this lane, then of its group
@@ -129,78 +103,249 @@ __global__ __launch_bounds__(256) void route_grouped_kernel(GroupedRouteArgs a, 
             if (within < width && within + width < a.lanes) { merge(o1); merge(o2); }
         }
         if (a.top2 && two > kScoreMasked && one > kScoreMasked) one = score_key(score_of_key(one) + score_of_key(two));
-        const uint64_t mine = shfl_u64(one, group < a.groups ? group * a.lanes : 0);
+        const uint64_t mine = shfl_u64(one, r.group < a.groups ? r.group * a.lanes : 0);
         int above = 0;
         for (int g = 0; g < a.groups; ++g) {
             const uint32_t lo = (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)one, g * a.lanes);
             const uint32_t hi = (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)(one >> 32), g * a.lanes);
             const uint64_t other = (uint64_t)hi << 32 | lo;
-            above += other > mine || (other == mine && g < group);
+            above += other > mine || (other == mine && g < r.group);
         }
         if (above >= a.kept) {
 #pragma unroll
             for (int j = 0; j < EPL; ++j) key[j] = 0;
         }
     }
-    // A lane's experts in falling order (insertion, an element moves up past strictly smaller ones only).
-    uint32_t order[EPL];
+    uint32_t taken = 0;
 #pragma unroll
-    for (int j = 0; j < EPL; ++j) order[j] = key[j] > kScoreMasked ? route_key(logit[j]) : 0;
+    for (int s = 0; s < EPL; ++s) {
+        id[s] = 0;
+        const int end = a.k - 64 * s < 64 ? a.k - 64 * s : 64;
+        for (int i = 0; i < end; ++i) {
+            uint64_t best = 0;                       // this lane's first of the largest scores, of those the largest logits
+            uint32_t order = 0;
+            int at = 0;
+#pragma unroll
+            for (int j = 0; j < EPL; ++j) {
+                const uint64_t k = taken >> j & 1 ? 0 : key[j];
+                const uint32_t o = k > kScoreMasked ? route_key(r.logit[j]) : 0;
+                const bool more = k > best || (k == best && o > order);
+                best = more ? k : best;
+                order = more ? o : order;
+                at = more ? j : at;
+            }
+            const uint32_t hi = (uint32_t)(best >> 32), most = wave_max_u32(hi);
+            bool mine = hi == most;
+            uint64_t who = __ballot(mine);
+            if (who & (who - 1)) {                   // several lanes: by the lower half, then by the logit, then the first
+                const uint32_t lo = mine ? (uint32_t)best : 0, most_lo = wave_max_u32(lo);
+                mine = mine && lo == most_lo;
+                const uint32_t o = mine ? order : 0, most_o = wave_max_u32(o);
+                who = __ballot(mine && o == most_o);
+            }
+            const int owner = __builtin_ctzll(who);
+            const int e = __builtin_amdgcn_readlane(r.first + at, owner);
+            if (lane == i) id[s] = e;
+            if (lane == owner) taken |= 1u << at;
+        }
+    }
+}
+
+// Order of fp32 scores as unsigned integers (numbers only).
+__device__ __forceinline__ uint32_t score_key32(float s) {
+    const uint32_t b = __float_as_uint(s);
+    return b & 0x80000000u ? ~b : b | 0x80000000u;
+}
+__device__ __forceinline__ float score_of_key32(uint32_t key) { return __uint_as_float(key & 0x80000000u ? key & 0x7fffffffu : ~key); }
+
+// The choice in 32 bits, where that shows that 64 would choose the same: every two neighbours in the order, the first one left out, and the groups on
+// either side of the border differ by more than their errors.  False: it does not show it.
+//
+// Errors, in parts of `size`, the row's largest p + |bias|: a fast exponential is off by 2^-22 of itself and 2^-24 of its argument x, and |x| e^-|x| is below 0.4
+// (a softmax, whose largest term is 1) or at most 7 times the largest p (a sigmoid, as long as that or a bias is 2^-10; smaller ones are left to 64 bits): 2^-20.
+// A softmax's sum, its terms' errors and 20 additions, and the quotient: 7 * 2^-22.  s is rounded by 2^-24.  Together 1.1 * 2^-19 a score, 2.2 * 2^-19 a difference
+// of two and 4.6 * 2^-19 one of two sums of two.
+template <int EPL>
+__device__ __forceinline__ bool choose_quickly(const GroupedRouteArgs& a, const GroupedRow<EPL>& r, int (&id)[EPL]) {
+    const int lane = __lane_id(), within = lane - r.group * a.lanes;
+    uint32_t key[EPL];
+    int expert[EPL];
+    float p[EPL], per_total = 1.f, size = 0.f;
+    if (a.sigmoid) {
+#pragma unroll
+        for (int j = 0; j < EPL; ++j) p[j] = __builtin_amdgcn_rcpf(1.f + __expf(-r.logit[j]));
+    } else {
+        float total = 0.f;
+#pragma unroll
+        for (int j = 0; j < EPL; ++j) {
+            p[j] = r.live >> j & 1 ? __expf(r.logit[j] - r.top) : 0.f;
+            total += p[j];
+        }
+        per_total = __builtin_amdgcn_rcpf(wave_sum(total));
+    }
+    bool number = true;
+#pragma unroll
+    for (int j = 0; j < EPL; ++j) {
+        const bool live = r.live >> j & 1;
+        const float s = fmaf(p[j], per_total, r.bias[j]), c = live ? fmaf(p[j], per_total, fabsf(r.bias[j])) : 0.f;
+        number = number && c <= 1e30f;               // (false for a NaN)
+        size = c > size ? c : size;
+        key[j] = j >= r.count ? 0 : live ? score_key32(s) : 1;
+        expert[j] = r.first + j;
+    }
+    size = __uint_as_float(wave_max_u32(__float_as_uint(size)));
+    if (__ballot(!number) || size < 0x1p-10f) return false;
+    const float apart = size * 0x1p-17f, groups_apart = size * 0x1p-16f;
+    // a lane's experts in falling order (insertion, an element moves up past strictly smaller ones only)
 #pragma unroll
     for (int j = 1; j < EPL; ++j) {
 #pragma unroll
         for (int i = j; i > 0; --i) {
-            const bool up = key[i] > key[i - 1] || (key[i] == key[i - 1] && order[i] > order[i - 1]);
-            const uint64_t kh = up ? key[i] : key[i - 1], kl = up ? key[i - 1] : key[i];
-            const uint32_t oh = up ? order[i] : order[i - 1], ol = up ? order[i - 1] : order[i];
+            const bool up = key[i] > key[i - 1];
+            const uint32_t kh = up ? key[i] : key[i - 1], kl = up ? key[i - 1] : key[i];
             const int eh = up ? expert[i] : expert[i - 1], el = up ? expert[i - 1] : expert[i];
             key[i - 1] = kh; key[i] = kl;
-            order[i - 1] = oh; order[i] = ol;
             expert[i - 1] = eh; expert[i] = el;
         }
     }
-    int id[EPL];
-    uint32_t chosen[EPL];                            // the order of a choice's logit, 0 of a masked one
+    if (a.kept < a.groups) {
+        uint32_t one = key[0], two = EPL > 1 ? key[EPL > 1] : 0;
+        auto merge = [&](uint32_t o1, uint32_t o2) __attribute__((always_inline)) {
+            const uint32_t low = o1 < one ? o1 : one, more = o2 > two ? o2 : two;
+            one = o1 > one ? o1 : one;
+            two = low > more ? low : more;
+        };
+        uint32_t mine;
+        auto group_score = [&]() __attribute__((always_inline)) {
+            return a.top2 && two > 1 ? score_key32(score_of_key32(one) + score_of_key32(two)) : one;
+        };
+        if (a.lanes <= 16 && (a.lanes & (a.lanes - 1)) == 0) {
+            // exchanges within 2, 4, 8 and 16 lanes; every lane of a group ends with its score
+#define MOE_EXCHANGE(ctrl) merge((uint32_t)__builtin_amdgcn_update_dpp(0, (int)one, ctrl, 0xf, 0xf, false), (uint32_t)__builtin_amdgcn_update_dpp(0, (int)two, ctrl, 0xf, 0xf, false))
+            if (a.lanes > 1) MOE_EXCHANGE(0xb1);     // quad_perm 1, 0, 3, 2
+            if (a.lanes > 2) MOE_EXCHANGE(0x4e);     // quad_perm 2, 3, 0, 1
+            if (a.lanes > 4) MOE_EXCHANGE(0x141);    // row_half_mirror
+            if (a.lanes > 8) MOE_EXCHANGE(0x140);    // row_mirror
+#undef MOE_EXCHANGE
+            mine = group_score();
+        } else {
+            int width = 32;
+            while (width >= a.lanes) width >>= 1;
+            for (; width > 0; width >>= 1) {
+                const uint32_t o1 = (uint32_t)__shfl((int)one, lane + width), o2 = (uint32_t)__shfl((int)two, lane + width);
+                if (within < width && within + width < a.lanes) merge(o1, o2);
+            }
+            mine = (uint32_t)__shfl((int)group_score(), r.group < a.groups ? r.group * a.lanes : 0);
+        }
+        int above = 0;
+        for (int g = 0; g < a.groups; ++g) above += (uint32_t)__builtin_amdgcn_readlane((int)mine, g * a.lanes) > mine;
+        const bool there = r.group < a.groups, stays = above < a.kept;
+        // (equal scores: all of them stay, or none does, and the numbers below do not add up)
+        const uint32_t least = ~wave_max_u32(there && stays ? ~mine : 0), most = wave_max_u32(there && !stays ? mine : 0);
+        const int staying = __popcll(__ballot(there && stays && within == 0));
+        if (staying != a.kept || (most > 1 && !(score_of_key32(least) - score_of_key32(most) > groups_apart))) return false;
+        if (!stays) {
 #pragma unroll
-    for (int s = 0; s < EPL; ++s) {
-        id[s] = 0;
-        chosen[s] = 0;
-        const int end = a.k - 64 * s < 64 ? a.k - 64 * s : 64;
-        for (int i = 0; i < end; ++i) {
-            const uint32_t hi = (uint32_t)(key[0] >> 32);
-            const uint32_t most = wave_max_u32(hi);
-            bool best = hi == most;
-            uint64_t who = __ballot(best);
-            if (who & (who - 1)) {                   // several lanes: by the lower half, then by the logit, then the first
-                const uint32_t lo = best ? (uint32_t)key[0] : 0, most_lo = wave_max_u32(lo);
-                best = best && lo == most_lo;
-                const uint32_t o = best ? order[0] : 0, most_o = wave_max_u32(o);
-                who = __ballot(best && o == most_o);
-            }
-            const int owner = __builtin_ctzll(who);
-            const int e = __builtin_amdgcn_readlane(expert[0], owner);
-            const uint32_t l = (uint32_t)__builtin_amdgcn_readlane((int)order[0], owner);
-            if (lane == i) {
-                id[s] = e;
-                chosen[s] = l;
-            }
-            if (lane == owner) {
-#pragma unroll
-                for (int j = 0; j + 1 < EPL; ++j) {
-                    key[j] = key[j + 1];
-                    order[j] = order[j + 1];
-                    expert[j] = expert[j + 1];
-                }
-                key[EPL - 1] = 0;
-            }
+            for (int j = 0; j < EPL; ++j) key[j] = 0;
         }
     }
+    uint32_t now = wave_max_u32(key[0]), chosen = 0;
+    id[0] = 0;
+    for (int i = 0; i < a.k; ++i) {
+        const int owner = __builtin_ctzll(__ballot(key[0] == now));
+        const int e = __builtin_amdgcn_readlane(expert[0], owner);
+        if (lane == i) {
+            id[0] = e;
+            chosen = now;
+        }
+        if (lane == owner) {
+#pragma unroll
+            for (int j = 0; j + 1 < EPL; ++j) {
+                key[j] = key[j + 1];
+                expert[j] = expert[j + 1];
+            }
+            key[EPL - 1] = 0;
+        }
+        now = wave_max_u32(key[0]);
+    }
+    if (lane == a.k) chosen = now;
+    // masked ones (1) come last and in order of their experts, nothing (0) comes behind them
+    const uint32_t before = (uint32_t)__shfl((int)chosen, lane > 0 ? lane - 1 : 0);
+    const bool told = lane == 0 || lane > a.k || chosen <= 1 || score_of_key32(before) - score_of_key32(chosen) > apart;
+    return __ballot(!told) == 0;
+}
+
+// A wavefront per token, four tokens a workgroup.  The i-th choice comes back in slot i / 64 of lane i % 64.
+template <int EPL, class Src>
+__global__ __launch_bounds__(256) void route_grouped_kernel(GroupedRouteArgs a, int32_t* __restrict__ ids, float* __restrict__ weights) {
+    const int64_t t = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+    if (t >= a.T) return;
+    const int lane = __lane_id();
+    const Src* row = static_cast<const Src*>(a.logits) + t * a.row_stride;
+    GroupedRow<EPL> r;
+    r.group = lane / a.lanes;
+    const int from = (lane - r.group * a.lanes) * EPL;
+    r.first = r.group * a.each + from;
+    r.count = r.group < a.groups && from < a.each ? (a.each - from < EPL ? a.each - from : EPL) : 0;
+    uint32_t first = 0;
+    r.live = 0;
+#pragma unroll
+    for (int j = 0; j < EPL; ++j) r.logit[j] = load_value(row + (j < r.count ? r.first + j : 0));
+    if (a.bias) {
+#pragma unroll
+        for (int j = 0; j < EPL; ++j) r.bias[j] = a.bias[j < r.count ? r.first + j : 0];
+    } else {
+#pragma unroll
+        for (int j = 0; j < EPL; ++j) r.bias[j] = 0.f;
+    }
+#pragma unroll
+    for (int j = 0; j < EPL; ++j) {
+        const bool live = (j < r.count) & (r.logit[j] != -__builtin_inff()) & (r.bias[j] != -__builtin_inff());
+        r.live |= live ? 1u << j : 0u;
+        const uint32_t key = live ? route_key(r.logit[j]) : 0;
+        first = key > first ? key : first;
+    }
+    // (a sigmoid needs no top; 0: every expert is masked, and no probability is asked for)
+    r.top = a.sigmoid ? 0.f : route_logit(wave_max_u32(first));
+    double per_total = 0.;
+    bool summed = false;
+    auto sum_up = [&]() __attribute__((always_inline)) {
+        if (a.sigmoid || summed) return;
+        double total = 0.;
+#pragma unroll
+        for (int j = 0; j < EPL; ++j) {
+            total += r.live >> j & 1 ? route_probability(r.logit[j], false, r.top, 1.) : 0.;
+            if (EPL > 4) __builtin_amdgcn_sched_barrier(0);
+        }
+        per_total = 1. / wave_sum_f64(total);
+        summed = true;
+    };
+    int id[EPL];
+    bool done = __ballot(r.live != 0) == 0;          // (a padding row: the first k, of the first groups)
+    if (done) {
+#pragma unroll
+        for (int s = 0; s < EPL; ++s) id[s] = 64 * s + lane;
+    }
+    if constexpr (EPL <= 16) {
+        if (!done && a.k < 64) done = choose_quickly<EPL>(a, r, id);
+    }
+    if (!done) {
+        sum_up();
+        choose_exactly<EPL>(a, r, per_total, id);
+    }
+    // Renormalised weights are quotients in which a softmax's sum drops out.
+    if (!a.renormalize) sum_up();
+    else if (!summed) per_total = 1.;
     double w[EPL], sum = 0.;
 #pragma unroll
     for (int s = 0; s < EPL; ++s) {
         w[s] = 0.;
-        if (64 * s < a.k) w[s] = 64 * s + lane < a.k && chosen[s] ? route_probability(route_logit(chosen[s]), a.sigmoid, top, per_total) : 0.;
-        sum += w[s];
+        const int i = 64 * s + lane;
+        if (i < a.k) {
+            const float l = load_value(row + id[s]), bias = a.bias ? a.bias[id[s]] : 0.f;
+            if (l != -__builtin_inff() && bias != -__builtin_inff()) w[s] = route_probability(l, a.sigmoid, r.top, per_total);
+        }
+        if (64 * s < a.k) sum += w[s];
     }
     if (a.renormalize) sum = wave_sum_f64(sum);
 #pragma unroll
