@@ -151,6 +151,22 @@ __device__ __forceinline__ void choose_exactly(const GroupedRouteArgs& a, const 
     }
 }
 
+// EPL consecutive elements.
+template <int EPL>
+__device__ __forceinline__ void load_lane(const float* p, float (&v)[EPL]) {
+    typedef float vec __attribute__((ext_vector_type(EPL), aligned(4)));
+    const vec w = *reinterpret_cast<const vec*>(p);
+#pragma unroll
+    for (int j = 0; j < EPL; ++j) v[j] = w[j];
+}
+template <int EPL>
+__device__ __forceinline__ void load_lane(const uint16_t* p, float (&v)[EPL]) {
+    typedef uint16_t vec __attribute__((ext_vector_type(EPL), aligned(2)));
+    const vec w = *reinterpret_cast<const vec*>(p);
+#pragma unroll
+    for (int j = 0; j < EPL; ++j) v[j] = __uint_as_float((uint32_t)w[j] << 16);
+}
+
 // Order of fp32 scores as unsigned integers (numbers only).
 __device__ __forceinline__ uint32_t score_key32(float s) {
     const uint32_t b = __float_as_uint(s);
@@ -158,44 +174,63 @@ __device__ __forceinline__ uint32_t score_key32(float s) {
 }
 __device__ __forceinline__ float score_of_key32(uint32_t key) { return __uint_as_float(key & 0x80000000u ? key & 0x7fffffffu : ~key); }
 
-// The choice in 32 bits, where that shows that 64 would choose the same: every two neighbours in the order, the first one left out, and the groups on
-// either side of the border differ by more than their errors.  False: it does not show it.
+// e^x of x <= 0, off by 3 * 2^-24 of itself: x / ln 2 with what its rounding leaves out.  (Below -200 all are 0; a NaN stays one.)
+__device__ __forceinline__ float exp_closely(float x) {
+    x = x < -200.f ? -200.f : x;
+    const float t = x * 1.44269502f, rest = fmaf(x, 1.44269502f, -t) + x * 1.92596303e-8f;
+    const float e = __builtin_amdgcn_exp2f(t);
+    return fmaf(e * 0.693147182f, rest, e);
+}
+// 1 / x of a normal x >= 1, off by 2^-24 of itself and a hair.
+__device__ __forceinline__ float inverse_closely(float x) {
+    const float r = __builtin_amdgcn_rcpf(x);
+    return fmaf(fmaf(-x, r, 1.f), r, r);
+}
+
+// What the choice in 32 bits shows of the one in 64.
+enum { kChosen, kSetChosen, kNotChosen };
+
+// The choice in 32 bits.  kChosen: every two neighbours in its order, the first one left out, and the groups on either side of the border differ by more
+// than their errors, so 64 bits choose the same.  kSetChosen: the first k and the one behind them (in lane k) are the first k + 1, in some order.
 //
-// Errors, in parts of `size`, the row's largest p + |bias|: a fast exponential is off by 2^-22 of itself and 2^-24 of its argument x, and |x| e^-|x| is below 0.4
-// (a softmax, whose largest term is 1) or at most 7 times the largest p (a sigmoid, as long as that or a bias is 2^-10; smaller ones are left to 64 bits): 2^-20.
-// A softmax's sum, its terms' errors and 20 additions, and the quotient: 7 * 2^-22.  s is rounded by 2^-24.  Together 1.1 * 2^-19 a score, 2.2 * 2^-19 a difference
-// of two and 4.6 * 2^-19 one of two sums of two.
+// Errors, in parts of `size`, the row's largest p + |bias|, and units of 2^-24.  sigmoid: e^-|l| 3 of itself, which p moves with; 1 + e 1; the inverse 1.1; the
+// product 1; s 1: less than 8 a score.  softmax: l - top is off by 1 of itself and moves e by 0.4 at most, e 3; the sum of terms 3 and (on average over their
+// shares, at most ln 1024) 7 off, and its EPL + 6 additions; the inverse 1.1; s 1: less than 22 + EPL.  `apart`: two scores'; sums of two scores: twice that and their
+// own roundings.
 template <int EPL>
-__device__ __forceinline__ bool choose_quickly(const GroupedRouteArgs& a, const GroupedRow<EPL>& r, int (&id)[EPL]) {
+__device__ __forceinline__ int choose_quickly(const GroupedRouteArgs& a, const GroupedRow<EPL>& r, int (&id)[EPL]) {
     const int lane = __lane_id(), within = lane - r.group * a.lanes;
     uint32_t key[EPL];
     int expert[EPL];
     float p[EPL], per_total = 1.f, size = 0.f;
     if (a.sigmoid) {
 #pragma unroll
-        for (int j = 0; j < EPL; ++j) p[j] = __builtin_amdgcn_rcpf(1.f + __expf(-r.logit[j]));
+        for (int j = 0; j < EPL; ++j) {
+            const float e = exp_closely(-fabsf(r.logit[j])), inverse = inverse_closely(1.f + e);
+            p[j] = r.logit[j] < 0.f ? e * inverse : inverse;
+        }
     } else {
         float total = 0.f;
 #pragma unroll
         for (int j = 0; j < EPL; ++j) {
-            p[j] = r.live >> j & 1 ? __expf(r.logit[j] - r.top) : 0.f;
+            p[j] = r.live >> j & 1 ? exp_closely(r.logit[j] - r.top) : 0.f;
             total += p[j];
         }
-        per_total = __builtin_amdgcn_rcpf(wave_sum(total));
+        per_total = inverse_closely(wave_sum(total));
     }
     bool number = true;
 #pragma unroll
     for (int j = 0; j < EPL; ++j) {
         const bool live = r.live >> j & 1;
         const float s = fmaf(p[j], per_total, r.bias[j]), c = live ? fmaf(p[j], per_total, fabsf(r.bias[j])) : 0.f;
-        number = number && c <= 1e30f;               // (false for a NaN)
+        number = number & (c <= 1e30f);              // (false for a NaN)
         size = c > size ? c : size;
         key[j] = j >= r.count ? 0 : live ? score_key32(s) : 1;
         expert[j] = r.first + j;
     }
     size = __uint_as_float(wave_max_u32(__float_as_uint(size)));
-    if (__ballot(!number) || size < 0x1p-10f) return false;
-    const float apart = size * 0x1p-17f, groups_apart = size * 0x1p-16f;
+    if (__ballot(!number) || size < 0x1p-100f) return kNotChosen;
+    const float apart = size * (a.sigmoid ? 16.f : 2.f * (22 + EPL)) * 0x1p-24f, groups_apart = 2.5f * apart;
     // a lane's experts in falling order (insertion, an element moves up past strictly smaller ones only)
 #pragma unroll
     for (int j = 1; j < EPL; ++j) {
@@ -243,7 +278,7 @@ __device__ __forceinline__ bool choose_quickly(const GroupedRouteArgs& a, const 
         // (equal scores: all of them stay, or none does, and the numbers below do not add up)
         const uint32_t least = ~wave_max_u32(there && stays ? ~mine : 0), most = wave_max_u32(there && !stays ? mine : 0);
         const int staying = __popcll(__ballot(there && stays && within == 0));
-        if (staying != a.kept || (most > 1 && !(score_of_key32(least) - score_of_key32(most) > groups_apart))) return false;
+        if (staying != a.kept || (most > 1 && !(score_of_key32(least) - score_of_key32(most) > groups_apart))) return kNotChosen;
         if (!stays) {
 #pragma unroll
             for (int j = 0; j < EPL; ++j) key[j] = 0;
@@ -251,7 +286,7 @@ __device__ __forceinline__ bool choose_quickly(const GroupedRouteArgs& a, const 
     }
     uint32_t now = wave_max_u32(key[0]), chosen = 0;
     id[0] = 0;
-    for (int i = 0; i < a.k; ++i) {
+    auto take = [&](int i) __attribute__((always_inline)) {
         const int owner = __builtin_ctzll(__ballot(key[0] == now));
         const int e = __builtin_amdgcn_readlane(expert[0], owner);
         if (lane == i) {
@@ -267,12 +302,38 @@ __device__ __forceinline__ bool choose_quickly(const GroupedRouteArgs& a, const 
             key[EPL - 1] = 0;
         }
         now = wave_max_u32(key[0]);
-    }
+    };
+    for (int i = 0; i < a.k; ++i) take(i);
     if (lane == a.k) chosen = now;
     // masked ones (1) come last and in order of their experts, nothing (0) comes behind them
     const uint32_t before = (uint32_t)__shfl((int)chosen, lane > 0 ? lane - 1 : 0);
     const bool told = lane == 0 || lane > a.k || chosen <= 1 || score_of_key32(before) - score_of_key32(chosen) > apart;
-    return __ballot(!told) == 0;
+    if (__ballot(!told) == 0) return kChosen;
+    if (now > 1) {
+        const float last = score_of_key32(now);
+        take(a.k);
+        if (now > 1 && !(last - score_of_key32(now) > apart)) return kNotChosen;
+    } else if (lane == a.k) {
+        id[0] = -1;                                  // nobody: a masked expert is no rival
+    }
+    return kSetChosen;
+}
+
+// The order of the experts of lanes 0 .. k (-1: none) by their scores in 64 bits; they change places between the lanes.
+__device__ __forceinline__ int put_in_order(const GroupedRouteArgs& a, int id, float logit, float bias, float top, double per_total) {
+    const int lane = __lane_id();
+    const bool live = lane <= a.k && id >= 0 && logit != -__builtin_inff() && bias != -__builtin_inff();
+    const uint64_t key = live ? score_key(route_probability(logit, a.sigmoid, top, per_total) + (double)bias) : lane <= a.k && id >= 0 ? kScoreMasked : 0;
+    const uint32_t order = live ? route_key(logit) : 0;
+    int rank = 0;
+    for (int i = 0; i <= a.k; ++i) {
+        const uint32_t lo = (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)key, i), hi = (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)(key >> 32), i);
+        const uint32_t o = (uint32_t)__builtin_amdgcn_readlane((int)order, i);
+        const int e = __builtin_amdgcn_readlane(id, i);
+        const uint64_t other = (uint64_t)hi << 32 | lo;
+        rank += other > key || (other == key && (o > order || (o == order && e < id)));
+    }
+    return __builtin_amdgcn_ds_permute(4 * (lane <= a.k ? rank : lane), id);
 }
 
 // A wavefront per token, four tokens a workgroup.  The i-th choice comes back in slot i / 64 of lane i % 64.
@@ -287,26 +348,37 @@ __global__ __launch_bounds__(256) void route_grouped_kernel(GroupedRouteArgs a, 
     const int from = (lane - r.group * a.lanes) * EPL;
     r.first = r.group * a.each + from;
     r.count = r.group < a.groups && from < a.each ? (a.each - from < EPL ? a.each - from : EPL) : 0;
-    uint32_t first = 0;
-    r.live = 0;
-#pragma unroll
-    for (int j = 0; j < EPL; ++j) r.logit[j] = load_value(row + (j < r.count ? r.first + j : 0));
-    if (a.bias) {
-#pragma unroll
-        for (int j = 0; j < EPL; ++j) r.bias[j] = a.bias[j < r.count ? r.first + j : 0];
+    if (a.each % EPL == 0) {              // a lane has all of its experts, or none: one access (at any alignment) for all of them
+        load_lane(row + (r.count ? r.first : 0), r.logit);
+        if (a.bias) load_lane(a.bias + (r.count ? r.first : 0), r.bias);
     } else {
+#pragma unroll
+        for (int j = 0; j < EPL; ++j) r.logit[j] = load_value(row + (j < r.count ? r.first + j : 0));
+        if (a.bias) {
+#pragma unroll
+            for (int j = 0; j < EPL; ++j) r.bias[j] = a.bias[j < r.count ? r.first + j : 0];
+        }
+    }
+    if (!a.bias) {
 #pragma unroll
         for (int j = 0; j < EPL; ++j) r.bias[j] = 0.f;
     }
+    r.live = 0;
 #pragma unroll
     for (int j = 0; j < EPL; ++j) {
         const bool live = (j < r.count) & (r.logit[j] != -__builtin_inff()) & (r.bias[j] != -__builtin_inff());
         r.live |= live ? 1u << j : 0u;
-        const uint32_t key = live ? route_key(r.logit[j]) : 0;
-        first = key > first ? key : first;
     }
-    // (a sigmoid needs no top; 0: every expert is masked, and no probability is asked for)
-    r.top = a.sigmoid ? 0.f : route_logit(wave_max_u32(first));
+    r.top = 0.f;                                     // (of a softmax only; NaN where every expert is masked, and no probability is asked for)
+    if (!a.sigmoid) {
+        uint32_t first = 0;
+#pragma unroll
+        for (int j = 0; j < EPL; ++j) {
+            const uint32_t key = r.live >> j & 1 ? route_key(r.logit[j]) : 0;
+            first = key > first ? key : first;
+        }
+        r.top = route_logit(wave_max_u32(first));
+    }
     double per_total = 0.;
     bool summed = false;
     auto sum_up = [&]() __attribute__((always_inline)) {
@@ -327,7 +399,15 @@ __global__ __launch_bounds__(256) void route_grouped_kernel(GroupedRouteArgs a, 
         for (int s = 0; s < EPL; ++s) id[s] = 64 * s + lane;
     }
     if constexpr (EPL <= 16) {
-        if (!done && a.k < 64) done = choose_quickly<EPL>(a, r, id);
+        if (!done && a.k < 63) {
+            const int seen = choose_quickly<EPL>(a, r, id);
+            done = seen != kNotChosen;
+            if (seen == kSetChosen) {
+                sum_up();
+                const int e = id[0] < 0 || lane > a.k ? 0 : id[0];
+                id[0] = put_in_order(a, id[0], load_value(row + e), a.bias ? a.bias[e] : 0.f, r.top, per_total);
+            }
+        }
     }
     if (!done) {
         sum_up();
@@ -340,12 +420,14 @@ __global__ __launch_bounds__(256) void route_grouped_kernel(GroupedRouteArgs a, 
 #pragma unroll
     for (int s = 0; s < EPL; ++s) {
         w[s] = 0.;
-        const int i = 64 * s + lane;
-        if (i < a.k) {
-            const float l = load_value(row + id[s]), bias = a.bias ? a.bias[id[s]] : 0.f;
-            if (l != -__builtin_inff() && bias != -__builtin_inff()) w[s] = route_probability(l, a.sigmoid, r.top, per_total);
+        if (64 * s < a.k) {
+            const int i = 64 * s + lane, e = i < a.k ? id[s] : 0;
+            const float l = load_value(row + e), bias = a.bias ? a.bias[e] : 0.f;
+            const double p = route_probability(l, a.sigmoid, r.top, per_total);
+            w[s] = (i < a.k) & (l != -__builtin_inff()) & (bias != -__builtin_inff()) ? p : 0.;
+            sum += w[s];
         }
-        if (64 * s < a.k) sum += w[s];
+        if (EPL > 4) __builtin_amdgcn_sched_barrier(0);
     }
     if (a.renormalize) sum = wave_sum_f64(sum);
 #pragma unroll
