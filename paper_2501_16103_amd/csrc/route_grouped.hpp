@@ -76,9 +76,10 @@ struct GroupedRow {
     float top;                   // largest logit that is not masked
 };
 
-// The choice in 64 bits.  A round looks at all of a lane's experts: nothing is kept in order, for this is the rare way.
+// The choice in 64 bits.  A round looks at all of a lane's experts: nothing is kept in order, for this is the rare way.  The first 64 choices go to `id` of
+// their lanes, the others to `ids` by the lane that reads them again.
 template <int EPL>
-__device__ __forceinline__ void choose_exactly(const GroupedRouteArgs& a, const GroupedRow<EPL>& r, double per_total, int (&id)[EPL]) {
+__device__ __forceinline__ void choose_exactly(const GroupedRouteArgs& a, const GroupedRow<EPL>& r, double per_total, int& id, int32_t* ids) {
     const int lane = __lane_id(), within = lane - r.group * a.lanes;
     uint64_t key[EPL];
 #pragma unroll
@@ -117,37 +118,35 @@ __device__ __forceinline__ void choose_exactly(const GroupedRouteArgs& a, const 
         }
     }
     uint32_t taken = 0;
+    for (int i = 0; i < a.k; ++i) {
+        uint64_t best = 0;                           // this lane's first of the largest scores, of those the largest logits
+        uint32_t order = 0;
+        int at = 0;
 #pragma unroll
-    for (int s = 0; s < EPL; ++s) {
-        id[s] = 0;
-        const int end = a.k - 64 * s < 64 ? a.k - 64 * s : 64;
-        for (int i = 0; i < end; ++i) {
-            uint64_t best = 0;                       // this lane's first of the largest scores, of those the largest logits
-            uint32_t order = 0;
-            int at = 0;
-#pragma unroll
-            for (int j = 0; j < EPL; ++j) {
-                const uint64_t k = taken >> j & 1 ? 0 : key[j];
-                const uint32_t o = k > kScoreMasked ? route_key(r.logit[j]) : 0;
-                const bool more = k > best || (k == best && o > order);
-                best = more ? k : best;
-                order = more ? o : order;
-                at = more ? j : at;
-            }
-            const uint32_t hi = (uint32_t)(best >> 32), most = wave_max_u32(hi);
-            bool mine = hi == most;
-            uint64_t who = __ballot(mine);
-            if (who & (who - 1)) {                   // several lanes: by the lower half, then by the logit, then the first
-                const uint32_t lo = mine ? (uint32_t)best : 0, most_lo = wave_max_u32(lo);
-                mine = mine && lo == most_lo;
-                const uint32_t o = mine ? order : 0, most_o = wave_max_u32(o);
-                who = __ballot(mine && o == most_o);
-            }
-            const int owner = __builtin_ctzll(who);
-            const int e = __builtin_amdgcn_readlane(r.first + at, owner);
-            if (lane == i) id[s] = e;
-            if (lane == owner) taken |= 1u << at;
+        for (int j = 0; j < EPL; ++j) {
+            const uint64_t k = taken >> j & 1 ? 0 : key[j];
+            const uint32_t o = k > kScoreMasked ? route_key(r.logit[j]) : 0;
+            const bool more = k > best || (k == best && o > order);
+            best = more ? k : best;
+            order = more ? o : order;
+            at = more ? j : at;
         }
+        const uint32_t hi = (uint32_t)(best >> 32), most = wave_max_u32(hi);
+        bool mine = hi == most;
+        uint64_t who = __ballot(mine);
+        if (who & (who - 1)) {                       // several lanes: by the lower half, then by the logit, then the first
+            const uint32_t lo = mine ? (uint32_t)best : 0, most_lo = wave_max_u32(lo);
+            mine = mine && lo == most_lo;
+            const uint32_t o = mine ? order : 0, most_o = wave_max_u32(o);
+            who = __ballot(mine && o == most_o);
+        }
+        const int owner = __builtin_ctzll(who);
+        const int e = __builtin_amdgcn_readlane(r.first + at, owner);
+        if (lane == (i & 63)) {
+            if (i < 64) id = e;
+            else ids[i] = e;
+        }
+        if (lane == owner) taken |= 1u << at;
     }
 }
 
@@ -198,7 +197,7 @@ enum { kChosen, kSetChosen, kNotChosen };
 // shares, at most ln 1024) 7 off, and its EPL + 6 additions; the inverse 1.1; s 1: less than 22 + EPL.  `apart`: two scores'; sums of two scores: twice that and their
 // own roundings.
 template <int EPL>
-__device__ __forceinline__ int choose_quickly(const GroupedRouteArgs& a, const GroupedRow<EPL>& r, int (&id)[EPL]) {
+__device__ __forceinline__ int choose_quickly(const GroupedRouteArgs& a, const GroupedRow<EPL>& r, int& id) {
     const int lane = __lane_id(), within = lane - r.group * a.lanes;
     uint32_t key[EPL];
     int expert[EPL];
@@ -285,12 +284,12 @@ __device__ __forceinline__ int choose_quickly(const GroupedRouteArgs& a, const G
         }
     }
     uint32_t now = wave_max_u32(key[0]), chosen = 0;
-    id[0] = 0;
+    id = 0;
     auto take = [&](int i) __attribute__((always_inline)) {
         const int owner = __builtin_ctzll(__ballot(key[0] == now));
         const int e = __builtin_amdgcn_readlane(expert[0], owner);
         if (lane == i) {
-            id[0] = e;
+            id = e;
             chosen = now;
         }
         if (lane == owner) {
@@ -314,7 +313,7 @@ __device__ __forceinline__ int choose_quickly(const GroupedRouteArgs& a, const G
         take(a.k);
         if (now > 1 && !(last - score_of_key32(now) > apart)) return kNotChosen;
     } else if (lane == a.k) {
-        id[0] = -1;                                  // nobody: a masked expert is no rival
+        id = -1;                                  // nobody: a masked expert is no rival
     }
     return kSetChosen;
 }
@@ -336,7 +335,7 @@ __device__ __forceinline__ int put_in_order(const GroupedRouteArgs& a, int id, f
     return __builtin_amdgcn_ds_permute(4 * (lane <= a.k ? rank : lane), id);
 }
 
-// A wavefront per token, four tokens a workgroup.  The i-th choice comes back in slot i / 64 of lane i % 64.
+// A wavefront per token, four tokens a workgroup.
 template <int EPL, class Src>
 __global__ __launch_bounds__(256) void route_grouped_kernel(GroupedRouteArgs a, int32_t* __restrict__ ids, float* __restrict__ weights) {
     const int64_t t = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
@@ -392,53 +391,48 @@ __global__ __launch_bounds__(256) void route_grouped_kernel(GroupedRouteArgs a, 
         per_total = 1. / wave_sum_f64(total);
         summed = true;
     };
-    int id[EPL];
-    bool done = __ballot(r.live != 0) == 0;          // (a padding row: the first k, of the first groups)
-    if (done) {
-#pragma unroll
-        for (int s = 0; s < EPL; ++s) id[s] = 64 * s + lane;
-    }
-    if constexpr (EPL <= 16) {
-        if (!done && a.k < 63) {
-            const int seen = choose_quickly<EPL>(a, r, id);
-            done = seen != kNotChosen;
-            if (seen == kSetChosen) {
-                sum_up();
-                const int e = id[0] < 0 || lane > a.k ? 0 : id[0];
-                id[0] = put_in_order(a, id[0], load_value(row + e), a.bias ? a.bias[e] : 0.f, r.top, per_total);
-            }
+    int32_t* ids_row = ids + t * a.k;
+    int id = lane;                                   // (a row of nothing but masked experts: the first k, of the first groups)
+    const bool padding = __ballot(r.live != 0) == 0;
+    if (padding) {
+        for (int i = 64 + lane; i < a.k; i += 64) ids_row[i] = i;
+    } else {
+        int seen = kNotChosen;
+        if constexpr (EPL <= 16) {
+            if (a.k < 63) seen = choose_quickly<EPL>(a, r, id);
         }
-    }
-    if (!done) {
-        sum_up();
-        choose_exactly<EPL>(a, r, per_total, id);
+        if (seen != kChosen) sum_up();
+        if (seen == kSetChosen) {
+            const int e = id < 0 || lane > a.k ? 0 : id;
+            id = put_in_order(a, id, load_value(row + e), a.bias ? a.bias[e] : 0.f, r.top, per_total);
+        } else if (seen == kNotChosen) {
+            choose_exactly<EPL>(a, r, per_total, id, ids_row);
+        }
     }
     // Renormalised weights are quotients in which a softmax's sum drops out.
     if (!a.renormalize) sum_up();
     else if (!summed) per_total = 1.;
-    double w[EPL], sum = 0.;
-#pragma unroll
-    for (int s = 0; s < EPL; ++s) {
-        w[s] = 0.;
-        if (64 * s < a.k) {
-            const int i = 64 * s + lane, e = i < a.k ? id[s] : 0;
-            const float l = load_value(row + e), bias = a.bias ? a.bias[e] : 0.f;
-            const double p = route_probability(l, a.sigmoid, r.top, per_total);
-            w[s] = (i < a.k) & (l != -__builtin_inff()) & (bias != -__builtin_inff()) ? p : 0.;
-            sum += w[s];
-        }
-        if (EPL > 4) __builtin_amdgcn_sched_barrier(0);
+    auto weight = [&](int e) {
+        const float l = load_value(row + e), bias = a.bias ? a.bias[e] : 0.f;
+        const double p = route_probability(l, a.sigmoid, r.top, per_total);
+        return (l != -__builtin_inff()) & (bias != -__builtin_inff()) ? p : 0.;
+    };
+    const double w = lane < a.k ? weight(id) : 0.;
+    double sum = w;
+    if (a.renormalize) {
+        for (int i = 64 + lane; i < a.k; i += 64) sum += weight(ids_row[i]);
+        sum = wave_sum_f64(sum);
     }
-    if (a.renormalize) sum = wave_sum_f64(sum);
-#pragma unroll
-    for (int s = 0; s < EPL; ++s) {
-        const int i = 64 * s + lane;
-        if (i < a.k) {
-            ids[t * a.k + i] = id[s];
-            if (a.renormalize) w[s] = sum == 0. ? 0. : w[s] / sum;   // (a sum may be small enough for its inverse to leave 64 bits)
-            weights[t * a.k + i] = (float)(w[s] * (double)a.scale);
-        }
+    float* weights_row = weights + t * a.k;
+    auto scaled = [&](double p) {
+        if (a.renormalize) p = sum == 0. ? 0. : p / sum;   // (a sum may be small enough for its inverse to leave 64 bits)
+        return (float)(p * (double)a.scale);
+    };
+    if (lane < a.k) {
+        ids_row[lane] = id;
+        weights_row[lane] = scaled(w);
     }
+    for (int i = 64 + lane; i < a.k; i += 64) weights_row[i] = scaled(weight(ids_row[i]));
 }
 
 }  // namespace moe
