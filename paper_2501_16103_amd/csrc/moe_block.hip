@@ -31,17 +31,26 @@ int launch_grouped(const GroupedRouteArgs& a, bool f32, int32_t* ids, float* wei
 
 constexpr int kNormCols = 65536;
 
+// Pieces of eight elements a thread: one up to 256 pieces, two beyond, with as many threads as that takes; more only where 1024 threads are too few.  us, one / two /
+// four: norm with both outputs, bf16, 1 row of 2048 2.5 / 2.9 / 3.4, of 7168 3.9 / 3.8 / 4.9, 4096 rows of 2048 18.3 / 19.5 / 20.4, of 7168 51.0 / 48.6 / 49.4, 777 of 3584
+// with an fp32 residual 11.3 / 11.8 / 12.0; rows alone, 8192 of 1408 9.6 / 9.4 / 9.1 (the side that loses), of 4096 20.7 / 19.5 / 19.7, of 14336 - / 61.3 / 63.2.
 template <class X, class R, class W>
-int launch_norm_rows(const NormArgs& a, int64_t rows, hipStream_t s) {
+int launch_norm_rows(NormArgs a, int64_t rows, hipStream_t s) {
     const int pieces = (a.cols + 7) / 8;
     const int each = pieces <= 256 ? 1 : pieces <= 2048 ? 2 : pieces <= 4096 ? 4 : 8;
     const int threads = ((pieces + each - 1) / each + 63) / 64 * 64;
-    const dim3 grid((unsigned)rows);
-    if (each == 1) norm_rows_kernel<1, 256, X, R, W><<<grid, threads, 0, s>>>(a);
-    else if (each == 2) norm_rows_kernel<2, 1024, X, R, W><<<grid, threads, 0, s>>>(a);
-    else if (each == 4) norm_rows_kernel<4, 1024, X, R, W><<<grid, threads, 0, s>>>(a);
-    else norm_rows_kernel<8, 1024, X, R, W><<<grid, threads, 0, s>>>(a);
-    return launched();
+    constexpr int64_t kRows = (1 << 22) - 1;         // of one launch: its work items are counted in 32 bits
+    static_assert(work_items_fit(kRows, 1024), "rows of a launch");
+    for (a.first_row = 0; a.first_row < rows; a.first_row += kRows) {
+        const dim3 grid((unsigned)(rows - a.first_row < kRows ? rows - a.first_row : kRows));
+        if (each == 1) norm_rows_kernel<1, 256, X, R, W><<<grid, threads, 0, s>>>(a);
+        else if (each == 2) norm_rows_kernel<2, 1024, X, R, W><<<grid, threads, 0, s>>>(a);
+        else if (each == 4) norm_rows_kernel<4, 1024, X, R, W><<<grid, threads, 0, s>>>(a);
+        else norm_rows_kernel<8, 1024, X, R, W><<<grid, threads, 0, s>>>(a);
+        const int rc = launched();
+        if (rc != MOE_OK) return rc;
+    }
+    return MOE_OK;
 }
 template <class X, class R>
 int launch_norm_rows(const NormArgs& a, bool weight_f32, int64_t rows, hipStream_t s) {
@@ -61,6 +70,15 @@ int check_w4(int K, int N, int group, int gated) {
 }
 int64_t w4_tiles(int K, int N, int gated) { return w4_tiles_n(N, gated) * w4_tiles_k(K); }
 
+// Tiles of columns a workgroup takes, and wavefronts that share K.  One tile while that gives about a workgroup per CU, with up to sixteen wavefronts of two
+// tiles along K at least; two beyond, with eight; four with four wavefronts from four rounds of single tiles on, where what counts is that tokens and
+// a workgroup's start serve more weights, and with eight from three on where tokens are many.  us, T = 1 / 16, one, two, four tiles of columns:
+//   4096 -> 4096 (256 tiles)    3.7, -, - / -;  eight and sixteen wavefronts 3.7 and 3.7;  14336 -> 4096 10.0 and 7.5 / 12.1 and 12.7
+//   4096 -> 5632 (352)          4.6, 4.5, - / 7.1, 5.4, -
+//   4096 -> 14336 (896)         8.2, 7.4, 7.5 / 12.2, 10.1, 8.7
+//   4096 -> 20480 (1280)        -, 9.8, 11.0 / -, 14.8, 14.8  (four lose a tenth here for one token);  eight wavefronts 12.2, 12.4 / 13.8, 15.5
+//   4096 -> 28672 gated (1792)  -, 13.3, 12.7 / -, 18.5, 15.3;  eight wavefronts 13.5, 13.6 / 18.3, 16.6
+//   gated 7168 -> 2816 (176)    -, 6.1, - with eight wavefronts, 5.7 with sixteen;  2048 -> 2816 3.4 with eight, 3.5 with sixteen
 template <int NT, int TR, int PER, bool GATED>
 int launch_w4(const W4Args& a, hipStream_t s) {
     const int grid = (a.tiles_n + NT - 1) / NT, most = a.tiles_n >= 4 * kCus ? 4 : grid > kCus || NT == 4 ? 8 : 16;
@@ -121,7 +139,7 @@ int moe_add_norm(const void* x, const void* residual, const void* weight, const 
     if (misaligned(x, xb) || (residual && (misaligned(residual, rb) || misaligned(residual_out, rb))) || (weight && misaligned(weight, wb)) || misaligned(y, 2) ||
         misaligned(scales, 4)) return MOE_ERR_INVALID_ARG;
     const int64_t xs = d->rows > 1 ? d->x_stride : 0, rs = d->rows > 1 ? d->residual_stride : 0;
-    const NormArgs a = {x, residual, weight, xs, rs, d->cols, d->eps, residual_out, static_cast<uint16_t*>(y), static_cast<uint8_t*>(codes), scales};
+    const NormArgs a = {x, residual, weight, xs, rs, 0, d->cols, d->eps, residual_out, static_cast<uint16_t*>(y), static_cast<uint8_t*>(codes), scales};
     const hipStream_t s = static_cast<hipStream_t>(stream);
     const bool r32 = d->residual_dtype == MOE_DTYPE_FP32, w32 = d->weight_dtype == MOE_DTYPE_FP32;
     return d->x_dtype == MOE_DTYPE_FP32 ? launch_norm_rows<float>(a, r32, w32, d->rows, s) : launch_norm_rows<uint16_t>(a, r32, w32, d->rows, s);

@@ -77,6 +77,20 @@ def test_scores_next_to_each_other():
     _check(x.to(DEV), x, 8, 8, 4, True, bias, True, True, 1.0)
 
 
+@pytest.mark.parametrize("k", [1, 2, 5, 6, 15, 16, 31])
+@pytest.mark.parametrize("sigmoid", [False, True])
+def test_neighbours_in_pairs(k, sigmoid):
+    """Pairs of scores that differ by less than 32 bits can tell, well apart from the next pair; the border of the choice lies between two pairs or in one."""
+    g = torch.Generator().manual_seed(k)
+    for groups, kept in ((8, 4), (1, 1)):
+        x = torch.randn(1, 64, generator=g)
+        p = torch.sigmoid(x.double()) if sigmoid else torch.softmax(x.double(), 1)
+        place = torch.randperm(64, generator=g)
+        bias = (1.5 - 0.01 * (place // 2) - p[0]).float()        # (rounded: the two of a pair end up some 2^-26 apart)
+        x = x + 1e-8 * torch.randn(60, 64, generator=g)
+        _check(x.to(DEV), x, k, groups, kept, False, bias, sigmoid, True, 1.0)
+
+
 def test_without_groups_and_bias_the_choices_are_moe_routes():
     for kind in ("normal", "ties", "masked", "large"):
         x, _ = _inputs(50, 96, 8, torch.float32, kind)
