@@ -198,16 +198,16 @@ enum { kChosen, kSetChosen, kNotChosen };
 // The choice in 32 bits.  kChosen: every two neighbours in its order, the first one left out, and the groups on either side of the border differ by more
 // than their errors, so 64 bits choose the same.  kSetChosen: the first k and the one behind them (in lane k) are the first k + 1, in some order.
 //
-// Errors, in parts of `size`, the row's largest p + |bias|, and units of 2^-24.  sigmoid: e^-|l| 3 of itself, which p moves with; 1 + e 1; the inverse 1.1; the
-// product 1; s 1: less than 8 a score.  softmax: l - top is off by 1 of itself and moves e by 0.4 at most, e 3; the sum of terms 3 and (on average over their
-// shares, at most ln 1024) 7 off, and its EPL + 6 additions; the inverse 1.1; s 1: less than 22 + EPL.  `apart`: two scores'; sums of two scores: twice that and their
-// own roundings.
+// Errors, in units of 2^-24.  Of p, in parts of the row's largest: sigmoid: e^-|l| 3 of itself, which p moves with; 1 + e 1; the inverse 1.1; the product 1: less than 8.
+// Softmax: l - top is off by 1 of itself and moves e by 0.4 at most, e 3; the sum of terms 3 and (on average over their shares, at most ln 1024) 7 off, and its
+// EPL + 6 additions; the inverse 1.1: less than 22 + EPL.  `apart`: those of two.  Of s = p + bias: 1 of itself more, of a sum of two 1 of each and of the sum (twice
+// that is asked for): a large bias of an expert that is out of reach does not count.
 template <int EPL>
 __device__ __forceinline__ int choose_quickly(const GroupedRouteArgs& a, const GroupedRow<EPL>& r, int& id) {
     const int lane = __lane_id(), within = lane - r.group * a.lanes;
     uint32_t key[EPL];
     int expert[EPL];
-    float p[EPL], per_total = 1.f, size = 0.f;
+    float p[EPL], per_total = 1.f, largest = 0.f;
     if (a.sigmoid) {
 #pragma unroll
         for (int j = 0; j < EPL; ++j) {
@@ -227,15 +227,15 @@ __device__ __forceinline__ int choose_quickly(const GroupedRouteArgs& a, const G
 #pragma unroll
     for (int j = 0; j < EPL; ++j) {
         const bool live = r.live >> j & 1;
-        const float s = fmaf(p[j], per_total, r.bias[j]), c = live ? fmaf(p[j], per_total, fabsf(r.bias[j])) : 0.f;
-        number = number & (c <= 1e30f);              // (false for a NaN)
-        size = c > size ? c : size;
+        const float s = fmaf(p[j], per_total, r.bias[j]), c = live ? p[j] : 0.f;
+        number = number & !(live & !(fabsf(s) <= 1e30f));   // (false for a NaN)
+        largest = c > largest ? c : largest;
         key[j] = j >= r.count ? 0 : live ? score_key32(s) : 1;
         expert[j] = r.first + j;
     }
-    size = __uint_as_float(wave_max_u32(__float_as_uint(size)));
-    if (__ballot(!number) || size < 0x1p-100f) return kNotChosen;
-    const float apart = size * (a.sigmoid ? 16.f : 2.f * (22 + EPL)) * 0x1p-24f, groups_apart = 2.5f * apart;
+    largest = __uint_as_float(wave_max_u32(__float_as_uint(largest))) * per_total;
+    if (__ballot(!number) || largest < 0x1p-100f) return kNotChosen;
+    const float apart = largest * (a.sigmoid ? 16.f : 2.f * (22 + EPL)) * 0x1p-24f;
     // a lane's experts in falling order (insertion, an element moves up past strictly smaller ones only)
 #pragma unroll
     for (int j = 1; j < EPL; ++j) {
@@ -256,8 +256,12 @@ __device__ __forceinline__ int choose_quickly(const GroupedRouteArgs& a, const G
             two = low > more ? low : more;
         };
         uint32_t mine;
+        float size;                                  // what the group's score is added up from
         auto group_score = [&]() __attribute__((always_inline)) {
-            return a.top2 && two > 1 ? score_key32(score_of_key32(one) + score_of_key32(two)) : one;
+            const bool both = a.top2 && two > 1;
+            const float first = score_of_key32(one), second = score_of_key32(two);
+            size = one > 1 ? fabsf(first) + (both ? fabsf(second) : 0.f) : 0.f;
+            return both ? score_key32(first + second) : one;
         };
         if (a.lanes <= 16 && (a.lanes & (a.lanes - 1)) == 0) {
             // exchanges within 2, 4, 8 and 16 lanes; every lane of a group ends with its score
@@ -275,7 +279,9 @@ __device__ __forceinline__ int choose_quickly(const GroupedRouteArgs& a, const G
                 const uint32_t o1 = (uint32_t)__shfl((int)one, lane + width), o2 = (uint32_t)__shfl((int)two, lane + width);
                 if (within < width && within + width < a.lanes) merge(o1, o2);
             }
-            mine = (uint32_t)__shfl((int)group_score(), r.group < a.groups ? r.group * a.lanes : 0);
+            const int leader = r.group < a.groups ? r.group * a.lanes : 0;
+            mine = (uint32_t)__shfl((int)group_score(), leader);
+            size = __shfl(size, leader);
         }
         int above = 0;
         for (int g = 0; g < a.groups; ++g) above += (uint32_t)__builtin_amdgcn_readlane((int)mine, g * a.lanes) > mine;
@@ -283,7 +289,12 @@ __device__ __forceinline__ int choose_quickly(const GroupedRouteArgs& a, const G
         // (equal scores: all of them stay, or none does, and the numbers below do not add up)
         const uint32_t least = ~wave_max_u32(there && stays ? ~mine : 0), most = wave_max_u32(there && !stays ? mine : 0);
         const int staying = __popcll(__ballot(there && stays && within == 0));
-        if (staying != a.kept || (most > 1 && !(score_of_key32(least) - score_of_key32(most) > groups_apart))) return kNotChosen;
+        if (staying != a.kept) return kNotChosen;
+        if (most > 1) {                              // every group is on its side of the middle by more than its error
+            const float middle = 0.5f * score_of_key32(least) + 0.5f * score_of_key32(most), from = score_of_key32(mine) - middle;
+            const bool told = !there || mine <= 1 || (stays ? from : -from) > apart + size * 0x1p-22f;
+            if (__ballot(!told)) return kNotChosen;
+        }
         if (!stays) {
 #pragma unroll
             for (int j = 0; j < EPL; ++j) key[j] = 0;
@@ -312,14 +323,18 @@ __device__ __forceinline__ int choose_quickly(const GroupedRouteArgs& a, const G
     if (lane == a.k) chosen = now;
     // masked ones (1) come last and in order of their experts, nothing (0) comes behind them
     const uint32_t before = (uint32_t)__shfl((int)chosen, lane > 0 ? lane - 1 : 0);
-    const bool told = lane == 0 || lane > a.k || chosen <= 1 || score_of_key32(before) - score_of_key32(chosen) > apart;
+    auto tells = [&](uint32_t upper, uint32_t lower) __attribute__((always_inline)) {
+        const float u = score_of_key32(upper), l = score_of_key32(lower);
+        return lower <= 1 || u - l > apart + (fabsf(u) + fabsf(l)) * 0x1p-23f;
+    };
+    const bool told = lane == 0 || lane > a.k || tells(before, chosen);
     if (__ballot(!told) == 0) return kChosen;
     if (now > 1) {
-        const float last = score_of_key32(now);
+        const uint32_t last = now;
         take(a.k);
-        if (now > 1 && !(last - score_of_key32(now) > apart)) return kNotChosen;
+        if (!tells(last, now)) return kNotChosen;
     } else if (lane == a.k) {
-        id = -1;                                  // nobody: a masked expert is no rival
+        id = -1;                                     // nobody: a masked expert is no rival
     }
     return kSetChosen;
 }

@@ -77,6 +77,18 @@ def test_scores_next_to_each_other():
     _check(x.to(DEV), x, 8, 8, 4, True, bias, True, True, 1.0)
 
 
+@pytest.mark.parametrize("low", [-1e9, -1e4, -30.0, 1e4])
+def test_experts_put_out_of_reach_by_their_bias(low):
+    """Biases far from the others' count as numbers: such experts come last (or first), and the others are told apart as without them."""
+    x, bias = _inputs(60, 128, 31, torch.float32, "normal")
+    bias[5::7] = low
+    bias[32:48] = low                                # a whole group
+    for sigmoid in (False, True):
+        for top2 in (False, True):
+            _check(x.to(DEV), x, 6, 8, 3, top2, bias, sigmoid, True, 1.0)
+            _check(x.to(DEV), x, 40, 8, 4, top2, bias, sigmoid, True, 1.0)
+
+
 @pytest.mark.parametrize("k", [1, 2, 5, 6, 15, 16, 31])
 @pytest.mark.parametrize("sigmoid", [False, True])
 def test_neighbours_in_pairs(k, sigmoid):
