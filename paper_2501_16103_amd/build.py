@@ -31,7 +31,7 @@ HIPCC_FLAGS = [
 # they cannot let a DMA wait pass early: loads retire in order and extra entries in vmcnt make a wait stricter.)
 # The 4-bit products and the layer for few tokens are held to the same: their loops over k, of fewer MFMAs a step, have loads of
 # later steps under way, which the wait for a reload drains as well.
-SPILL_CHECKED = "(?:gemm|few_tokens)"
+SPILL_CHECKED = "(?:gemm|few_tokens|w4_matvec)"
 
 
 def check_no_spill_in_k_loops(asm_text: str) -> None:
@@ -41,7 +41,7 @@ def check_no_spill_in_k_loops(asm_text: str) -> None:
             raise RuntimeError(f"{m.group(1)}: {m.group(2)} bytes of private memory per lane (an array left in memory?)")
     for m in re.finditer(rf"^(_ZN3moe\S*{SPILL_CHECKED}\S*):\s*(?:;.*)?$", asm_text, re.M):
         name = m.group(1)
-        least = 4 if "mx4_gemm" in name or "few_tokens" in name else 16   # MFMAs of a k-step
+        least = 4 if "mx4_gemm" in name or "few_tokens" in name or "w4_matvec" in name else 16   # MFMAs of a k-step
         end = asm_text.find(".Lfunc_end", m.end())
         lines = asm_text[m.end():end].splitlines()
         label_at = {ln.split(":")[0]: k for k, ln in enumerate(lines) if ln.startswith(".LBB")}
