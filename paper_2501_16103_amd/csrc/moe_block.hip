@@ -36,7 +36,8 @@ constexpr int kNormCols = 65536;
 // with an fp32 residual 11.3 / 11.8 / 12.0; rows alone, 8192 of 1408 9.6 / 9.4 / 9.1 (the side that loses), of 4096 20.7 / 19.5 / 19.7, of 14336 - / 61.3 / 63.2.
 template <class X, class R, class W>
 int launch_norm_rows(NormArgs a, int64_t rows, hipStream_t s) {
-    const int pieces = (a.cols + 7) / 8;
+    if (a.cols + 14 >= kNormCols + 8) a.in_step = 0;   // (a piece more than the largest launch has)
+    const int pieces = (a.cols + 7 + (a.in_step ? 7 : 0)) / 8;
     const int each = pieces <= 256 ? 1 : pieces <= 2048 ? 2 : pieces <= 4096 ? 4 : 8;
     const int threads = ((pieces + each - 1) / each + 63) / 64 * 64;
     constexpr int64_t kRows = (1 << 22) - 1;         // of one launch: its work items are counted in 32 bits
@@ -139,7 +140,9 @@ int moe_add_norm(const void* x, const void* residual, const void* weight, const 
     if (misaligned(x, xb) || (residual && (misaligned(residual, rb) || misaligned(residual_out, rb))) || (weight && misaligned(weight, wb)) || misaligned(y, 2) ||
         misaligned(scales, 4)) return MOE_ERR_INVALID_ARG;
     const int64_t xs = d->rows > 1 ? d->x_stride : 0, rs = d->rows > 1 ? d->residual_stride : 0;
-    const NormArgs a = {x, residual, weight, xs, rs, 0, d->cols, d->eps, residual_out, static_cast<uint16_t*>(y), static_cast<uint8_t*>(codes), scales};
+    const int in_step = d->cols % 8 != 0 && d->cols > 8 && !misaligned(x, 16) && (xs - d->cols) % 8 == 0 &&
+                        (!residual || (!misaligned(residual, 16) && (rs - d->cols) % 8 == 0 && !misaligned(residual_out, 16))) && !misaligned(y, 16) && !misaligned(codes, 8);
+    const NormArgs a = {x, residual, weight, xs, rs, 0, d->cols, in_step, d->eps, residual_out, static_cast<uint16_t*>(y), static_cast<uint8_t*>(codes), scales};
     const hipStream_t s = static_cast<hipStream_t>(stream);
     const bool r32 = d->residual_dtype == MOE_DTYPE_FP32, w32 = d->weight_dtype == MOE_DTYPE_FP32;
     return d->x_dtype == MOE_DTYPE_FP32 ? launch_norm_rows<float>(a, r32, w32, d->rows, s) : launch_norm_rows<uint16_t>(a, r32, w32, d->rows, s);
@@ -155,6 +158,7 @@ int moe_fp8_quantize(const void* src, int dtype, int64_t rows, int cols, int64_t
     NormArgs a{};
     a.x = src; a.x_stride = row_stride; a.cols = cols;
     a.codes = static_cast<uint8_t*>(codes); a.scales = scales;
+    a.in_step = cols % 8 != 0 && cols > 8 && !misaligned(src, 16) && (row_stride - cols) % 8 == 0 && !misaligned(codes, 8);
     const hipStream_t s = static_cast<hipStream_t>(stream);
     return dtype == MOE_DTYPE_FP32 ? launch_norm_rows<float, void, void>(a, rows, s) : launch_norm_rows<uint16_t, void, void>(a, rows, s);
 }

@@ -8,8 +8,9 @@
 // A row with an infinity or a NaN (in h or in y) has the scale NaN and codes of NaN.
 //
 // What bounds it: memory, with many rows (4096 rows of 7168 with all outputs, 264 MB, 48.6 us, 5.4 TB/s read and written; 8192 rows of 14336 alone 61.2 us, 5.8 TB/s; a large
-// copy: 5.15); with few the launch and one chain of load, two exchanges and store (one row of 2048: 2.5 us back to back, 6.3 with the call's own time).  Rows that
-// do not begin on 16 bytes cost a quarter (777 of 3583 with an fp32 residual 14.3 us, of 3584 11.5).  Elements are held as they are stored, bf16 by
+// copy: 5.15); with few the launch and one chain of load, two exchanges and store (one row of 2048: 2.5 us back to back, 6.3 with the call's own time).  Rows of an odd
+// length begin anywhere; with pieces on multiples of eight of the whole tensor all accesses but those at a row's ends are aligned (2529 rows of 5143, bf16 with an fp32 weight,
+// all outputs, 30.7 us, of 5144 29.0; with pieces counted from the row's beginning 43.3).  Elements are held as they are stored, bf16 by
 // twos, until they are used: as floats, 4096 rows of 7168 took 64.6.
 #pragma once
 #include <hip/hip_runtime.h>
@@ -31,6 +32,7 @@ struct NormArgs {
     int64_t x_stride, residual_stride;
     int64_t first_row;           // of this launch
     int cols;
+    int in_step;                 // 1: all rows begin as far from a multiple of eight elements as row * cols does (see RowPiece)
     float eps;
     void* sum;                   // [rows][cols] of the residual's type, or null
     uint16_t* y;                 // [rows][cols], or null
@@ -57,27 +59,48 @@ struct Eight {
     }
 };
 
-// Eight consecutive elements of a row of `cols`, at any alignment; the last piece of a row may be a part of eight.
+// Elements at .. at + 7 of a row of `cols`; the first and the last piece of a row may hold fewer.  Pieces begin on multiples of eight of row * cols + element
+// where all rows do so alike: then what is not whole is at the row's ends, and everything between is aligned, whatever `cols` is.
 struct RowPiece {
     int at, cols;
-    __device__ __forceinline__ bool has(int i) const { return at + i < cols; }
-    __device__ __forceinline__ bool whole() const { return at + 8 <= cols; }
-    // Whole pieces; of the others the row's first elements are read (a choice here would wait for what was loaded).  cols >= 8.
+    __device__ __forceinline__ bool has(int i) const { return (unsigned)(at + i) < (unsigned)cols; }
+    __device__ __forceinline__ bool whole() const { return at >= 0 && at + 8 <= cols; }
+    __device__ __forceinline__ int from() const { return at < 0 ? 0 : at + 8 <= cols ? at : cols - 8; }
+    // The eight elements of the row that hold the piece's (cols >= 8), which fit() then moves to their places: a choice made here would wait for them.
     template <class T>
     __device__ __forceinline__ void load(const void* base, int64_t row_at, Eight<T>& e) const {
-        const T* p = static_cast<const T*>(base) + row_at + (whole() ? at : 0);
+        const char* p = reinterpret_cast<const char*>(static_cast<const T*>(base) + row_at + from());
 #pragma unroll
-        for (int i = 0; i < (int)sizeof(T) / 2; ++i) e.v[i] = *reinterpret_cast<const u32x4_any_t*>(reinterpret_cast<const char*>(p) + 16 * i);
+        for (int i = 0; i < (int)sizeof(T) / 2; ++i) e.v[i] = *reinterpret_cast<const u32x4_any_t*>(p + 16 * i);
     }
-    // A piece that is not whole: its elements one by one, zeros beyond.
     template <class T>
-    __device__ __forceinline__ void load_part(const void* base, int64_t row_at, Eight<T>& e) const {
+    __device__ __forceinline__ void fit(Eight<T>& e) const {
+        typedef unsigned __int128 u128;
+        const int by = at - from();                  // element i of the piece is element i + by of what was read
+        if constexpr (sizeof(T) == 2) {
+            u128 v = __builtin_bit_cast(u128, e.v[0]);
+            v = by >= 8 ? 0 : by >= 0 ? v >> (16 * by) : v << (-16 * by);
+            e.v[0] = __builtin_bit_cast(u32x4_t, v);
+        } else {
+            u128 lo = __builtin_bit_cast(u128, e.v[0]), hi = __builtin_bit_cast(u128, e.v[1]);
+            if (by >= 4) { lo = hi; hi = 0; }
+            if (by <= -4) { hi = lo; lo = 0; }
+            const int rest = by >= 8 ? 4 : by >= 0 ? by & 3 : -(-by & 3);
+            if (rest == 4) lo = 0;
+            else if (rest > 0) { lo = lo >> (32 * rest) | hi << (128 - 32 * rest); hi >>= 32 * rest; }
+            else if (rest < 0) { hi = hi << (-32 * rest) | lo >> (128 + 32 * rest); lo <<= -32 * rest; }
+            e.v[0] = __builtin_bit_cast(u32x4_t, lo);
+            e.v[1] = __builtin_bit_cast(u32x4_t, hi);
+        }
+    }
+    // The same of a row of fewer than eight elements.
+    template <class T>
+    __device__ __forceinline__ void load_short(const void* base, int64_t row_at, Eight<T>& e) const {
         float f[8];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            f[i] = 0.f;
-            if (has(i)) f[i] = load_value(static_cast<const T*>(base) + row_at + at + i);
-        }
+        for (int i = 0; i < 8; ++i) f[i] = load_value(static_cast<const T*>(base) + row_at + (has(i) ? at + i : 0));
+#pragma unroll
+        for (int i = 0; i < 8; ++i) f[i] = has(i) ? f[i] : 0.f;
         e.set(f);
     }
     template <class T>
@@ -162,8 +185,9 @@ __global__ __launch_bounds__(THREADS) void norm_rows_kernel(NormArgs a) {
     {
         Eight<X> x[CH];
         Eight<H> r[CH];
+        const int ahead = a.in_step ? (int)((row * a.cols) & 7) : 0;
 #pragma unroll
-        for (int c = 0; c < CH; ++c) piece[c] = RowPiece{8 * (c * threads + (int)threadIdx.x), a.cols};
+        for (int c = 0; c < CH; ++c) piece[c] = RowPiece{8 * (c * threads + (int)threadIdx.x) - ahead, a.cols};
         if (a.cols >= 8) {
 #pragma unroll
             for (int c = 0; c < CH; ++c) piece[c].load(a.x, x_at, x[c]);
@@ -175,13 +199,20 @@ __global__ __launch_bounds__(THREADS) void norm_rows_kernel(NormArgs a) {
 #pragma unroll
                 for (int c = 0; c < CH; ++c) piece[c].load(a.weight, 0, w[c]);
             }
-        }
 #pragma unroll
-        for (int c = 0; c < CH; ++c) {
-            if (!piece[c].whole()) {                 // (a part of a row's end, or nothing)
-                piece[c].load_part(a.x, x_at, x[c]);
-                if constexpr (ADD) piece[c].load_part(a.residual, r_at, r[c]);
-                if (NORM && a.weight) piece[c].load_part(a.weight, 0, w[c]);
+            for (int c = 0; c < CH; ++c) {
+                if (!piece[c].whole()) {
+                    piece[c].fit(x[c]);
+                    if constexpr (ADD) piece[c].fit(r[c]);
+                    if (NORM && a.weight) piece[c].fit(w[c]);
+                }
+            }
+        } else {
+#pragma unroll
+            for (int c = 0; c < CH; ++c) {
+                piece[c].load_short(a.x, x_at, x[c]);
+                if constexpr (ADD) piece[c].load_short(a.residual, r_at, r[c]);
+                if (NORM && a.weight) piece[c].load_short(a.weight, 0, w[c]);
             }
         }
 #pragma unroll

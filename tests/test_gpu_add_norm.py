@@ -68,7 +68,8 @@ def _check(x, residual, weight, eps=1e-6, want_y=True, want_rows=True, want_sum=
         assert bool((rows.codes[T] == 9).all()) and float(rows.scales[T]) == 9.0
 
 
-@pytest.mark.parametrize("T,H", [(1, 1), (1, 2048), (3, 7), (5, 64), (2, 65), (33, 520), (7, 1408), (4, 2049), (3, 3583), (2, 7168), (2, 16384), (2, 16385), (1, 20000), (1, 65536)])
+@pytest.mark.parametrize("T,H", [(1, 1), (1, 2048), (3, 7), (5, 64), (2, 65), (33, 520), (7, 1408), (4, 2049), (3, 3583), (2, 7168), (2, 16384), (2, 16385), (1, 20000), (1, 65536),
+                                 (9, 9), (17, 4091), (9, 65535)])
 @pytest.mark.parametrize("x,residual,weight", [(BF16, BF16, BF16), (BF16, None, BF16), (BF16, F32, F32), (F32, F32, BF16), (F32, BF16, F32), (F32, None, None), (BF16, BF16, None)])
 def test_add_norm(T, H, x, residual, weight):
     w = None if weight is None else (1 + 0.2 * torch.randn(H, generator=torch.Generator().manual_seed(H))).to(weight)
@@ -107,6 +108,14 @@ def test_rows_apart_and_unaligned():
     _check(_rows(8, 512, 12, BF16), _rows(8, 512, 13, BF16), _rows(1, 512, 14, BF16)[0], to=inside)
     _check(_rows(8, 129, 12, F32), _rows(8, 129, 13, BF16), None, to=inside)
 
+    def in_step(t):                                  # rows that begin as far from 16 bytes as those of the outputs, and do not follow one another
+        wide = torch.full((t.shape[0], t.shape[1] + 24), 3.0, dtype=t.dtype, device=DEV)
+        wide[:, 8: 8 + t.shape[1]] = t.to(DEV)
+        return wide[:, 8: 8 + t.shape[1]]
+    for H in (9, 15, 77, 1001, 5143):
+        _check(_rows(11, H, 23, BF16), _rows(11, H, 24, F32), _rows(1, H, 25, BF16)[0], to=in_step)
+        _check(_rows(11, H, 23, F32), _rows(11, H, 24, BF16), _rows(1, H, 25, F32)[0], to=in_step)
+
     def every_other(t):
         wide = torch.full((2 * t.shape[0], t.shape[1]), 3.0, dtype=t.dtype, device=DEV)
         wide[::2] = t.to(DEV)
@@ -116,13 +125,14 @@ def test_rows_apart_and_unaligned():
 
 def test_in_place():
     """The sum over the residual, and over x."""
-    x, r = _rows(11, 776, 17, BF16), _rows(11, 776, 18, BF16)
-    h, want = ref.add_norm(x, r, None, 1e-6)
-    for over in (0, 1):
-        xg, rg, y = x.to(DEV), r.to(DEV), torch.empty(11, 776, dtype=BF16, device=DEV)
-        mb.moe_add_norm(xg, None, 1e-6, residual=rg, residual_out=(xg, rg)[over], y=y)
-        assert torch.equal((xg, rg)[over].cpu(), h)
-        assert bool(((y.cpu().double() - want).abs() <= want.abs() * (2.0 ** -8 + _relative(776))).all())
+    for H in (776, 777, 4099):
+        x, r = _rows(11, H, 17, BF16), _rows(11, H, 18, BF16)
+        h, want = ref.add_norm(x, r, None, 1e-6)
+        for over in (0, 1):
+            xg, rg, y = x.to(DEV), r.to(DEV), torch.empty(11, H, dtype=BF16, device=DEV)
+            mb.moe_add_norm(xg, None, 1e-6, residual=rg, residual_out=(xg, rg)[over], y=y)
+            assert torch.equal((xg, rg)[over].cpu(), h)
+            assert bool(((y.cpu().double() - want).abs() <= want.abs() * (2.0 ** -8 + _relative(H))).all())
 
 
 @pytest.mark.parametrize("dtype", [BF16, F32])
