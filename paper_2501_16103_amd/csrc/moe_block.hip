@@ -34,7 +34,7 @@ constexpr int kNormCols = 65536;
 // Pieces of eight elements a thread: one up to 256 pieces, two beyond, with as many threads as that takes; more only where 1024 threads are too few.  us, one / two /
 // four: norm with both outputs, bf16, 1 row of 2048 2.5 / 2.9 / 3.4, of 7168 3.9 / 3.8 / 4.9, 4096 rows of 2048 18.3 / 19.5 / 20.4, of 7168 51.0 / 48.6 / 49.4, 777 of 3584
 // with an fp32 residual 11.3 / 11.8 / 12.0; rows alone, 8192 of 1408 9.6 / 9.4 / 9.1 (the side that loses), of 4096 20.7 / 19.5 / 19.7, of 14336 - / 61.3 / 63.2.
-template <class X, class R, class W>
+template <class X, class R, class W, bool ENDS>
 int launch_norm_rows(NormArgs a, int64_t rows, hipStream_t s) {
     if (a.cols + 14 >= kNormCols + 8) a.in_step = 0;   // (a piece more than the largest launch has)
     const int pieces = (a.cols + 7 + (a.in_step ? 7 : 0)) / 8;
@@ -44,14 +44,18 @@ int launch_norm_rows(NormArgs a, int64_t rows, hipStream_t s) {
     static_assert(work_items_fit(kRows, 1024), "rows of a launch");
     for (a.first_row = 0; a.first_row < rows; a.first_row += kRows) {
         const dim3 grid((unsigned)(rows - a.first_row < kRows ? rows - a.first_row : kRows));
-        if (each == 1) norm_rows_kernel<1, 256, X, R, W><<<grid, threads, 0, s>>>(a);
-        else if (each == 2) norm_rows_kernel<2, 1024, X, R, W><<<grid, threads, 0, s>>>(a);
-        else if (each == 4) norm_rows_kernel<4, 1024, X, R, W><<<grid, threads, 0, s>>>(a);
-        else norm_rows_kernel<8, 1024, X, R, W><<<grid, threads, 0, s>>>(a);
+        if (each == 1) norm_rows_kernel<1, 256, X, R, W, ENDS><<<grid, threads, 0, s>>>(a);
+        else if (each == 2) norm_rows_kernel<2, 1024, X, R, W, ENDS><<<grid, threads, 0, s>>>(a);
+        else if (each == 4) norm_rows_kernel<4, 1024, X, R, W, ENDS><<<grid, threads, 0, s>>>(a);
+        else norm_rows_kernel<8, 1024, X, R, W, ENDS><<<grid, threads, 0, s>>>(a);
         const int rc = launched();
         if (rc != MOE_OK) return rc;
     }
     return MOE_OK;
+}
+template <class X, class R, class W>
+int launch_norm_rows(const NormArgs& a, int64_t rows, hipStream_t s) {
+    return a.cols % 8 != 0 ? launch_norm_rows<X, R, W, true>(a, rows, s) : launch_norm_rows<X, R, W, false>(a, rows, s);
 }
 template <class X, class R>
 int launch_norm_rows(const NormArgs& a, bool weight_f32, int64_t rows, hipStream_t s) {
