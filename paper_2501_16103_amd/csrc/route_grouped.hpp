@@ -8,10 +8,10 @@
 // among 256 is another one every few calls.  The choice is that of scores in 64 bits, where that does not happen, compared as integers of both halves.
 //
 // It is made in 32 bits, whose scores are off by a few roundings, and most rows show that 64 bits would choose the same (choose_quickly).  Where neighbours in the
-// order are too near to tell, their scores in 64 bits put them in order (of 8192 tokens with 256 experts 4 or 5); where the border of the groups or of the set
-// is, the whole choice is made again in 64 bits (one row in 23 000).  What bounds it: few tokens, the launch and a chain of k + 5 maxima and two 64-bit exponentials (one token, 6 of 64:
-// 3.6 us, 5.2 with the call's own time); many, the issue of vector instructions: 8192 tokens, 8 of 256 in 8 groups of which 4 stay, sigmoid, bias, are 645 of them a
-// wavefront, eight wavefronts a SIMD, 8.6 of the 10.2 us (in 64 bits throughout 18.0).
+// order are too near to tell, their scores in 64 bits put them in order (of 8192 tokens with 256 experts two); where the border of the groups or of the set
+// is, the whole choice is made again in 64 bits (one row in 26 000).  What bounds it: few tokens, the launch and a chain of k + 5 maxima and two 64-bit exponentials (one token, 6 of
+// 64: 3.6 us, 5.2 with the call's own time); many, the issue of vector instructions: 8192 tokens, 8 of 256 in 8 groups of which 4 stay, sigmoid, bias, are 655 of them a wavefront,
+// eight wavefronts a SIMD, 8.7 of the 10.3 us, 11 to 13 where one of the rows is chosen in 64 bits (in 64 bits throughout 18.0).
 #pragma once
 #include <hip/hip_runtime.h>
 #include <stdint.h>
@@ -198,10 +198,10 @@ enum { kChosen, kSetChosen, kNotChosen };
 // The choice in 32 bits.  kChosen: every two neighbours in its order, the first one left out, and the groups on either side of the border differ by more
 // than their errors, so 64 bits choose the same.  kSetChosen: the first k and the one behind them (in lane k) are the first k + 1, in some order.
 //
-// Errors, in units of 2^-24.  Of p, in parts of the row's largest: sigmoid: e^-|l| 3 of itself, which p moves with; 1 + e 1; the inverse 1.1; the product 1: less than 8.
-// Softmax: l - top is off by 1 of itself and moves e by 0.4 at most, e 3; the sum of terms 3 and (on average over their shares, at most ln 1024) 7 off, and its
-// EPL + 6 additions; the inverse 1.1: less than 22 + EPL.  `apart`: those of two.  Of s = p + bias: 1 of itself more, of a sum of two 1 of each and of the sum (twice
-// that is asked for): a large bias of an expert that is out of reach does not count.
+// Errors of p, in units of 2^-24.  Sigmoid: e^-|l| is 3 of itself off, 1 + e 1, the inverse 1.1, the product for l < 0 1: 6.1 of p, and as p moves by p (1 - p) of what e
+// does, 2.9 of 1 however large p is.  Softmax, in parts of the row's largest p: l - top is off by 1 of itself and moves e by 0.4 at most, e 3; the sum of terms 3 and (on
+// average over their shares, at most ln 1024) 7 off, and its EPL + 6 additions; the inverse 1.1: less than 22 + EPL.  `apart`: those of two.  Of s = p + bias: 1 of itself
+// more, of a sum of two 1 of each and of the sum (twice that is asked for): a large bias of an expert that is out of reach does not count.
 template <int EPL>
 __device__ __forceinline__ int choose_quickly(const GroupedRouteArgs& a, const GroupedRow<EPL>& r, int& id) {
     const int lane = __lane_id(), within = lane - r.group * a.lanes;
@@ -235,7 +235,7 @@ __device__ __forceinline__ int choose_quickly(const GroupedRouteArgs& a, const G
     }
     largest = __uint_as_float(wave_max_u32(__float_as_uint(largest))) * per_total;
     if (__ballot(!number) || largest < 0x1p-100f) return kNotChosen;
-    const float apart = largest * (a.sigmoid ? 16.f : 2.f * (22 + EPL)) * 0x1p-24f;
+    const float apart = (a.sigmoid ? fminf(13.f * largest, 6.f) : 2.f * (22 + EPL) * largest) * 0x1p-24f;
     // a lane's experts in falling order (insertion, an element moves up past strictly smaller ones only)
 #pragma unroll
     for (int j = 1; j < EPL; ++j) {
