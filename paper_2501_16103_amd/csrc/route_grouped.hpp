@@ -198,44 +198,62 @@ enum { kChosen, kSetChosen, kNotChosen };
 // The choice in 32 bits.  kChosen: every two neighbours in its order, the first one left out, and the groups on either side of the border differ by more
 // than their errors, so 64 bits choose the same.  kSetChosen: the first k and the one behind them (in lane k) are the first k + 1, in some order.
 //
+// Without a bias scores rise with the logits, and those choose, exactly (equal scores go by the logits too); scores are needed only where a group's is a sum of two, and a
+// softmax's sum drops out of their order.  Groups of equal scores go by their index, so a border between groups has to lie where scores in 64 bits differ as logits do.
+//
 // Errors of p, in units of 2^-24.  Sigmoid: e^-|l| is 3 of itself off, 1 + e 1, the inverse 1.1, the product for l < 0 1: 6.1 of p, and as p moves by p (1 - p) of what e
 // does, 2.9 of 1 however large p is.  Softmax, in parts of the row's largest p: l - top is off by 1 of itself and moves e by 0.4 at most, e 3; the sum of terms 3 and (on
 // average over their shares, at most ln 1024) 7 off, and its EPL + 6 additions; the inverse 1.1: less than 22 + EPL.  `apart`: those of two.  Of s = p + bias: 1 of itself
-// more, of a sum of two 1 of each and of the sum (twice that is asked for): a large bias of an expert that is out of reach does not count.
+// more, of a sum of two 1 of each and of the sum (twice that is asked for): a large bias of an expert that is out of reach does not count.  Without a bias, of themselves: a
+// sigmoid 6.1, an exponential 3 and |x| < 88; 2^-17 is 128.
 template <int EPL>
 __device__ __forceinline__ int choose_quickly(const GroupedRouteArgs& a, const GroupedRow<EPL>& r, int& id) {
     const int lane = __lane_id(), within = lane - r.group * a.lanes;
+    const bool by_logit = a.bias == nullptr;
     uint32_t key[EPL];
     int expert[EPL];
-    float p[EPL], per_total = 1.f, largest = 0.f;
-    if (a.sigmoid) {
-#pragma unroll
-        for (int j = 0; j < EPL; ++j) {
-            const float e = exp_closely(-fabsf(r.logit[j])), inverse = inverse_closely(1.f + e);
-            p[j] = r.logit[j] < 0.f ? e * inverse : inverse;
-        }
-    } else {
-        float total = 0.f;
-#pragma unroll
-        for (int j = 0; j < EPL; ++j) {
-            p[j] = r.live >> j & 1 ? exp_closely(r.logit[j] - r.top) : 0.f;
-            total += p[j];
-        }
-        per_total = inverse_closely(wave_sum(total));
-    }
+    float apart = 0.f;
     bool number = true;
+    auto sigmoid = [&](float l) __attribute__((always_inline)) {
+        const float e = exp_closely(-fabsf(l)), inverse = inverse_closely(1.f + e);
+        return l < 0.f ? e * inverse : inverse;
+    };
+    if (by_logit) {
 #pragma unroll
-    for (int j = 0; j < EPL; ++j) {
-        const bool live = r.live >> j & 1;
-        const float s = fmaf(p[j], per_total, r.bias[j]), c = live ? p[j] : 0.f;
-        number = number & !(live & !(fabsf(s) <= 1e30f));   // (false for a NaN)
-        largest = c > largest ? c : largest;
-        key[j] = j >= r.count ? 0 : live ? score_key32(s) : 1;
-        expert[j] = r.first + j;
+        for (int j = 0; j < EPL; ++j) {
+            const bool live = r.live >> j & 1;
+            number = number & !(live & !(r.logit[j] <= 3.4e38f));   // (false for a NaN)
+            key[j] = j >= r.count ? 0 : live ? route_key(r.logit[j]) : 1;
+        }
+        if (__ballot(!number)) return kNotChosen;
+    } else {
+        float p[EPL], per_total = 1.f, largest = 0.f;
+        if (a.sigmoid) {
+#pragma unroll
+            for (int j = 0; j < EPL; ++j) p[j] = sigmoid(r.logit[j]);
+        } else {
+            float total = 0.f;
+#pragma unroll
+            for (int j = 0; j < EPL; ++j) {
+                p[j] = r.live >> j & 1 ? exp_closely(r.logit[j] - r.top) : 0.f;
+                total += p[j];
+            }
+            per_total = inverse_closely(wave_sum(total));
+        }
+#pragma unroll
+        for (int j = 0; j < EPL; ++j) {
+            const bool live = r.live >> j & 1;
+            const float s = fmaf(p[j], per_total, r.bias[j]), c = live ? p[j] : 0.f;
+            number = number & !(live & !(fabsf(s) <= 1e30f));
+            largest = c > largest ? c : largest;
+            key[j] = j >= r.count ? 0 : live ? score_key32(s) : 1;
+        }
+        largest = __uint_as_float(wave_max_u32(__float_as_uint(largest))) * per_total;
+        if (__ballot(!number) || largest < 0x1p-100f) return kNotChosen;
+        apart = (a.sigmoid ? fminf(13.f * largest, 6.f) : 2.f * (22 + EPL) * largest) * 0x1p-24f;
     }
-    largest = __uint_as_float(wave_max_u32(__float_as_uint(largest))) * per_total;
-    if (__ballot(!number) || largest < 0x1p-100f) return kNotChosen;
-    const float apart = (a.sigmoid ? fminf(13.f * largest, 6.f) : 2.f * (22 + EPL) * largest) * 0x1p-24f;
+#pragma unroll
+    for (int j = 0; j < EPL; ++j) expert[j] = r.first + j;
     // a lane's experts in falling order (insertion, an element moves up past strictly smaller ones only)
 #pragma unroll
     for (int j = 1; j < EPL; ++j) {
@@ -255,23 +273,14 @@ __device__ __forceinline__ int choose_quickly(const GroupedRouteArgs& a, const G
             one = o1 > one ? o1 : one;
             two = low > more ? low : more;
         };
-        uint32_t mine;
-        float size;                                  // what the group's score is added up from
-        auto group_score = [&]() __attribute__((always_inline)) {
-            const bool both = a.top2 && two > 1;
-            const float first = score_of_key32(one), second = score_of_key32(two);
-            size = one > 1 ? fabsf(first) + (both ? fabsf(second) : 0.f) : 0.f;
-            return both ? score_key32(first + second) : one;
-        };
         if (a.lanes <= 16 && (a.lanes & (a.lanes - 1)) == 0) {
-            // exchanges within 2, 4, 8 and 16 lanes; every lane of a group ends with its score
+            // exchanges within 2, 4, 8 and 16 lanes; every lane of a group ends with its two largest
 #define MOE_EXCHANGE(ctrl) merge((uint32_t)__builtin_amdgcn_update_dpp(0, (int)one, ctrl, 0xf, 0xf, false), (uint32_t)__builtin_amdgcn_update_dpp(0, (int)two, ctrl, 0xf, 0xf, false))
             if (a.lanes > 1) MOE_EXCHANGE(0xb1);     // quad_perm 1, 0, 3, 2
             if (a.lanes > 2) MOE_EXCHANGE(0x4e);     // quad_perm 2, 3, 0, 1
             if (a.lanes > 4) MOE_EXCHANGE(0x141);    // row_half_mirror
             if (a.lanes > 8) MOE_EXCHANGE(0x140);    // row_mirror
 #undef MOE_EXCHANGE
-            mine = group_score();
         } else {
             int width = 32;
             while (width >= a.lanes) width >>= 1;
@@ -280,8 +289,25 @@ __device__ __forceinline__ int choose_quickly(const GroupedRouteArgs& a, const G
                 if (within < width && within + width < a.lanes) merge(o1, o2);
             }
             const int leader = r.group < a.groups ? r.group * a.lanes : 0;
-            mine = (uint32_t)__shfl((int)group_score(), leader);
-            size = __shfl(size, leader);
+            one = (uint32_t)__shfl((int)one, leader);
+            two = (uint32_t)__shfl((int)two, leader);
+        }
+        uint32_t mine = one;                         // the group's score; at most 1: all of its experts are masked
+        float size = 0.f;                            // what it is added up from
+        const bool ranked = by_logit && !a.top2;     // by the largest logit
+        if (!ranked) {
+            float first, second;
+            if (by_logit) {
+                first = a.sigmoid ? sigmoid(route_logit(one)) : exp_closely(route_logit(one) - r.top);
+                second = two <= 1 ? 0.f : a.sigmoid ? sigmoid(route_logit(two)) : exp_closely(route_logit(two) - r.top);
+            } else {
+                first = score_of_key32(one);
+                second = a.top2 && two > 1 ? score_of_key32(two) : 0.f;
+            }
+            if (one > 1) {
+                mine = score_key32(first + second);
+                size = fabsf(first) + fabsf(second);
+            }
         }
         int above = 0;
         for (int g = 0; g < a.groups; ++g) above += (uint32_t)__builtin_amdgcn_readlane((int)mine, g * a.lanes) > mine;
@@ -290,9 +316,13 @@ __device__ __forceinline__ int choose_quickly(const GroupedRouteArgs& a, const G
         const uint32_t least = ~wave_max_u32(there && stays ? ~mine : 0), most = wave_max_u32(there && !stays ? mine : 0);
         const int staying = __popcll(__ballot(there && stays && within == 0));
         if (staying != a.kept) return kNotChosen;
-        if (most > 1) {                              // every group is on its side of the middle by more than its error
+        if (most > 1 && ranked) {
+            const float l = route_logit(least), m = route_logit(most);
+            if (!(l - m > 0x1p-20f && (a.sigmoid ? m > -600.f && m < 18.f : m - r.top > -600.f))) return kNotChosen;
+        } else if (most > 1) {                       // every group is on its side of the middle by more than its error
             const float middle = 0.5f * score_of_key32(least) + 0.5f * score_of_key32(most), from = score_of_key32(mine) - middle;
-            const bool told = !there || mine <= 1 || (stays ? from : -from) > apart + size * 0x1p-22f;
+            const float off = by_logit ? size * 0x1p-17f + 0x1p-100f : apart + size * 0x1p-22f;
+            const bool told = !there || mine <= 1 || (stays ? from : -from) > off;
             if (__ballot(!told)) return kNotChosen;
         }
         if (!stays) {
@@ -320,6 +350,7 @@ __device__ __forceinline__ int choose_quickly(const GroupedRouteArgs& a, const G
         now = wave_max_u32(key[0]);
     };
     for (int i = 0; i < a.k; ++i) take(i);
+    if (by_logit) return kChosen;
     if (lane == a.k) chosen = now;
     // masked ones (1) come last and in order of their experts, nothing (0) comes behind them
     const uint32_t before = (uint32_t)__shfl((int)chosen, lane > 0 ? lane - 1 : 0);
