@@ -40,6 +40,24 @@ def test_rows():
     assert bool(((codes - v).abs() <= ref.half_step(v) * (1 + 2.0 ** -20) + v.abs() * 2.0 ** -22).all())
 
 
+def test_more_rows_than_a_launch():
+    T, H = (1 << 22) + 4099, 9
+    g = torch.Generator().manual_seed(6)
+    x = torch.zeros(T, H, dtype=BF16, device=DEV)
+    places = torch.cat([torch.arange(0, 3), torch.arange((1 << 22) - 4, (1 << 22) + 4), torch.arange(T - 3, T)])
+    some = torch.randn(len(places), H, generator=g).to(BF16)
+    x[places.to(DEV)] = some.to(DEV)
+    y, rows = torch.empty(T, H, dtype=BF16, device=DEV), mb.Fp8Rows(T, H, DEV)
+    mb.moe_add_norm(x, None, 1e-6, y=y, rows=rows)
+    _, want = ref.add_norm(some, None, None, 1e-6)
+    at = places.to(DEV)
+    assert bool(((y[at].cpu().double() - want).abs() <= want.abs() * (2.0 ** -8 + 32 * 2.0 ** -24)).all())
+    assert int((y != 0).any(1).sum()) == len(places) and int((rows.codes != 0).any(1).sum()) == len(places)
+    rows.codes.fill_(1)
+    rows.quantize(x)
+    assert torch.equal(rows.scales[at].cpu(), some.float().abs().amax(1) / 448.0) and int((rows.codes != 0).any(1).sum()) == len(places)
+
+
 def test_logits_far_apart():
     wide = torch.empty(1100, 1 << 22, dtype=BF16, device=DEV)
     assert wide.numel() > 1 << 32

@@ -80,6 +80,16 @@ def test_gated(T, K, N):
         _check(x, q, s, z, group, gated=True, add=_tokens(T, N // 2, 78))
 
 
+@pytest.mark.parametrize("T,K,N,gated", [(1, 300, 4640, False), (7, 129, 4700, False), (16, 256, 5000, False), (8, 257, 12304, False), (16, 300, 12304, False), (9, 128, 12290, True),
+                                         (1, 300, 16400, False), (6, 640, 16386, False), (16, 130, 16500, False), (1, 1100, 16420, True), (5, 96, 16402, True), (13, 264, 16400, True)])
+def test_many_columns(T, K, N, gated):
+    """Workgroups of two and of four tiles of columns, the last of which may not have all of them."""
+    for group, zeros in ((32, True), (64, False), (128, True)):
+        q, s, z = _weight(K, N, group, K + N, zeros)
+        x = _tokens(T, K, T + 2)
+        _check(x, q, s, z, group, gated=gated, add=_tokens(T, N // 2 if gated else N, 79) if group == 64 else None)
+
+
 def test_layouts_give_the_same():
     q, s, z = _weight(520, 70, 64, 3)
     x = _tokens(6, 520, 4)
