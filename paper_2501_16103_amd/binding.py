@@ -815,10 +815,7 @@ class MoeFewTokensPlan:
 
 
 _current_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
-
-
-def _stream_at(device: int) -> int:
-    return _raw_stream(device) if _raw_stream is not None else torch.cuda.current_stream(device).cuda_stream
+_stream_at = _raw_stream if _raw_stream is not None else lambda device: torch.cuda.current_stream(device).cuda_stream
 
 
 def _here(*tensors) -> bool:
@@ -827,7 +824,21 @@ def _here(*tensors) -> bool:
     return not at or (len(at) == 1 and min(at) >= 0 and min(at) == _current_device())
 
 
-# (The calls of a token's step look at devices in place: what they cost is their host side.)
+# (The C entry points take sizes of 32 bits; the calls refuse what does not fit, where ctypes would cut it off.)
+# The calls below are made once or more for every token generated, and what they cost is their host side: they look at their tensors in place, and a
+# description of sizes, types and options is made once for each combination (never changed then, so calls of several threads may share it).
+_MOST_DESCRIPTIONS = 4096
+_descriptions: dict = {}
+
+
+def _described(kind, *fields):
+    """A pointer to kind(*fields)."""
+    if len(_descriptions) >= _MOST_DESCRIPTIONS:
+        _descriptions.clear()
+    d = _descriptions[(kind, *fields)] = ctypes.byref(kind(*fields))
+    return d
+
+
 def moe_route_grouped(logits: torch.Tensor, k: int, topk_ids: torch.Tensor, topk_weights: torch.Tensor, groups: int, kept: int,
                       group_score: int = MOE_GROUP_MAX, bias: Optional[torch.Tensor] = None, score: int = MOE_SCORE_SOFTMAX, renormalize: bool = True,
                       scale: float = 1.0, check: bool = True) -> int:
@@ -839,10 +850,10 @@ def moe_route_grouped(logits: torch.Tensor, k: int, topk_ids: torch.Tensor, topk
     if (topk_ids.numel() >= n and topk_weights.numel() >= n and topk_ids.dtype is torch.int32 and topk_weights.dtype is torch.float32 and
             topk_ids.is_contiguous() and topk_weights.is_contiguous() and (step == 1 or E <= 1) and
             (bias is None or (_holds(bias, E, torch.float32) and bias.get_device() == at)) and
-            topk_ids.get_device() == at and topk_weights.get_device() == at and at >= 0 and at == _current_device()):
-        d = moe_route_desc(T, k, E, _DTYPES.get(logits.dtype, -1), row, score, renormalize, scale)
-        rc = lib().moe_route_grouped(logits.data_ptr(), None if bias is None else bias.data_ptr(), ctypes.byref(d), groups, kept, group_score,
-                                     topk_ids.data_ptr(), topk_weights.data_ptr(), _stream_at(at))
+            topk_ids.get_device() == at and topk_weights.get_device() == at and at >= 0 and at == _current_device() and (n | E) >> 31 == 0):
+        fields = (moe_route_desc, T, k, E, _DTYPES.get(logits.dtype, -1), row, score, renormalize, scale)
+        rc = (_lib or lib()).moe_route_grouped(logits.data_ptr(), None if bias is None else bias.data_ptr(), _descriptions.get(fields) or _described(*fields),
+                                               groups, kept, group_score, topk_ids.data_ptr(), topk_weights.data_ptr(), _stream_at(at))
     if check and rc != MOE_OK:
         raise MoeError(rc, "moe_route_grouped")
     return rc
@@ -870,8 +881,8 @@ def moe_fp8_quantize(src: torch.Tensor, out: Fp8Rows, check: bool = True) -> int
     row, step = src.stride()
     at = src.get_device()
     rc = MOE_ERR_INVALID_ARG
-    if rows <= out.rows and cols == out.cols and (step == 1 or cols <= 1) and at >= 0 and out.codes.get_device() == at and at == _current_device():
-        rc = lib().moe_fp8_quantize(src.data_ptr(), _DTYPES.get(src.dtype, -1), rows, cols, row, out.codes.data_ptr(), out.scales.data_ptr(), _stream_at(at))
+    if rows <= out.rows and cols == out.cols and cols >> 31 == 0 and (step == 1 or cols <= 1) and at >= 0 and out.codes.get_device() == at and at == _current_device():
+        rc = (_lib or lib()).moe_fp8_quantize(src.data_ptr(), _DTYPES.get(src.dtype, -1), rows, cols, row, out.codes.data_ptr(), out.scales.data_ptr(), _stream_at(at))
     if check and rc != MOE_OK:
         raise MoeError(rc, "moe_fp8_quantize")
     return rc
@@ -884,11 +895,12 @@ def moe_add_norm(x: torch.Tensor, weight: Optional[torch.Tensor], eps: float, re
     T, H = shape = x.shape
     x_row, x_step = x.stride()
     n, at = T * H, x.get_device()
-    fits = (x_step == 1 or H <= 1) and at >= 0 and at == _current_device()
+    fits = (x_step == 1 or H <= 1) and H >> 31 == 0 and at >= 0 and at == _current_device()
     x_type = w_type = r_type = _DTYPES.get(x.dtype, -1)
-    r_row, w, r, r_out, y_at, codes, scales = 0, None, None, None, None, None, None
+    r_row = 0
+    w = r = r_out = y_at = codes = scales = None
     if weight is not None:
-        fits = fits and weight.numel() == H and weight.dim() == 1 and weight.is_contiguous() and weight.get_device() == at
+        fits = fits and weight.shape == (H,) and weight.is_contiguous() and weight.get_device() == at
         w, w_type = weight.data_ptr(), _DTYPES.get(weight.dtype, -1)
     if residual is not None:
         r_row, r_step = residual.stride()
@@ -902,12 +914,13 @@ def moe_add_norm(x: torch.Tensor, weight: Optional[torch.Tensor], eps: float, re
         fits = fits and y.dtype is torch.bfloat16 and y.numel() >= n and y.is_contiguous() and y.get_device() == at
         y_at = y.data_ptr()
     if rows is not None:
-        fits = fits and T <= rows.rows and rows.cols == H and rows.codes.get_device() == at
-        codes, scales = rows.codes.data_ptr(), rows.scales.data_ptr()
+        out = rows.codes
+        fits = fits and T <= rows.rows and rows.cols == H and out.get_device() == at
+        codes, scales = out.data_ptr(), rows.scales.data_ptr()
     rc = MOE_ERR_INVALID_ARG
     if fits:
-        d = moe_norm_desc(T, x_row, r_row, H, x_type, r_type, w_type, eps)
-        rc = lib().moe_add_norm(x.data_ptr(), r, w, ctypes.byref(d), r_out, y_at, codes, scales, _stream_at(at))
+        fields = (moe_norm_desc, T, x_row, r_row, H, x_type, r_type, w_type, eps)
+        rc = (_lib or lib()).moe_add_norm(x.data_ptr(), r, w, _descriptions.get(fields) or _described(*fields), r_out, y_at, codes, scales, _stream_at(at))
     if check and rc != MOE_OK:
         raise MoeError(rc, "moe_add_norm")
     return rc
@@ -962,15 +975,15 @@ def moe_w4_matvec(X: torch.Tensor, W: W4Weights, out: torch.Tensor, add: Optiona
     """X bf16 [T, W.K], T <= 16, rows of consecutive elements -> out bf16 [T, W.N, or W.N / 2 of gated weights], with `add` (of its shape) added."""
     T, K = X.shape
     row, step = X.stride()
-    gated, at = W.gated, X.get_device()
+    gated, codes, at = W.gated, W.codes, X.get_device()
     n = T * (W.N // 2 if gated else W.N)
     rc = MOE_ERR_INVALID_ARG
     if (K == W.K and X.dtype is torch.bfloat16 and (step == 1 or K <= 1) and out.dtype is torch.bfloat16 and out.numel() >= n and out.is_contiguous() and
             (add is None or (_holds(add, n, torch.bfloat16) and add.get_device() == at)) and
-            W.codes.get_device() == at and out.get_device() == at and at >= 0 and at == _current_device()):
-        d = moe_w4_desc(T, K, W.N, W.group, gated)
-        rc = lib().moe_w4_matvec(X.data_ptr(), row, W.codes.data_ptr(), W.words.data_ptr(), ctypes.byref(d), None if add is None else add.data_ptr(),
-                                 out.data_ptr(), _stream_at(at))
+            codes.get_device() == at and out.get_device() == at and at >= 0 and at == _current_device() and T >> 31 == 0):
+        fields = (moe_w4_desc, T, K, W.N, W.group, gated)
+        rc = (_lib or lib()).moe_w4_matvec(X.data_ptr(), row, codes.data_ptr(), W.words.data_ptr(), _descriptions.get(fields) or _described(*fields),
+                                           None if add is None else add.data_ptr(), out.data_ptr(), _stream_at(at))
     if check and rc != MOE_OK:
         raise MoeError(rc, "moe_w4_matvec")
     return rc

@@ -103,3 +103,16 @@ def test_tokens_far_apart():
     mb.moe_w4_matvec(wide[:, :256], W, out)
     mb.moe_w4_matvec(x.to(DEV), W, near)
     assert torch.equal(out, near)
+
+
+def test_sizes_beyond_32_bits_are_refused():
+    """A row of 2^32 + 64 elements is not one of 64, and 2^32 + 8 rows are not 8."""
+    row = torch.empty(1, (1 << 32) + 64, dtype=BF16, device=DEV)
+    ids, w = torch.empty(1, 2, dtype=torch.int32, device=DEV), torch.empty(1, 2, device=DEV)
+    y = torch.empty(1, 64, dtype=BF16, device=DEV)
+    assert mb.moe_route_grouped(row, 2, ids, w, 8, 4, check=False) == mb.MOE_ERR_INVALID_ARG
+    assert mb.moe_add_norm(row, None, 1e-6, y=row, check=False) == mb.MOE_ERR_INVALID_ARG
+    assert mb.moe_add_norm(row[:, :64], None, 1e-6, y=y, check=False) == mb.MOE_OK
+    column = row.reshape(-1, 1)[: (1 << 32) + 8]
+    W = mb.W4Weights(1, 1, 32, device=DEV)
+    assert mb.moe_w4_matvec(column, W, column, check=False) == mb.MOE_ERR_INVALID_ARG
