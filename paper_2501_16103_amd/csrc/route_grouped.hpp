@@ -72,6 +72,22 @@ __device__ __forceinline__ double route_probability(float l, bool sigmoid, float
     return exp((double)l - (double)top) * scale;
 }
 
+// The same for weights, which are rounded to 32 bits: off by 2^-40 of itself instead of 2^-52.  e^x by its series on either side of 0, up to ln 2 / 2: the first term left out
+// is 0.347^11 / 11! = 2^-42.  (Below -760 e^x is 0; a NaN stays one.)
+__device__ __forceinline__ double exp_near(double x) {
+    x = x < -760. ? -760. : x;
+    const double n = rint(x * 1.4426950408889634), r = fma(n, -0.69314718055994531, x);
+    double s = 1. / 3628800.;
+    s = fma(s, r, 1. / 362880.); s = fma(s, r, 1. / 40320.); s = fma(s, r, 1. / 5040.); s = fma(s, r, 1. / 720.); s = fma(s, r, 1. / 120.);
+    s = fma(s, r, 1. / 24.); s = fma(s, r, 1. / 6.); s = fma(s, r, 0.5); s = fma(s, r, 1.); s = fma(s, r, 1.);
+    return __builtin_amdgcn_ldexp(s, (int)n);
+}
+__device__ __forceinline__ double weight_probability(float l, bool sigmoid, float top, double scale) {
+    if (!sigmoid) return exp_near((double)l - (double)top) * scale;
+    const double x = 1. + exp_near(-(double)(l < kSigmoidNone ? kSigmoidNone : l)), about = __builtin_amdgcn_rcp(x);   // (off by 2^-23 of itself)
+    return l < kSigmoidNone ? 0. : fma(fma(-x, about, 1.), about, about);
+}
+
 // A lane's experts: `lanes` neighbouring lanes hold a group, EPL consecutive experts each, so that lanes and experts rise together.
 template <int EPL>
 struct GroupedRow {
@@ -310,16 +326,18 @@ __device__ __forceinline__ int choose_quickly(const GroupedRouteArgs& a, const G
             }
         }
         int above = 0;
-        for (int g = 0; g < a.groups; ++g) above += (uint32_t)__builtin_amdgcn_readlane((int)mine, g * a.lanes) > mine;
+        for (int g = 0; g < a.groups; ++g) {
+            const uint32_t other = (uint32_t)__builtin_amdgcn_readlane((int)mine, g * a.lanes);
+            above += (other > mine) | ((other == mine) & (g < r.group));
+        }
         const bool there = r.group < a.groups, stays = above < a.kept;
-        // (equal scores: all of them stay, or none does, and the numbers below do not add up)
-        const uint32_t least = ~wave_max_u32(there && stays ? ~mine : 0), most = wave_max_u32(there && !stays ? mine : 0);
-        const int staying = __popcll(__ballot(there && stays && within == 0));
-        if (staying != a.kept) return kNotChosen;
-        if (most > 1 && ranked) {
-            const float l = route_logit(least), m = route_logit(most);
-            if (!(l - m > 0x1p-20f && (a.sigmoid ? m > -600.f && m < 18.f : m - r.top > -600.f))) return kNotChosen;
+        const uint32_t most = wave_max_u32(there && !stays ? mine : 0);
+        if (most > 1 && ranked) {                    // (equal logits have equal scores, which go by their index; others have to have scores that differ)
+            const float m = route_logit(most), v = route_logit(mine);
+            const bool told = !there || mine <= 1 || v == m || fabsf(v - m) > 0x1p-20f;
+            if (__ballot(!told) || !(a.sigmoid ? m > -600.f && m < 18.f : m - r.top > -600.f)) return kNotChosen;
         } else if (most > 1) {                       // every group is on its side of the middle by more than its error
+            const uint32_t least = ~wave_max_u32(there && stays ? ~mine : 0);
             const float middle = 0.5f * score_of_key32(least) + 0.5f * score_of_key32(most), from = score_of_key32(mine) - middle;
             const float off = by_logit ? size * 0x1p-17f + 0x1p-100f : apart + size * 0x1p-22f;
             const bool told = !there || mine <= 1 || (stays ? from : -from) > off;
@@ -430,15 +448,16 @@ __global__ __launch_bounds__(256) void route_grouped_kernel(GroupedRouteArgs a, 
         }
         r.top = route_logit(wave_max_u32(first));
     }
-    double per_total = 0.;
-    bool summed = false;
-    auto sum_up = [&]() __attribute__((always_inline)) {
-        if (a.sigmoid || summed) return;
+    double per_total = 1.;                           // of a softmax: 1 / sum
+    bool summed = a.sigmoid;
+    auto sum_up = [&](auto probability) __attribute__((always_inline)) {
+        if (summed) return;
         double total = 0.;
 #pragma unroll
         for (int j = 0; j < EPL; ++j) {
-            total += r.live >> j & 1 ? route_probability(r.logit[j], false, r.top, 1.) : 0.;
-            if (EPL > 4) __builtin_amdgcn_sched_barrier(0);
+            const double p = probability(r.live >> j & 1 ? r.logit[j] : -__builtin_inff(), false, r.top, 1.);
+            total += p;
+            if (EPL > 8) __builtin_amdgcn_sched_barrier(0);
         }
         per_total = 1. / wave_sum_f64(total);
         summed = true;
@@ -453,7 +472,7 @@ __global__ __launch_bounds__(256) void route_grouped_kernel(GroupedRouteArgs a, 
         if constexpr (EPL <= 16) {
             if (a.k < 63) seen = choose_quickly<EPL>(a, r, id);
         }
-        if (seen != kChosen) sum_up();
+        if (seen != kChosen) sum_up(route_probability);
         if (seen == kSetChosen) {
             const int e = id < 0 || lane > a.k ? 0 : id;
             id = put_in_order(a, id, load_value(row + e), a.bias ? a.bias[e] : 0.f, r.top, per_total);
@@ -461,12 +480,10 @@ __global__ __launch_bounds__(256) void route_grouped_kernel(GroupedRouteArgs a, 
             choose_exactly<EPL>(a, r, per_total, id, ids_row);
         }
     }
-    // Renormalised weights are quotients in which a softmax's sum drops out.
-    if (!a.renormalize) sum_up();
-    else if (!summed) per_total = 1.;
+    if (!a.renormalize) sum_up(weight_probability);  // (renormalised weights are quotients, in which a softmax's sum drops out)
     auto weight = [&](int e) {
         const float l = load_value(row + e), bias = a.bias ? a.bias[e] : 0.f;
-        const double p = route_probability(l, a.sigmoid, r.top, per_total);
+        const double p = weight_probability(l, a.sigmoid, r.top, per_total);
         return (l != -__builtin_inff()) & (bias != -__builtin_inff()) ? p : 0.;
     };
     const double w = lane < a.k ? weight(id) : 0.;
