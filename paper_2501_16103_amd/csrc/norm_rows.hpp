@@ -8,7 +8,7 @@
 // A row with an infinity or a NaN (in h or in y) has the scale NaN and codes of NaN.
 //
 // What bounds it: memory, with many rows (4096 rows of 7168 with all outputs, 264 MB, 48.6 us, 5.4 TB/s read and written; 8192 rows of 14336 alone 61.2 us, 5.8 TB/s; a large
-// copy: 5.15); with few the launch and one chain of load, two exchanges and store (one row of 2048: 2.5 us back to back, 6.3 with the call's own time).  Rows of an odd
+// copy: 5.15); with few the launch and one chain of load, two exchanges and store (one row of 2048: 2.5 us back to back, 6.8 with the call's own time).  Rows of an odd
 // length begin anywhere; with pieces on multiples of eight of the whole tensor all accesses but those at a row's ends are aligned (2529 rows of 5143, bf16 with an fp32 weight,
 // all outputs, 30.7 us, of 5144 29.0; with pieces counted from the row's beginning 43.3).  Elements are held as they are stored, bf16 by
 // twos, until they are used: as floats, 4096 rows of 7168 took 64.6.

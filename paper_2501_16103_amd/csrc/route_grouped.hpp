@@ -10,8 +10,8 @@
 // It is made in 32 bits, whose scores are off by a few roundings, and most rows show that 64 bits would choose the same (choose_quickly).  Where neighbours in the
 // order are too near to tell, their scores in 64 bits put them in order (of 8192 tokens with 256 experts two); where the border of the groups or of the set
 // is, the whole choice is made again in 64 bits (one row in 26 000).  What bounds it: few tokens, the launch and a chain of k + 5 maxima and two 64-bit exponentials (one token, 6 of
-// 64: 3.6 us, 5.2 with the call's own time); many, the issue of vector instructions: 8192 tokens, 8 of 256 in 8 groups of which 4 stay, sigmoid, bias, are 655 of them a wavefront,
-// eight wavefronts a SIMD, 8.7 of the 10.3 us, 11 to 13 where one of the rows is chosen in 64 bits (in 64 bits throughout 18.0).
+// 64: 3.4 us, 5.2 with the call's own time); many, the issue of vector instructions: 8192 tokens, 8 of 256 in 8 groups of which 4 stay, sigmoid, bias, are 650 of them a wavefront,
+// eight wavefronts a SIMD, 8.6 of the 10.3 us, 11 to 13 where one of the rows is chosen in 64 bits (in 64 bits throughout 18.0).
 #pragma once
 #include <hip/hip_runtime.h>
 #include <stdint.h>
