@@ -21,12 +21,22 @@ bool misaligned(const void* p, int bytes) { return ((uintptr_t)p & (bytes - 1)) 
 int bytes_of(int dtype) { return dtype == MOE_DTYPE_FP32 ? 4 : 2; }
 bool fp32_or_bf16(int dtype) { return dtype == MOE_DTYPE_FP32 || dtype == MOE_DTYPE_BF16; }
 
-template <int EPL>
+template <int EPL, bool TOGETHER>
 int launch_grouped(const GroupedRouteArgs& a, bool f32, int32_t* ids, float* weights, hipStream_t s) {
     const dim3 grid((a.T + 3) / 4);
-    if (f32) route_grouped_kernel<EPL, float><<<grid, 256, 0, s>>>(a, ids, weights);
-    else route_grouped_kernel<EPL, uint16_t><<<grid, 256, 0, s>>>(a, ids, weights);
+    if (f32) route_grouped_kernel<EPL, float, TOGETHER><<<grid, 256, 0, s>>>(a, ids, weights);
+    else route_grouped_kernel<EPL, uint16_t, TOGETHER><<<grid, 256, 0, s>>>(a, ids, weights);
     return launched();
+}
+// Weights of four tokens by one wavefront where a sigmoid's have to be made, from two workgroups on.  us, each by its own / together, sigmoid, bias, 8 of 256, 4 of 8 groups:
+// 64 tokens 4.96 / 4.74, 1024 5.00 / 4.86, 8192 10.7 / 9.8 (a third of that for a softmax's part not being there); 6 of 64 in one group 700 3.38 / 3.18, 4096 4.35 / 4.17, 16384
+// 11.0 / 9.8.  One token 4.42 / 4.60 (a barrier for nothing); softmax, 8 of 128 10.26 / 10.47, 6 of 72 9.27 / 9.31; eight experts a lane 9.07 / 9.12.
+template <int EPL>
+int launch_grouped(const GroupedRouteArgs& a, bool f32, int32_t* ids, float* weights, hipStream_t s) {
+    if constexpr (EPL <= 4) {
+        if (a.sigmoid && a.k <= 16 && a.T > 4) return launch_grouped<EPL, true>(a, f32, ids, weights, s);
+    }
+    return launch_grouped<EPL, false>(a, f32, ids, weights, s);
 }
 
 constexpr int kNormCols = 65536;

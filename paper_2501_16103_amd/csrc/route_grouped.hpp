@@ -10,8 +10,8 @@
 // It is made in 32 bits, whose scores are off by a few roundings, and most rows show that 64 bits would choose the same (choose_quickly).  Where neighbours in the
 // order are too near to tell, their scores in 64 bits put them in order (of 8192 tokens with 256 experts two); where the border of the groups or of the set
 // is, the whole choice is made again in 64 bits (one row in 26 000).  What bounds it: few tokens, the launch and a chain of k + 5 maxima and two 64-bit exponentials (one token, 6 of
-// 64: 3.4 us, 5.2 with the call's own time); many, the issue of vector instructions: 8192 tokens, 8 of 256 in 8 groups of which 4 stay, sigmoid, bias, are 650 of them a wavefront,
-// eight wavefronts a SIMD, 8.6 of the 10.3 us, 11 to 13 where one of the rows is chosen in 64 bits (in 64 bits throughout 18.0).
+// 64: 3.4 us, 5.2 with the call's own time); many, the issue of vector instructions: 8192 tokens, 8 of 256 in 8 groups of which 4 stay, sigmoid, bias, are 578 of them a wavefront,
+// eight wavefronts a SIMD, 7.7 of the 9.8 us, 11 to 12 where one of the rows is chosen in 64 bits (in 64 bits throughout 18.0).
 #pragma once
 #include <hip/hip_runtime.h>
 #include <stdint.h>
@@ -60,6 +60,21 @@ __device__ __forceinline__ double wave_sum_f64(double v) {
     const uint64_t b = (uint64_t)__double_as_longlong(v);
     const uint32_t lo = (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)b, 63), hi = (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)(b >> 32), 63);
     return __longlong_as_double((long long)((uint64_t)hi << 32 | lo));
+}
+// Over each sixteen lanes, in all of them.
+__device__ __forceinline__ double row_sum_f64(double v) {
+    auto step = [&](auto ctrl) __attribute__((always_inline)) {
+        const uint64_t b = (uint64_t)__double_as_longlong(v);
+        const uint32_t lo = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)(uint32_t)b, decltype(ctrl)::value, 0xf, 0xf, false);
+        const uint32_t hi = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)(uint32_t)(b >> 32), decltype(ctrl)::value, 0xf, 0xf, false);
+        v += __longlong_as_double((long long)((uint64_t)hi << 32 | lo));
+    };
+    using std::integral_constant;
+    step(integral_constant<int, 0xb1>{});            // quad_perm 1, 0, 3, 2
+    step(integral_constant<int, 0x4e>{});            // quad_perm 2, 3, 0, 1
+    step(integral_constant<int, 0x141>{});           // row_half_mirror
+    step(integral_constant<int, 0x140>{});           // row_mirror
+    return v;
 }
 __device__ __forceinline__ uint64_t shfl_u64(uint64_t v, int lane) {
     const uint32_t lo = (uint32_t)__shfl((int)(uint32_t)v, lane), hi = (uint32_t)__shfl((int)(uint32_t)(v >> 32), lane);
@@ -405,11 +420,18 @@ __device__ __forceinline__ int put_in_order(const GroupedRouteArgs& a, int id, f
     return __builtin_amdgcn_ds_permute(4 * (lane <= a.k ? rank : lane), id);
 }
 
-// A wavefront per token, four tokens a workgroup.
-template <int EPL, class Src>
+// A wavefront per token, four tokens a workgroup.  TOGETHER (sigmoid, k <= 16): the weights of all four, sixteen lanes each, are the work of one of the wavefronts; 64-bit instructions
+// for eight lanes of each cost as much as for all 64.
+template <int EPL, class Src, bool TOGETHER>
 __global__ __launch_bounds__(256) void route_grouped_kernel(GroupedRouteArgs a, int32_t* __restrict__ ids, float* __restrict__ weights) {
-    const int64_t t = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
-    if (t >= a.T) return;
+    if constexpr (TOGETHER) a.sigmoid = 1;           // (known here, so that a softmax's part falls away)
+    const int wave = threadIdx.x >> 6;
+    int64_t t = (int64_t)blockIdx.x * 4 + wave;
+    const bool token = t < a.T;
+    if (!token) {
+        if (!TOGETHER) return;
+        t = a.T - 1;                                 // (this one waits with the others)
+    }
     const int lane = __lane_id();
     const Src* row = static_cast<const Src*>(a.logits) + t * a.row_stride;
     GroupedRow<EPL> r;
@@ -481,6 +503,29 @@ __global__ __launch_bounds__(256) void route_grouped_kernel(GroupedRouteArgs a, 
         }
     }
     if (!a.renormalize) sum_up(weight_probability);  // (renormalised weights are quotients, in which a softmax's sum drops out)
+    if constexpr (TOGETHER) {
+        __shared__ float chosen[4][16];              // logits, -inf of masked ones
+        if (token && lane < a.k) {
+            const float l = load_value(row + id), bias = a.bias ? a.bias[id] : 0.f;
+            ids_row[lane] = id;
+            chosen[wave][lane] = bias == -__builtin_inff() ? bias : l;
+        }
+        __syncthreads();
+        const unsigned b = blockIdx.x, turn = b ^ b >> 2 ^ b >> 4 ^ b >> 6 ^ b >> 8 ^ b >> 10;
+        if (wave != (int)(turn & 3)) return;         // (not always the same one: a workgroup's first may always be on the same SIMD)
+        const int of = lane >> 4, i = lane & 15;
+        const int64_t mine = (int64_t)blockIdx.x * 4 + of;
+        const bool there = mine < a.T && i < a.k;
+        const float l = there ? chosen[of][i] : -__builtin_inff();
+        double w = weight_probability(l, true, 0.f, 1.);
+        w = l == -__builtin_inff() ? 0. : w;
+        if (a.renormalize) {
+            const double sum = row_sum_f64(w);
+            w = sum == 0. ? 0. : w / sum;
+        }
+        if (there) weights[mine * a.k + i] = (float)(w * (double)a.scale);
+        return;
+    }
     auto weight = [&](int e) {
         const float l = load_value(row + e), bias = a.bias ? a.bias[e] : 0.f;
         const double p = weight_probability(l, a.sigmoid, r.top, per_total);

@@ -65,6 +65,17 @@ def test_many_tokens():
     _check(x.to(DEV), x, 6, 8, 3, True, bias, True, True, 2.5)
 
 
+@pytest.mark.parametrize("T", [4, 5, 6, 7, 8])
+@pytest.mark.parametrize("k", [1, 15, 16, 17])
+@pytest.mark.parametrize("E", [64, 120, 256, 512])
+def test_four_tokens_of_a_workgroup(T, k, E):
+    """Every number of tokens in the last workgroup, choices on either side of a quarter of the lanes."""
+    for kind in ("normal", "masked"):
+        x, bias = _inputs(T, E, T * 100 + k, torch.float32, kind)
+        for renormalize in (False, True):
+            _check(x.to(DEV), x, k, 4, 3, True, bias, True, renormalize, 2.5)
+
+
 @pytest.mark.parametrize("spread", [1e-9, 1e-4, 1.0, 30.0, 300.0])
 @pytest.mark.parametrize("shift", [-650.0, -40.0, 0.0, 15.0, 40.0])
 def test_flat_and_peaked_rows_without_a_bias(spread, shift):
