@@ -257,7 +257,8 @@ __global__ __launch_bounds__(THREADS) void norm_rows_kernel(NormArgs a) {
     bool wide = false;                               // squares or products that leave fp32: the same in 64 bits
     double factor64 = 0.;
     if constexpr (NORM) {
-        if (squares >= 1e-25f && squares <= 1e37f && largest <= 1e37f) {
+        // (the largest product below 1e-30: it and those next to it have lost bits, though y may have all of its own; a zero comes here too, of a weight of zeros or lost as a whole)
+        if (squares >= 1e-25f && squares <= 1e37f && largest >= 1e-30f && largest <= 1e37f) {
             factor = 1.f / sqrtf(squares / (float)a.cols + a.eps);
             largest *= factor;
         } else {

@@ -90,6 +90,17 @@ def test_ranges(kind, eps, H):
     _check(_rows(5, H, 6, BF16, kind), _rows(5, H, 8, BF16, kind), None, eps=eps)
 
 
+@pytest.mark.parametrize("H", [100, 1024, 7168])
+@pytest.mark.parametrize("w_size", [1e-32, 1e-31, 1e-29])
+@pytest.mark.parametrize("eps", [0.0, 1e-24])
+def test_products_below_fp32(H, w_size, eps):
+    """h in range, its products with the weight below fp32's normal numbers (hardly a bit of them left at 1e-32), y in range again.  Scales are above 1e-35, of which a last
+    bit of fp32 is 2^-32: the roundings of a small y, of its quotient and of that one's remainder stay below the 2^-30 that the least half step is widened by."""
+    w = _rows(1, H, 26, F32)[0] * w_size
+    _check(_rows(5, H, 27, F32) * 2e-13, None, w, eps=eps)
+    _check((_rows(5, H, 28, BF16).float() * 2e-13).to(BF16), _rows(5, H, 29, F32) * 2e-13, w, eps=eps)
+
+
 def test_not_finite():
     x, w = _rows(6, 264, 9, BF16), _rows(1, 264, 10, F32)[0]
     x[1, 3], x[2, 263], x[4, 0] = float("nan"), float("inf"), -float("inf")
