@@ -824,8 +824,12 @@ def _here(*tensors) -> bool:
     return not at or (len(at) == 1 and min(at) >= 0 and min(at) == _current_device())
 
 
-# (The C entry points take sizes of 32 bits; the calls refuse what does not fit, where ctypes would cut it off.)
-# The calls below are made once or more for every token generated, and what they cost is their host side: they look at their tensors in place, and a
+def _int32(*values) -> bool:
+    """Whether all of these reach the library as they are: its sizes and options have 32 bits, and ctypes would cut off what does not fit."""
+    return all(-1 << 31 <= v < 1 << 31 for v in values)
+
+
+# The calls below are made once or more for every token generated, and what they cost is their host side: they look at their tensors and sizes in place, and a
 # description of sizes, types and options is made once for each combination (never changed then, so calls of several threads may share it).
 _MOST_DESCRIPTIONS = 4096
 _descriptions: dict = {}
@@ -850,7 +854,8 @@ def moe_route_grouped(logits: torch.Tensor, k: int, topk_ids: torch.Tensor, topk
     if (topk_ids.numel() >= n and topk_weights.numel() >= n and topk_ids.dtype is torch.int32 and topk_weights.dtype is torch.float32 and
             topk_ids.is_contiguous() and topk_weights.is_contiguous() and (step == 1 or E <= 1) and
             (bias is None or (_holds(bias, E, torch.float32) and bias.get_device() == at)) and
-            topk_ids.get_device() == at and topk_weights.get_device() == at and at >= 0 and at == _current_device() and (n | E) >> 31 == 0):
+            topk_ids.get_device() == at and topk_weights.get_device() == at and at >= 0 and at == _current_device() and
+            (n | E | k | groups | kept | group_score | score) >> 31 == 0):
         fields = (moe_route_desc, T, k, E, _DTYPES.get(logits.dtype, -1), row, score, renormalize, scale)
         rc = (_lib or lib()).moe_route_grouped(logits.data_ptr(), None if bias is None else bias.data_ptr(), _descriptions.get(fields) or _described(*fields),
                                                groups, kept, group_score, topk_ids.data_ptr(), topk_weights.data_ptr(), _stream_at(at))
@@ -927,11 +932,11 @@ def moe_add_norm(x: torch.Tensor, weight: Optional[torch.Tensor], eps: float, re
 
 
 def moe_w4_code_bytes(K: int, N: int, gated: bool = False) -> int:
-    return int(lib().moe_w4_code_bytes(K, N, int(gated)))
+    return int(lib().moe_w4_code_bytes(K, N, int(gated))) if _int32(K, N, int(gated)) else 0
 
 
 def moe_w4_word_bytes(K: int, N: int, group: int, gated: bool = False) -> int:
-    return int(lib().moe_w4_word_bytes(K, N, group, int(gated)))
+    return int(lib().moe_w4_word_bytes(K, N, group, int(gated))) if _int32(K, N, group, int(gated)) else 0
 
 
 class W4Weights:
@@ -961,7 +966,8 @@ def moe_w4_pack_weights(q: torch.Tensor, scales: torch.Tensor, zeros: Optional[t
     if w_layout == MOE_W_LAYOUT_NK:
         shape, small = shape[::-1], small[::-1]
     fits = (q.shape == shape and q.dtype == torch.uint8 and q.is_contiguous() and scales.shape == small and scales.is_contiguous() and
-            (zeros is None or (zeros.shape == small and zeros.dtype == torch.uint8 and zeros.is_contiguous())) and _here(q, scales, zeros, W.codes))
+            (zeros is None or (zeros.shape == small and zeros.dtype == torch.uint8 and zeros.is_contiguous())) and _here(q, scales, zeros, W.codes) and
+            _int32(w_layout))
     rc = MOE_ERR_INVALID_ARG
     if fits:
         rc = lib().moe_w4_pack_weights(_ptr(q), _ptr(scales), _ptr(zeros), _SCALE_DTYPES.get(scales.dtype, -1), w_layout, W.K, W.N, W.group, int(W.gated),

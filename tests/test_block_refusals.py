@@ -123,3 +123,80 @@ def test_bindings_refuse_what_does_not_fit():
                  lambda: mb.MoeFp8LayerPlan(4, 2, 8, 130, 128, "cpu")):
         with pytest.raises(mb.MoeError):
             make()
+
+
+class _OnCard(torch.Tensor):
+    """A tensor of the host that says it is on the first card, for calls that are looked at before they reach one."""
+
+    def get_device(self):
+        return 0
+
+
+def _card(*shape, dtype=torch.float32):
+    return torch.Tensor._make_subclass(_OnCard, torch.empty(*shape, dtype=dtype))
+
+
+class _Listener:
+    """In the library's place: notes the calls that would have launched something, with what their descriptions hold."""
+
+    def __init__(self):
+        self.calls = []
+
+    def __getattr__(self, name):
+        sizes = {"moe_w4_code_bytes", "moe_w4_word_bytes", "moe_strerror"}
+        if name in sizes:
+            return getattr(self.library, name)
+
+        def call(*args):
+            fields = [{n: getattr(a._obj, n) for n, _ in a._obj._fields_} for a in args if hasattr(a, "_obj")]
+            self.calls.append((name, args, fields[0] if fields else None))
+            return OK
+        return call
+
+
+@pytest.fixture
+def listener(monkeypatch):
+    there = _Listener()
+    there.library = mb.lib()
+    monkeypatch.setattr(mb, "_lib", there)
+    monkeypatch.setattr(mb, "_current_device", lambda: 0)
+    monkeypatch.setattr(mb, "_stream_at", lambda device: 0)
+    monkeypatch.setattr(mb, "_stream", lambda: 0)
+    return there
+
+
+MANY = 1 << 32
+
+
+@pytest.mark.parametrize("K,N,group", [(MANY + 64, 32, 32), (64, MANY + 32, 32), (64, 32, MANY + 32), (MANY + 64, MANY + 32, MANY + 32), (64 - MANY, 32, 32), (64, 32 - MANY, 32)])
+def test_weights_of_sizes_beyond_32_bits(K, N, group):
+    """Sizes that are others once they are cut off at 32 bits."""
+    with pytest.raises(mb.MoeError):
+        mb.W4Weights(K, N, group, device="cpu")
+    assert mb.moe_w4_word_bytes(K, N, group) == 0
+    assert mb.moe_w4_code_bytes(K, N) == (0 if (K, N) != (64, 32) else 2 * 1024)
+    with pytest.raises(mb.MoeError):
+        mb.W4Weights(64, 32, 32, MANY, "cpu")        # (true, and 0 where it is cut off)
+
+
+@pytest.mark.parametrize("kw", [dict(groups=MANY + 4), dict(kept=MANY + 2), dict(group_score=MANY), dict(score=MANY + 1), dict(groups=4 - MANY), dict(kept=2 - MANY)])
+def test_options_beyond_32_bits(listener, kw):
+    good = dict(groups=4, kept=2)
+    args = _card(4, 8), 2, _card(4, 2, dtype=torch.int32), _card(4, 2)
+    assert mb.moe_route_grouped(*args, **good) == OK and len(listener.calls) == 1
+    assert mb.moe_route_grouped(*args, **{**good, **kw}, check=False) == INVALID and len(listener.calls) == 1
+
+
+def test_choices_beyond_32_bits(listener):
+    """No tokens, so that the product of tokens and choices says nothing."""
+    args = _card(0, 2), _card(0, 2, dtype=torch.int32), _card(0, 2)
+    assert mb.moe_route_grouped(args[0], 2, *args[1:], 1, 1) == OK and len(listener.calls) == 1
+    assert mb.moe_route_grouped(args[0], MANY + 2, *args[1:], 1, 1, check=False) == INVALID and len(listener.calls) == 1
+
+
+def test_layout_beyond_32_bits(listener):
+    W = mb.W4Weights(64, 32, 32, device="cpu")
+    W.codes, W.words = _card(W.codes.numel(), dtype=torch.uint8), _card(W.words.numel(), dtype=torch.uint8)
+    args = _card(64, 32, dtype=torch.uint8), _card(2, 32, dtype=torch.float16), None
+    assert mb.moe_w4_pack_weights(*args, mb.MOE_W_LAYOUT_KN, W) == OK and len(listener.calls) == 1
+    assert mb.moe_w4_pack_weights(*args, MANY + mb.MOE_W_LAYOUT_NK, W, check=False) == INVALID and len(listener.calls) == 1
