@@ -200,3 +200,22 @@ def test_layout_beyond_32_bits(listener):
     args = _card(64, 32, dtype=torch.uint8), _card(2, 32, dtype=torch.float16), None
     assert mb.moe_w4_pack_weights(*args, mb.MOE_W_LAYOUT_KN, W) == OK and len(listener.calls) == 1
     assert mb.moe_w4_pack_weights(*args, MANY + mb.MOE_W_LAYOUT_NK, W, check=False) == INVALID and len(listener.calls) == 1
+
+
+def test_what_a_description_holds_is_what_the_call_was_given(listener):
+    """Descriptions are kept for each combination of values; a number that a tensor holds may be another one at the next call."""
+    scale, renormalize, k, score, eps = torch.tensor(2.5), torch.tensor(True), torch.tensor(2), torch.tensor(0), torch.tensor(0.5)
+    for turn in range(2):
+        mb.moe_route_grouped(_card(4, 8), k, _card(4, 2, dtype=torch.int32), _card(4, 2), 4, 2, score=score, renormalize=renormalize, scale=scale)
+        d = listener.calls[-1][2]
+        assert (d["scale"], bool(d["renormalize"]), d["k"], d["score"]) == (scale.item(), renormalize.item(), k.item(), score.item())
+        mb.moe_add_norm(_card(4, 8), None, eps, y=_card(4, 8, dtype=torch.bfloat16))
+        assert listener.calls[-1][2]["eps"] == eps.item()
+        scale.fill_(0.75), renormalize.fill_(False), k.fill_(1), score.fill_(1), eps.fill_(0.25)
+    K = torch.tensor(64)
+    W = mb.W4Weights(K, torch.tensor(32), torch.tensor(32), device="cpu")
+    W.codes, W.words = _card(W.codes.numel(), dtype=torch.uint8), _card(W.words.numel(), dtype=torch.uint8)
+    mb.moe_w4_matvec(_card(4, 64, dtype=torch.bfloat16), W, _card(4, 32, dtype=torch.bfloat16))
+    K.fill_(96)
+    assert W.K == 64
+    assert mb.moe_w4_matvec(_card(4, 96, dtype=torch.bfloat16), W, _card(4, 32, dtype=torch.bfloat16), check=False) == INVALID
