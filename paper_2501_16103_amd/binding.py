@@ -1097,6 +1097,10 @@ class MoeLayerPlan:
         return self.out
 
 
+# What e4m3 weights are held as (the other types of a byte are other values).
+_E4M3_BYTES = (torch.uint8, torch.int8, torch.float8_e4m3fn)
+
+
 class MoeFp8LayerPlan:
     """Buffers and tilings of one MoE feed-forward layer over fp8 weights, tokens and activations (each row of them with a scale):
 
@@ -1129,7 +1133,7 @@ class MoeFp8LayerPlan:
             raise MoeError(MOE_ERR_INVALID_ARG, where)
         _contiguous(where, W_gate_up, (E, self.hidden, 2 * self.inter))
         _contiguous(where, W_down, (E, self.inter, self.hidden))
-        if W_gate_up.element_size() != 1 or W_down.element_size() != 1:
+        if W_gate_up.dtype not in _E4M3_BYTES or W_down.dtype not in _E4M3_BYTES:
             raise MoeError(MOE_ERR_INVALID_ARG, where)
         _contiguous(where, up_scale, (E,), torch.float32)
         _contiguous(where, down_scale, (E,), torch.float32)

@@ -137,3 +137,18 @@ def test_plan_refuses():
                 dict(up_scale=up_scale[:7]), dict(down_scale=down_scale.double()), dict(topk_ids=ids.long()), dict(topk_ids=ids[:2]), dict(topk_weights=w.cpu())):
         with pytest.raises(mb.MoeError):
             b.plan.forward(**{**good, **bad})
+
+
+@pytest.mark.parametrize("other", [torch.float8_e5m2, torch.float8_e4m3fnuz, torch.bool])
+def test_plan_refuses_other_types_of_a_byte(other):
+    """Weights whose elements are a byte but not e4m3: read as that they would give another product."""
+    b = _Block(3, 2, 8, 256, 128, 4, 2, 51)
+    _, _, _, up, up_scale, down, down_scale = b.gpu
+    ids, w = torch.zeros(3, 2, dtype=torch.int32, device=DEV), torch.ones(3, 2, device=DEV)
+    b.plan.rows.quantize(b.xg)
+    want = b.plan.forward(b.plan.rows, up, up_scale, down, down_scale, ids, w).clone()
+    for same in (torch.float8_e4m3fn, torch.int8):
+        assert torch.equal(b.plan.forward(b.plan.rows, up.view(same), up_scale, down.view(same), down_scale, ids, w), want)
+    for up_type, down_type in ((other, torch.uint8), (torch.uint8, other)):
+        with pytest.raises(mb.MoeError):
+            b.plan.forward(b.plan.rows, up.view(up_type), up_scale, down.view(down_type), down_scale, ids, w)
