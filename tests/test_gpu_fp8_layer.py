@@ -152,3 +152,49 @@ def test_plan_refuses_other_types_of_a_byte(other):
     for up_type, down_type in ((other, torch.uint8), (torch.uint8, other)):
         with pytest.raises(mb.MoeError):
             b.plan.forward(b.plan.rows, up.view(up_type), up_scale, down.view(down_type), down_scale, ids, w)
+
+
+def _bytes(seed, *shape):
+    """e4m3 bytes of random numbers, drawn on the GPU, an expert at a time."""
+    g = torch.Generator(device=DEV).manual_seed(seed)
+    out = torch.empty(shape, dtype=torch.uint8, device=DEV)
+    for e in range(shape[0]):
+        out[e] = (torch.randn(shape[1:], generator=g, device=DEV) * 100.0).clamp(-448, 448).to(torch.float8_e4m3fn).view(torch.uint8)
+    return out
+
+
+@pytest.mark.parametrize("T,k,E,hidden,inter", [(1, 6, 64, 2048, 1408), (128, 6, 64, 2048, 1408), (1024, 6, 64, 2048, 1408), (1, 2, 8, 4096, 14336), (128, 2, 8, 4096, 14336)])
+def test_layer_at_full_size(T, k, E, hidden, inter):
+    """A few rows of three experts and all sums, each step from what the step before it wrote."""
+    g = torch.Generator().manual_seed(T + E)
+    up, down = _bytes(1, E, hidden, 2 * inter), _bytes(2, E, inter, hidden)
+    up_scale, down_scale = ((0.5 + torch.rand(E, generator=g)) * (0.01 * n ** -0.5) for n in (hidden, inter))
+    x = torch.randn(T, hidden, generator=g).to(BF16)
+    ids = torch.stack([torch.randperm(E, generator=g)[:k] for _ in range(T)]).to(torch.int32)
+    weights = torch.rand(T, k, generator=g)
+    plan = mb.MoeFp8LayerPlan(T, k, E, hidden, inter, DEV)
+    plan.rows.quantize(x.to(DEV))
+    plan.forward(plan.rows, up, up_scale.to(DEV), down, down_scale.to(DEV), ids.to(DEV), weights.to(DEV))
+    codes, scales = plan.rows.codes.cpu().view(torch.float8_e4m3fn).double(), plan.rows.scales.cpu().double()
+    act_codes, act_scales = plan.act_rows.codes.cpu().view(torch.float8_e4m3fn).double(), plan.act_rows.scales.cpu()
+    flat, act, out = ids.reshape(-1).long(), plan.act.cpu(), plan.down.cpu()
+    assert torch.equal(act_scales, (act.float().abs().amax(1) / 448.0).clamp(min=2.0 ** -126))
+    v = act.double() / act_scales.double()[:, None]
+    assert bool(((act_codes - v).abs() <= ref.half_step(v) * (1 + 2.0 ** -20) + v.abs() * 2.0 ** -22).all())
+    used = torch.unique(flat)
+    for e in used[torch.linspace(0, len(used) - 1, 3).long()].unique().tolist():
+        rows = torch.nonzero(flat == e).squeeze(1)
+        rows = rows[torch.linspace(0, len(rows) - 1, 3).long().unique()]
+        cols = torch.randperm(inter, generator=g)[:200]
+        w = up[e].cpu().view(torch.float8_e4m3fn)[:, torch.cat([cols, inter + cols])].double()
+        a, factor = codes[rows // k], scales[rows // k, None] * float(up_scale[e])
+        s, off = a @ w * factor, H.fp8_adder_bound(a.float(), w.float()) * factor
+        (gate, u), (dg, du) = s.chunk(2, dim=1), off.chunk(2, dim=1)
+        f = ref.silu(gate)
+        _near(act[rows][:, cols], f * u, 1.1 * dg * (u.abs() + du) + f.abs() * du + (f * u).abs() * 100 * 2.0 ** -24)   # (as in test_block)
+        cols = torch.randperm(hidden, generator=g)[:200]
+        w = down[e].cpu().view(torch.float8_e4m3fn)[:, cols].double()
+        a, factor = act_codes[rows], act_scales[rows, None].double() * float(down_scale[e])
+        _near(out[rows][:, cols], a @ w * factor, H.fp8_adder_bound(a.float(), w.float()) * factor + (a @ w * factor).abs() * 4 * 2.0 ** -24)
+    parts = out.double().reshape(T, k, hidden) * weights.double()[..., None]
+    _near(plan.out, parts.sum(1), parts.abs().sum(1) * (k + 1) * 2.0 ** -24)

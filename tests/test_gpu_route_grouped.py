@@ -182,3 +182,20 @@ def test_captured_and_on_a_stream():
         torch.cuda.synchronize()
         want, weights = ref.route_grouped(x, 8, 8, 4, True, bias, True, True, 1.0)
         assert torch.equal(ids.cpu(), want) and torch.allclose(w.cpu().double(), weights, rtol=1.01 * 2.0 ** -24, atol=0)
+
+
+def test_on_a_stream_of_its_own():
+    """What a call on another stream than the default one writes, behind inputs that are made there."""
+    x, bias = _inputs(70, 256, 22, torch.float32, "normal")
+    ids, w = torch.full((70, 8), -7, dtype=torch.int32, device=DEV), torch.full((70, 8), 7.0, device=DEV)
+    xg, bg = torch.zeros(70, 256, device=DEV), bias.to(DEV)
+    late = x.to(DEV)
+    torch.cuda.synchronize()
+    s = torch.cuda.Stream()
+    with torch.cuda.stream(s):
+        torch.cuda._sleep(1 << 22)
+        xg.copy_(late)
+        mb.moe_route_grouped(xg, 8, ids, w, 8, 4, mb.MOE_GROUP_TOP2, bg, mb.MOE_SCORE_SIGMOID)
+    s.synchronize()
+    want, weights = ref.route_grouped(x, 8, 8, 4, True, bias, True, True, 1.0)
+    assert torch.equal(ids.cpu(), want) and torch.allclose(w.cpu().double(), weights, rtol=1.01 * 2.0 ** -24, atol=0)

@@ -162,6 +162,22 @@ def test_the_same_every_time_and_for_every_number_of_tokens():
         assert torch.equal(whole, again)
 
 
+@pytest.mark.parametrize("K,N,gated", [(4096, 256, True), (520, 4096, False), (1024, 5632, False), (640, 12304, False), (384, 14336, False), (640, 16400, False), (300, 16420, True)])
+def test_a_token_has_the_same_bits_whatever_their_number(K, N, gated):
+    """All forms of a token count (up to 4, 8 and 16) and of a workgroup's columns, those that change with the token count among them."""
+    q, s, z = _weight(K, N, 64, 21)
+    x = _tokens(16, K, 22).to(DEV)
+    W = _packed(q, s, z, 64, gated)
+    n = N // 2 if gated else N
+    whole = torch.empty(16, n, dtype=BF16, device=DEV)
+    mb.moe_w4_matvec(x, W, whole)
+    for T in (1, 4, 5, 8, 9, 15):
+        for first in (0, 16 - T):
+            out = torch.empty(T, n, dtype=BF16, device=DEV)
+            mb.moe_w4_matvec(x[first: first + T], W, out)
+            assert torch.equal(out, whole[first: first + T])
+
+
 def test_no_tokens():
     q, s, z = _weight(64, 16, 32, 18)
     assert mb.moe_w4_matvec(torch.empty(0, 64, dtype=BF16, device=DEV), _packed(q, s, z, 32, False), torch.empty(0, 16, dtype=BF16, device=DEV)) == mb.MOE_OK
