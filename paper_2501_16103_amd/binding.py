@@ -11,6 +11,7 @@ from __future__ import annotations
 import ctypes
 import os
 from dataclasses import dataclass
+from numbers import Number
 from operator import index
 from typing import Optional
 
@@ -575,7 +576,7 @@ def moe_route(logits: torch.Tensor, k: int, topk_ids: torch.Tensor, topk_weights
     # (as _holds does it; a token's call is its host side)
     if (topk_ids.numel() >= n and topk_weights.numel() >= n and topk_ids.dtype is torch.int32 and topk_weights.dtype is torch.float32 and
             topk_ids.is_contiguous() and topk_weights.is_contiguous() and (step == 1 or E <= 1)):
-        d = moe_route_desc(T, k, E, _DTYPES.get(logits.dtype, -1), row, score, renormalize, scale)
+        d = moe_route_desc(T, k, E, _DTYPES.get(logits.dtype, -1), row, score, bool(renormalize), scale)
         rc = lib().moe_route(logits.data_ptr(), ctypes.byref(d), topk_ids.data_ptr(), topk_weights.data_ptr(), _stream())
     if check and rc != MOE_OK:
         raise MoeError(rc, "moe_route")
@@ -837,10 +838,12 @@ _descriptions: dict = {}
 
 
 def _described(kind, *fields):
-    """A pointer to kind(*fields).  Fields are numbers: of a tensor that holds one the description would be kept by the tensor, whatever it holds by then."""
-    if len(_descriptions) >= _MOST_DESCRIPTIONS:
-        _descriptions.clear()
-    d = _descriptions[(kind, *fields)] = ctypes.byref(kind(*fields))
+    """A pointer to kind(*fields), kept for the next call with the same numbers.  With a tensor that holds one it is not: what it holds may change."""
+    d = ctypes.byref(kind(*fields))
+    if all(isinstance(f, Number) for f in fields):
+        if len(_descriptions) >= _MOST_DESCRIPTIONS:
+            _descriptions.clear()
+        _descriptions[(kind, *fields)] = d
     return d
 
 
@@ -849,7 +852,6 @@ def moe_route_grouped(logits: torch.Tensor, k: int, topk_ids: torch.Tensor, topk
                       scale: float = 1.0, check: bool = True) -> int:
     """moe_route among the experts of the `kept` best of `groups` groups, by score + bias (fp32 [E])."""
     T, E = logits.shape
-    k, score = index(k), index(score)
     row, step = logits.stride()
     n, at = T * k, logits.get_device()
     rc = MOE_ERR_INVALID_ARG
@@ -858,7 +860,7 @@ def moe_route_grouped(logits: torch.Tensor, k: int, topk_ids: torch.Tensor, topk
             (bias is None or (_holds(bias, E, torch.float32) and bias.get_device() == at)) and
             topk_ids.get_device() == at and topk_weights.get_device() == at and at >= 0 and at == _current_device() and
             (n | E | k | groups | kept | group_score | score) >> 31 == 0):
-        fields = (moe_route_desc, T, k, E, _DTYPES.get(logits.dtype, -1), row, score, bool(renormalize), float(scale))
+        fields = (moe_route_desc, T, k, E, _DTYPES.get(logits.dtype, -1), row, score, bool(renormalize), scale)
         rc = (_lib or lib()).moe_route_grouped(logits.data_ptr(), None if bias is None else bias.data_ptr(), _descriptions.get(fields) or _described(*fields),
                                                groups, kept, group_score, topk_ids.data_ptr(), topk_weights.data_ptr(), _stream_at(at))
     if check and rc != MOE_OK:
@@ -926,7 +928,7 @@ def moe_add_norm(x: torch.Tensor, weight: Optional[torch.Tensor], eps: float, re
         codes, scales = out.data_ptr(), rows.scales.data_ptr()
     rc = MOE_ERR_INVALID_ARG
     if fits:
-        fields = (moe_norm_desc, T, x_row, r_row, H, x_type, r_type, w_type, float(eps))
+        fields = (moe_norm_desc, T, x_row, r_row, H, x_type, r_type, w_type, eps)
         rc = (_lib or lib()).moe_add_norm(x.data_ptr(), r, w, _descriptions.get(fields) or _described(*fields), r_out, y_at, codes, scales, _stream_at(at))
     if check and rc != MOE_OK:
         raise MoeError(rc, "moe_add_norm")
