@@ -600,6 +600,8 @@ size_t moe_few_tokens_workspace_bytes(const moe_few_tokens_desc* desc);
  * the softmax, its weight is 0, and it is chosen only where the groups that stay have fewer than k others (by rising index, after them); a group
  * of nothing else comes after all others.  A row of nothing but masked experts has ids 0 .. k-1 and weights 0.  A NaN score counts as larger than
  * every number; a NaN or +inf logit in a softmax row makes all its scores NaN.  With one group and no bias these are moe_route's choices.
+ * (In 64 bits a softmax's p is 0 where the logit is more than 745 below the row's largest, and has lost bits where it is more than 708 below: a bias can make all of a
+ * row's choices such ones, and where all are 0, so are the weights.)
  * logits, desc, topk_ids, topk_weights: as for moe_route.  groups divides E, 1 <= kept <= groups, k <= kept * (E / groups), else
  * MOE_ERR_INVALID_ARG; groups <= 64, else MOE_ERR_UNSUPPORTED.  Deterministic.
  */
@@ -663,8 +665,9 @@ size_t moe_w4_word_bytes(int K, int N, int group, int gated);
  *   add    DEVICE bf16, of out's shape, or NULL; may be out itself
  *   out    DEVICE bf16 [T][N], or [T][N / 2] of gated weights; overlaps X nowhere
  * Products are exact, sums, activation and addition fp32, one rounding to bf16.  A sum over a group of q - z is formed as one over 128 + q less one of
- * 128 + z: it is off by about 2^-24 of 144 times the sum of |X| there.  An infinity or NaN in a token's X makes all its outputs NaN; tokens do not
- * touch each other.  T <= 16, else MOE_ERR_UNSUPPORTED; T = 0 does nothing.  Deterministic.
+ * 128 + z: it is off by about 2^-24 of 144 times the sum of |X| there, and that sum has to stay below 2^119 (beyond, fp32 overflows, and outputs may be infinite
+ * or NaN).  An infinity or NaN in a token's X makes all its outputs NaN; tokens do not touch each other, and a token's outputs are the same bits whatever T is.
+ * T <= 16, else MOE_ERR_UNSUPPORTED; T = 0 does nothing.  Deterministic.
  */
 typedef struct moe_w4_desc {
     int32_t T, K, N;

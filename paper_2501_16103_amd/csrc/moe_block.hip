@@ -41,9 +41,11 @@ int launch_grouped(const GroupedRouteArgs& a, bool f32, int32_t* ids, float* wei
 
 constexpr int kNormCols = 65536;
 
-// Pieces of eight elements a thread: one up to 256 pieces, two beyond, with as many threads as that takes; more only where 1024 threads are too few.  us, one / two /
-// four: norm with both outputs, bf16, 1 row of 2048 2.5 / 2.9 / 3.4, of 7168 3.9 / 3.8 / 4.9, 4096 rows of 2048 18.3 / 19.5 / 20.4, of 7168 51.0 / 48.6 / 49.4, 777 of 3584
-// with an fp32 residual 11.3 / 11.8 / 12.0; rows alone, 8192 of 1408 9.6 / 9.4 / 9.1 (the side that loses), of 4096 20.7 / 19.5 / 19.7, of 14336 - / 61.3 / 63.2.
+// Pieces of eight elements a thread: one up to 256 pieces, two beyond, with as many threads as that takes; more only where 1024 threads are too few.  us, inputs and outputs of up to
+// 40 calls in turn, one / two / four / eight: norm with all outputs, bf16, 1 row of 2048 2.4 / 2.8 / 3.2, of 7168 - / 3.8 / 4.0, 4096 rows of 2048 17.5 / 18.5 / 19.3, of 7168 - / 48.8 / 49.0,
+// 777 of 3584 with an fp32 residual - / 11.8 / 12.3, 1024 of 32768 - / - / 71.6 / 83.7, of 65536 - / - / - / 169.5; rows alone, 8192 of 4096 - / 19.7 / 19.9, of 14336 - / 61.0 / 63.5, 1024 of
+// 32768 - / - / 21.5 / 21.3.  Where the side taken loses: rows alone, 8192 of 1408 9.6 / 9.1 / 8.8; 2529 of 5144 with a residual - / 30.1 / 29.3, without one - / 22.1 / 20.0 (5143: 34.9 / 32.7
+// and 25.0 / 22.4); 1024 of 16384, workgroups of 1024 against 512 threads, - / 41.6 / 35.9.
 template <class X, class R, class W, bool ENDS>
 int launch_norm_rows(NormArgs a, int64_t rows, hipStream_t s) {
     if (a.cols + 14 >= kNormCols + 8) a.in_step = 0;   // (a piece more than the largest launch has)
@@ -86,14 +88,21 @@ int check_w4(int K, int N, int group, int gated) {
 int64_t w4_tiles(int K, int N, int gated) { return w4_tiles_n(N, gated) * w4_tiles_k(K); }
 
 // Tiles of columns a workgroup takes, and wavefronts that share K.  One tile while that gives about a workgroup per CU, with up to sixteen wavefronts of two
-// tiles along K at least; two beyond, with eight; four with four wavefronts from four rounds of single tiles on, where what counts is that tokens and
-// a workgroup's start serve more weights, and with eight from three on where tokens are many.  us, T = 1 / 16, one, two, four tiles of columns:
-//   4096 -> 4096 (256 tiles)    3.7, -, - / -;  eight and sixteen wavefronts 3.7 and 3.7;  14336 -> 4096 10.0 and 7.5 / 12.1 and 12.7
-//   4096 -> 5632 (352)          4.6, 4.5, - / 7.1, 5.4, -
-//   4096 -> 14336 (896)         8.2, 7.4, 7.5 / 12.2, 10.1, 8.7
-//   4096 -> 20480 (1280)        -, 9.8, 11.0 / -, 14.8, 14.8  (four lose a tenth here for one token);  eight wavefronts 12.2, 12.4 / 13.8, 15.5
-//   4096 -> 28672 gated (1792)  -, 13.3, 12.7 / -, 18.5, 15.3;  eight wavefronts 13.5, 13.6 / 18.3, 16.6
-//   gated 7168 -> 2816 (176)    -, 6.1, - with eight wavefronts, 5.7 with sixteen;  2048 -> 2816 3.4 with eight, 3.5 with sixteen
+// tiles along K at least; two beyond, with eight where there are more workgroups than CUs; four with four wavefronts from four rounds of single tiles on, where what counts is that tokens
+// and a workgroup's start serve more weights, and with eight from three on where tokens are many.  us, T = 1 / 4 / 8 / 16, weights of 640 MB in turn, so that they come from memory, tiles
+// of columns x wavefronts, what is taken first:
+//   4096 -> 4096 (256 tiles)    1 x 16 4.0 / 4.1 / 4.4 / 5.6;  1 x 8 4.6 / 4.7 / 4.8 / 5.4;  2 x 16 4.7 / 4.8 / 5.4 / 6.2
+//   14336 -> 4096               1 x 16 7.7 / 7.9 / 9.4 / 13.2;  1 x 8 10.4 / 10.5 / 10.9 / 12.5;  2 x 16 10.5 / 11.0 / 12.7 / 15.6
+//   4096 -> 5632 (352)          2 x 16 4.8 / 5.0 / 5.6 / 6.4;  2 x 8 5.3 / 5.3 / 5.5 / 6.3;  1 x 8 5.1 / 5.1 / 6.0 / 8.1
+//   4096 -> 14336 (896)         T <= 8 2 x 8 7.4 / 7.6 / 8.8, 16 4 x 8 8.9;  4 x 8 7.5 / 7.6 / 7.8, 2 x 8 10.4;  4 x 4 9.0 / 9.0 / 9.4 / 10.1
+//   4096 -> 16384 (1024)        4 x 4 9.2 / 9.3 / 9.6 / 10.3;  2 x 8 7.8 / 7.7 / 8.9 / 10.3;  4 x 8 8.1 / 8.1 / 8.2 / 9.1
+//   4096 -> 20480 (1280)        4 x 4 10.8 / 11.1 / 12.2 / 14.7;  2 x 4 9.7 / 9.9 / 11.1 / 14.8;  2 x 8 12.2 / 12.4 / 11.5 / 13.7;  4 x 8 12.3 / 12.5 / 13.3 / 15.5
+//   4096 -> 24576 (1536)        4 x 4 11.2 / 11.5 / 12.4 / 14.9;  2 x 4 10.9 / 11.0 / 11.2 / 14.8;  2 x 8 12.3 / 12.6 / 12.4 / 14.7
+//   4096 -> 28672 gated (1792)  4 x 4 12.6 / 12.7 / 13.0 / 15.2;  2 x 4 13.1 / 13.3 / 15.1 / 18.1;  4 x 8 13.4 / 13.3 / 14.0 / 16.6
+//   gated 7168 -> 2816 (176)    2 x 16 6.1 / 6.3 / 7.6 / 9.0;  2 x 8 6.8 / 6.9 / 7.2 / 8.5
+//   gated 2048 -> 2816          2 x 8 3.7 / 3.8 / 4.0 / 4.5;  2 x 4 4.8 / 4.9 / 5.0 / 5.2;  4 x 8 4.6 / 4.7 / 4.9 / 5.5
+// The side taken loses with 1024 to 1536 tiles (up to a sixth at 1024, a tenth at 1280, a fiftieth to a tenth at 1536), with 768 to 1023 at eight tokens (an eighth), and with sixteen wavefronts at eight
+// to sixteen tokens (a twentieth).  Weights that the last-level cache holds take 0.4 to 2.8 less, and order the sides alike but for 1 x 16, which does not lose then.
 template <int NT, int TR, int PER, bool GATED>
 int launch_w4(const W4Args& a, hipStream_t s) {
     const int grid = (a.tiles_n + NT - 1) / NT, most = a.tiles_n >= 4 * kCus ? 4 : grid > kCus || NT == 4 ? 8 : 16;
@@ -133,6 +142,8 @@ int moe_route_grouped(const void* logits, const float* bias, const moe_route_des
                                 group_score == MOE_GROUP_TOP2, d->renormalize != 0, d->scale};
     const hipStream_t s = static_cast<hipStream_t>(stream);
     const bool f32 = d->dtype == MOE_DTYPE_FP32;
+    // Experts a lane; us, sigmoid, bias, sums of two, 8 chosen, 1 / 700 / 4096 tokens: 512 experts in 8 groups (8 a lane) 5.0 / 5.8 / 9.0; 576 in 8 (9) 7.8 / 9.4 / 35.2, 1024 in 8 (16) 7.6 / 8.6 / 31.3;
+    // 1000 in 40 (25) 22.4 / 26.5 / 61.4.  Up to 8 take 95 registers at most, 9 to 16 308 and 309, one wavefront a SIMD; beyond 16 (189, two) every choice is made in 64 bits.
     const int per_lane = (each + lanes - 1) / lanes;
     if (per_lane <= 1) return launch_grouped<1>(a, f32, topk_ids, topk_weights, s);
     if (per_lane <= 2) return launch_grouped<2>(a, f32, topk_ids, topk_weights, s);

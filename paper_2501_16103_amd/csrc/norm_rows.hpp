@@ -3,15 +3,18 @@
 //   h = x + residual (rounded to the residual's type, which is what the next block reads);   y = h / sqrt(mean h^2 + eps) * weight
 //   scale = max |y| / 448, at least 2^-126;   code = e4m3(y / scale), to nearest even;   y itself in bf16
 //
-// A row stays in its workgroup's registers between the two things that need all of it, the norm and the largest magnitude.  As y is h * weight
+// A row of up to 32768 elements stays in its workgroup's registers between the two things that need all of it, the norm and the largest magnitude (of longer ones, eight pieces
+// a thread with a weight, what 128 registers do not hold goes to scratch memory: 92 to 632 bytes a thread).  As y is h * weight
 // times one factor, both come out of one pass: sum h^2 and max |h * weight|, joined over the workgroup in one exchange.
 // A row with an infinity or a NaN (in h or in y) has the scale NaN and codes of NaN.
 //
-// What bounds it: memory, with many rows (4096 rows of 7168 with all outputs, 264 MB, 48.6 us, 5.4 TB/s read and written; 8192 rows of 14336 alone 61.2 us, 5.8 TB/s; a large
-// copy: 5.15); with few the launch and one chain of load, two exchanges and store (one row of 2048: 2.5 us back to back, 6.8 with the call's own time).  Rows of an odd
-// length begin anywhere; with pieces on multiples of eight of the whole tensor all accesses but those at a row's ends are aligned (2529 rows of 5143, bf16 with an fp32 weight,
-// all outputs, 30.7 us, of 5144 29.0; with pieces counted from the row's beginning 43.3).  Elements are held as they are stored, bf16 by
-// twos, until they are used: as floats, 4096 rows of 7168 took 64.6.
+// What bounds it: memory, with many rows (4096 rows of 7168 with all outputs, 264 MB, 48.7 us, 5.4 TB/s read and written; 8192 rows of 14336 alone 61.0 us, 5.8 TB/s; a kernel that
+// only moves the same bytes takes 48.1 and 59.6 with ordinary stores, 45.3 and 57.6 with non-temporal ones); with few the launch and one chain of load, two exchanges and store (one row
+// of 2048: 2.4 us back to back, 6.8 with the call's own time); beyond 32768 columns the scratch memory as well (1024 rows of 32768 with all outputs 71.6 us, 4.2 TB/s, of 65536 169.5, 3.6;
+// 512 of 65536 in fp32 222, 2.3; rows alone, which have no weight and no scratch, 1024 of 65536 43.5, 4.6).  Rows of an odd
+// length begin anywhere; with pieces on multiples of eight of the whole tensor all accesses but those at a row's ends are aligned (2529 rows of 5143, bf16 and a bf16 residual with
+// an fp32 weight, all outputs, 34.9 us, of 5144 30.1; with pieces counted from the row's beginning 37.6).  Elements are held as they are stored, bf16 by
+// twos, until they are used: as floats, 4096 rows of 7168 took 64.6.  (Inputs and outputs of up to 40 calls in turn, from memory.)
 #pragma once
 #include <hip/hip_runtime.h>
 #include <stdint.h>

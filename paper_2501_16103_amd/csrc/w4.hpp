@@ -12,10 +12,11 @@
 // a group's sum begins at -(128 + z) sum x, where sum x is one more column of the product (a weight of ones).  All products are exact; sums are fp32,
 // and about 30 times the rounding of sums over q - z, 2^-19 of a sum's size beside bf16's 2^-9.
 //
-// What bounds it.  One token: memory; 4096 -> 28672 (63 MB) 11.9 us of which a launch is 2, 14336 -> 4096 (33 MB) 7.5, 6 TB/s.  16 tokens: tokens' way into the CUs as well,
-// which every column stripe reads anew: 14336 -> 4096 10.7 us, 117 MB from the second-level caches beside the 33 from memory.  Small weights: the launch
-// (2048 -> 2 x 1408: 3.4 us back to back, 5.4 with the call's own time).  Tiles of one k lie side by side over all columns, which is the order in which a
-// launch reads them; with a stripe's tiles side by side, workgroups in step met the same channels (14336 -> 4096, 16 wavefronts 9.5 us, 8.8 so).
+// What bounds it.  One token: memory; 4096 -> 28672 (63 MB) 12.6 us of which a launch is 2, 14336 -> 4096 (33 MB) 7.7, 5.9 TB/s with weights from memory (what the second-level caches miss is 62.6 and
+// 33.3 MB); 11.7 and 6.9 where the last-level cache holds them.  16 tokens: tokens' way into the CUs as well, which every column stripe reads anew: 14336 -> 4096 13.2 us, 10.4 with cached weights;
+// 153 MB asked of the second-level caches, of which 116 hit (tokens) and 37 come from behind them.  Small weights: the launch
+// (2048 -> 2 x 1408: 3.7 us back to back, 3.3 cached, 5.1 with the call's own time).  Tiles of one k lie side by side over all columns, which is the order in which a
+// launch reads them; with a stripe's tiles side by side, workgroups in step met the same channels (14336 -> 4096, 16 wavefronts, of this kernel at an earlier time, 9.5 us, 8.8 so).
 #pragma once
 #include <hip/hip_runtime.h>
 #include <stdint.h>
